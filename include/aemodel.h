@@ -393,6 +393,78 @@ int model_fold_linear(const void* w, const float* b, int64_t out, int64_t in, co
 int model_fold_embedding(const void* e, int64_t vocab, int64_t d, const void* a, const float* v, int dtype, void* e_out,
                          void* stream);
 
+/* ---- 8-bit products with a scale for each block of 128 ----------------------------------------------------------
+ * A matrix in 8 bits is E4M3 codes of the OCP 8-bit floating point specification (one byte each, NaN = 0x7F / 0xFF, no
+ * infinities, largest value 448) with a binary32 scale for each block; an element is worth scale * value(code).
+ *   AE_FP8_ROWS : a block is 128 consecutive elements of a row; scales [ceil(cols/128)][rows], block by block.
+ *   AE_FP8_TILES: a block is 128 x 128 elements;                scales [ceil(rows/128)][ceil(cols/128)].
+ * Blocks at the end of a row or matrix hold what is left.  Codes are row-major; rows begin on 16-byte borders: the base
+ * address and the row stride ld (bytes) are multiples of 16, and all rows * ld bytes are readable (what lies between a
+ * row's end and the next row is never used).
+ *
+ * model_fp8_quantize  quantises x [rows][cols] (dtype, row stride ldx elements, any alignment of the elements' own):
+ *     scale = max(amax / 448, 2^-126), amax the largest finite magnitude of the block,
+ *     code  = E4M3(x * (1 / scale)), rounded to nearest even, magnitudes over 448 (infinities too) to 448, NaN to NaN;
+ *   quotient, reciprocal and product are correctly rounded binary32 operations, so codes and scales are reproducible.
+ *   q [rows][cols], scale: the codes of x (both nullable together).  qt [cols][rows], scale_t: the codes of the
+ *   transposed matrix (both nullable together): for AE_FP8_ROWS its own blocks of 128 along the rows of x, for
+ *   AE_FP8_TILES the same codes and scales transposed.  Both orientations take one pass over x.
+ * model_fp8_matmul    y[i][j] = bias[j] + sum over blocks c of a_scale[c][i] * b_scale[c; j] * sum over k in c of a[i][k] * b[j][k]:
+ *   a [m][k] in AE_FP8_ROWS, b [n][k] in either form (b_blocks), so that y = a b^T; bias binary32 [n], nullable; y [m][n]
+ *   in dtype, row stride ldy elements.  Sums are binary32 on the matrix cores, scaled block by block, rounded to dtype
+ *   once.  With the codes of x and W (tiles) it is a layer's forward pass; with those of dY and W^T its input gradient;
+ *   with those of dY^T and X^T (rows) its weight gradient.
+ * model_fp8_linear    y = x W^T + bias with x [m][k] in dtype quantised by the call as above (AE_FP8_ROWS) and W [n][k] in
+ *   AE_FP8_TILES: the values are those of model_fp8_quantize followed by model_fp8_matmul.
+ * workspace: the matching _workspace bytes (0 for many shapes: then it may be null), 16-byte aligned; its contents need
+ * not be kept.  Sizes up to 2^31 - 1 each; m or n of zero is no work; k at least 1. */
+enum ae_fp8_blocks { AE_FP8_ROWS = 0, AE_FP8_TILES = 1 };
+int model_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int blocks, void* q, int64_t ldq,
+                       float* scale, void* qt, int64_t ldqt, float* scale_t, void* stream);
+int model_fp8_matmul_workspace(int64_t m, int64_t n, int64_t k, int64_t* bytes);
+int model_fp8_matmul(const void* a, int64_t lda, const float* a_scale, const void* b, int64_t ldb, const float* b_scale,
+                     int b_blocks, const float* bias, int64_t m, int64_t n, int64_t k, int dtype, void* y, int64_t ldy,
+                     void* workspace, void* stream);
+int model_fp8_linear_workspace(int64_t m, int64_t n, int64_t k, int64_t* bytes);
+int model_fp8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* w_scale, const float* bias, int64_t m,
+                     int64_t n, int64_t k, int dtype, void* y, int64_t ldy, void* workspace, void* stream);
+
+/* ---- log probabilities and distillation over a vocabulary --------------------------------------------------------
+ * logits z [rows][vocab] in dtype (row stride ld elements, no alignment beyond the element's own); temperature T > 0:
+ * every row is the distribution q_j = exp(z_j / T - lse), lse = log sum_j exp(z_j / T).  Logits of -infinity are
+ * outcomes that cannot occur.  A row in which all are is empty: its lse and log probabilities are -infinity, its
+ * entropy, loss and gradient zero.  A row that holds a NaN or +infinity gives NaN for its own results only.  All sums
+ * are binary32 or wider; a row's results do not depend on the other rows.  1 <= vocab <= 2^20.
+ *
+ * model_token_logprobs  for every row
+ *   logprob [rows][n_tokens]: log q of the given tokens [rows][n_tokens] (int32); an index outside 0 .. vocab - 1 marks a
+ *     place that is not scored and gets 0.  n_tokens 0 .. 1 024 (then tokens and logprob may be null).
+ *   entropy [rows] = -sum_j q_j log q_j (nullable); lse [rows] (nullable).
+ *   the top_k (0 .. 256, at most vocab) most probable tokens, in the order of falling logits, equal ones by their index,
+ *     NaN last: top_id (int32), top_logit = z, top_logprob = log q, each [rows][top_k] binary32, each nullable.
+ * model_loss_distill    the Kullback-Leibler divergence from a teacher's list of top logits t_i at tokens c_i, and its
+ *   gradient.  top_id [rows][top_k] (int32; an entry outside 0 .. vocab - 1 is no entry, the others of a row are
+ *   distinct), top_logit [rows][top_k] binary32, 1 <= top_k <= vocab.
+ *     teacher_lse null: p_i = exp(t_i / T) / sum over the list, no rest (p_r = 0);
+ *     teacher_lse [rows] (the teacher's lse over its whole vocabulary, at the same T): p_i = exp(t_i / T - teacher_lse),
+ *       p_r = max(0, 1 - sum p_i), the probability of all other tokens as one outcome (left out where the student has
+ *       none: q_r = 0).
+ *     L_r = sum_i p_i (log p_i - log q_{c_i}) + p_r (log p_r - log q_r),  q_r = sum of q_j outside the list;
+ *     dL/dz_j = (P q_j - p_j) / T in the list, q_j (P - p_r / q_r) / T outside, P = sum p_i + p_r.
+ *   loss_rows [rows] = L_r (nullable); loss [1] = sum_r w_r L_r (nullable); d_logits [rows][vocab] in dtype, row stride ldd:
+ *   the gradient of that sum (nullable; it may be logits itself, with the same stride).  weight [rows] (nullable: 1): a
+ *   row whose weight is 0 is not read, its loss and gradient are 0.  A list of one token is the cross entropy with a
+ *   label.  Terms with p = 0 are 0.
+ * workspace: the matching _workspace bytes, 16-byte aligned; its contents need not be kept. */
+int model_token_logprobs_workspace(int64_t rows, int64_t vocab, int top_k, int dtype, int64_t* bytes);
+int model_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, float temperature,
+                         const int* tokens, int n_tokens, int top_k, float* logprob, float* entropy, float* lse, int* top_id,
+                         float* top_logit, float* top_logprob, void* workspace, void* stream);
+int model_loss_distill_workspace(int64_t rows, int64_t vocab, int dtype, int64_t* bytes);
+int model_loss_distill(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, float temperature,
+                       const int* top_id, const float* top_logit, int top_k, const float* teacher_lse, const float* weight,
+                       float* loss_rows, float* loss, void* d_logits, int64_t ldd, void* workspace, void* stream);
+
 /* Measurement aid: TFLOP/s of a loop of nothing but independent 32x32x16 bf16 matrix-core
  * instructions on every compute unit (two workgroups of four wavefronts each, two wavefronts per
  * SIMD), the practical ceiling beside the nominal peak; with lds_reads = 6 each wavefront also reads

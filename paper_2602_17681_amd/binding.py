@@ -23,7 +23,7 @@ SYMBOLS = [
     "model_set_sample_offset", "model_forward", "model_backward", "model_loss_mse", "model_noise",
     "model_pnorm_awgn", "model_gen_bits", "model_count_errors", "model_monte_carlo", "model_num_steps", "model_step_info",
     "model_get_activation", "model_get_conv_output", "model_timing_enable", "model_set_overlap", "model_set_params_static", "model_set_inference", "model_set_recompute", "model_set_fused_backward", "model_calibrate_mfma", "model_mx_quantize", "model_mx_quantize_elem", "model_transform_mse_workspace",
-    "model_transform_mse", "model_transform_mse_elem", "model_transform_mse_static", "model_inverse_shift", "model_lu_workspace", "model_lu_compose", "model_lu_backward", "model_vol_penalty", "model_lu_inverse_workspace", "model_lu_inverse", "model_lu_compose_batch", "model_lu_backward_batch", "model_lu_inverse_batch", "model_lu_timing", "model_qr_workspace", "model_qr_squarings", "model_qr_compose", "model_qr_backward", "model_qr_inverse", "model_fold_workspace", "model_fold_linear", "model_fold_embedding", "model_timing_slots",
+    "model_transform_mse", "model_transform_mse_elem", "model_transform_mse_static", "model_inverse_shift", "model_lu_workspace", "model_lu_compose", "model_lu_backward", "model_vol_penalty", "model_lu_inverse_workspace", "model_lu_inverse", "model_lu_compose_batch", "model_lu_backward_batch", "model_lu_inverse_batch", "model_lu_timing", "model_qr_workspace", "model_qr_squarings", "model_qr_compose", "model_qr_backward", "model_qr_inverse", "model_fold_workspace", "model_fold_linear", "model_fold_embedding", "model_fp8_quantize", "model_fp8_matmul_workspace", "model_fp8_matmul", "model_fp8_linear_workspace", "model_fp8_linear", "model_token_logprobs_workspace", "model_token_logprobs", "model_loss_distill_workspace", "model_loss_distill", "model_timing_slots",
     "model_timing_read", "model_timing_reset", "model_last_error",
 ]
 
@@ -91,6 +91,16 @@ def _load():
     L.model_fold_workspace.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int, i64p]
     L.model_fold_linear.argtypes = [vp, vp, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp, C.c_int64, vp, C.c_int, vp, vp, vp, vp]
     L.model_fold_embedding.argtypes = [vp, C.c_int64, C.c_int64, vp, vp, C.c_int, vp, vp]
+    i64 = C.c_int64
+    L.model_fp8_quantize.argtypes = [vp, i64, i64, i64, C.c_int, C.c_int, vp, i64, vp, vp, i64, vp, vp]
+    L.model_fp8_matmul_workspace.argtypes = [i64, i64, i64, i64p]
+    L.model_fp8_matmul.argtypes = [vp, i64, vp, vp, i64, vp, C.c_int, vp, i64, i64, i64, C.c_int, vp, i64, vp, vp]
+    L.model_fp8_linear_workspace.argtypes = [i64, i64, i64, i64p]
+    L.model_fp8_linear.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, C.c_int, vp, i64, vp, vp]
+    L.model_token_logprobs_workspace.argtypes = [i64, i64, C.c_int, C.c_int, i64p]
+    L.model_token_logprobs.argtypes = [vp, i64, i64, i64, C.c_int, C.c_float, vp, C.c_int, C.c_int, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.model_loss_distill_workspace.argtypes = [i64, i64, C.c_int, i64p]
+    L.model_loss_distill.argtypes = [vp, i64, i64, i64, C.c_int, C.c_float, vp, vp, C.c_int, vp, vp, vp, vp, vp, i64, vp, vp]
     L.model_timing_slots.argtypes = [vp, C.POINTER(C.c_int)]
     L.model_timing_read.argtypes = [vp, C.c_int, C.c_char_p, C.c_int, C.POINTER(C.c_double), i64p,
                                     C.POINTER(C.c_double), C.POINTER(C.c_double)]
@@ -121,6 +131,50 @@ def _ptr(t, dtype=None):
     if dtype is not None:
         assert t.dtype == dtype, (t.dtype, dtype)
     return C.c_void_p(t.data_ptr())
+
+
+def _mat(t, rows, cols, dtype=None):
+    """(data pointer, row stride) of a device matrix whose rows are contiguous; (null, 0) for None."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, "device-resident [%d][%d] matrix required" % (rows, cols)
+    assert dtype is None or t.dtype == dtype, (t.dtype, dtype)
+    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    assert (cols <= 1 or t.stride(1) == 1) and ld >= cols, "rows must be contiguous and must not overlap"
+    return t.data_ptr(), ld
+
+
+def _codes(t, rows, cols):
+    """(data pointer, row stride in bytes) of a matrix of 8-bit codes (float8_e4m3fn or uint8); null for None."""
+    if t is None:
+        return None, 0
+    assert t.dtype == torch.float8_e4m3fn or t.dtype == torch.uint8, t.dtype
+    p, ld = _mat(t, rows, cols)
+    ld = -(-ld // 16) * 16 if rows == 1 else ld     # the stride of a single row plays no part
+    assert rows == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= rows * ld, "all rows * stride bytes must be there"
+    return p, ld
+
+
+def _vec(t, n, dtype=torch.float32):
+    """Data pointer of a contiguous device array of n elements; None for None."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), "contiguous device array of %d %s required" % (n, dtype)
+    return t.data_ptr()
+
+
+def _room(t, nbytes):
+    """Data pointer of a workspace of at least nbytes; None will do where none is needed."""
+    if t is None:
+        assert nbytes == 0, "a workspace of %d bytes is needed" % nbytes
+        return None
+    assert t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes
+    return t.data_ptr()
+
+
+def _dtype_of(t):
+    assert t.dtype == torch.bfloat16 or t.dtype == torch.float32, t.dtype
+    return AE_BF16 if t.dtype == torch.bfloat16 else AE_F32
 
 
 def model_last_error():
@@ -461,6 +515,90 @@ def model_fold_embedding(e, vocab, d, a, v, e_out):
     assert v is None or v.numel() == d
     _check(lib.model_fold_embedding(_ptr(e), vocab, d, _ptr(a), _ptr(None) if v is None else _ptr(v, torch.float32), dtype,
                                     _ptr(e_out), _stream()))
+
+
+FP8_BLOCKS = {"rows": 0, "tiles": 1}
+FP8_BLOCK = 128
+
+
+def _fp8_scales(t, rows, cols, blocks):
+    rb, cb = -(-rows // FP8_BLOCK), -(-cols // FP8_BLOCK)
+    return _vec(t, cb * rows if blocks == "rows" else rb * cb)
+
+
+def model_fp8_quantize(x, rows, cols, blocks, q=None, scale=None, qt=None, scale_t=None):
+    xp, ldx = _mat(x, rows, cols)
+    qp, ldq = _codes(q, rows, cols)
+    tp, ldt = _codes(qt, cols, rows)
+    _check(lib.model_fp8_quantize(xp, rows, cols, ldx, _dtype_of(x), FP8_BLOCKS[blocks], qp, ldq, _fp8_scales(scale, rows, cols, blocks),
+                                  tp, ldt, _fp8_scales(scale_t, cols, rows, blocks), _stream()))
+
+
+def model_fp8_matmul_workspace(m, n, k):
+    b = C.c_int64()
+    _check(lib.model_fp8_matmul_workspace(m, n, k, C.byref(b)))
+    return b.value
+
+
+def model_fp8_matmul(a, a_scale, b, b_scale, b_blocks, bias, m, n, k, y, workspace=None):
+    """y[m][n] = a b^T + bias of 8-bit matrices; a in row blocks, b in row blocks or tiles."""
+    ap, lda = _codes(a, m, k)
+    bp, ldb = _codes(b, n, k)
+    yp, ldy = _mat(y, m, n)
+    _check(lib.model_fp8_matmul(ap, lda, _fp8_scales(a_scale, m, k, "rows"), bp, ldb, _fp8_scales(b_scale, n, k, b_blocks),
+                                FP8_BLOCKS[b_blocks], _vec(bias, n), m, n, k, _dtype_of(y), yp, ldy,
+                                _room(workspace, model_fp8_matmul_workspace(m, n, k)), _stream()))
+
+
+def model_fp8_linear_workspace(m, n, k):
+    b = C.c_int64()
+    _check(lib.model_fp8_linear_workspace(m, n, k, C.byref(b)))
+    return b.value
+
+
+def model_fp8_linear(x, w, w_scale, bias, m, n, k, y, workspace=None):
+    """y[m][n] = x w^T + bias with x quantised by the call and w in tiles."""
+    xp, ldx = _mat(x, m, k)
+    wp, ldw = _codes(w, n, k)
+    yp, ldy = _mat(y, m, n, x.dtype)
+    _check(lib.model_fp8_linear(xp, ldx, wp, ldw, _fp8_scales(w_scale, n, k, "tiles"), _vec(bias, n), m, n, k, _dtype_of(x), yp, ldy,
+                                _room(workspace, model_fp8_linear_workspace(m, n, k)), _stream()))
+
+
+def model_token_logprobs_workspace(rows, vocab, top_k, dtype):
+    b = C.c_int64()
+    _check(lib.model_token_logprobs_workspace(rows, vocab, top_k, dtype, C.byref(b)))
+    return b.value
+
+
+def model_token_logprobs(logits, rows, vocab, tokens, top_k, logprob, entropy, lse, top_id, top_logit, top_logprob, workspace, temperature=1.0):
+    """Log probabilities of given tokens, entropy, log-sum-exp and the top alternatives of every row (each output may be None)."""
+    zp, ld = _mat(logits, rows, vocab)
+    dtype = _dtype_of(logits)
+    assert tokens is None or tokens.dim() == 2, "[rows][n] tokens required"
+    n_tokens = 0 if tokens is None else tokens.shape[1]
+    _check(lib.model_token_logprobs(zp, rows, vocab, ld, dtype, temperature, _vec(tokens, rows * n_tokens, torch.int32), n_tokens, top_k,
+                                    _vec(logprob, rows * n_tokens), _vec(entropy, rows), _vec(lse, rows), _vec(top_id, rows * top_k, torch.int32),
+                                    _vec(top_logit, rows * top_k), _vec(top_logprob, rows * top_k),
+                                    _room(workspace, model_token_logprobs_workspace(rows, vocab, top_k, dtype)), _stream()))
+
+
+def model_loss_distill_workspace(rows, vocab, dtype):
+    b = C.c_int64()
+    _check(lib.model_loss_distill_workspace(rows, vocab, dtype, C.byref(b)))
+    return b.value
+
+
+def model_loss_distill(logits, rows, vocab, top_id, top_logit, loss_rows, loss, d_logits, workspace, teacher_lse=None, weight=None, temperature=1.0):
+    """Divergence from a teacher's top logits and its gradient (loss_rows, loss and d_logits may be None)."""
+    zp, ld = _mat(logits, rows, vocab)
+    gp, ldd = _mat(d_logits, rows, vocab, logits.dtype)
+    dtype = _dtype_of(logits)
+    assert top_id.dim() == 2, "[rows][top_k] lists required"
+    top_k = top_id.shape[1]
+    _check(lib.model_loss_distill(zp, rows, vocab, ld, dtype, temperature, _vec(top_id, rows * top_k, torch.int32), _vec(top_logit, rows * top_k),
+                                  top_k, _vec(teacher_lse, rows), _vec(weight, rows), _vec(loss_rows, rows), _vec(loss, 1), gp, ldd,
+                                  _room(workspace, model_loss_distill_workspace(rows, vocab, dtype)), _stream()))
 
 
 def model_calibrate_mfma(lds_reads, random_data=0, iters=4000):
