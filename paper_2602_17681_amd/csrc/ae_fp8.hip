@@ -284,6 +284,221 @@ __global__ __launch_bounds__(256) void k_fp8_direct(const uint8_t* __restrict__ 
       if (row[i] + e < m) store_out<T>(y + (int64_t)(row[i] + e) * ldy + col, acc[i][e] + bb);
 }
 
+// ---- product of many rows: tiles staged in LDS -----------------------------------------------------------------------
+// A workgroup of WGM x WGN wavefronts makes a tile of BM x BN results, a wavefront 16 MI x 16 NJ of them, in steps of one
+// block (128 codes) of K.  The codes of a step go from memory straight into LDS (16 bytes a lane, a row of 128 in eight
+// pieces) while the step before is multiplied; two such stages.  The first matrix operand is b and the second a, so that a
+// lane's results are four neighbouring columns of one row: the row's scale is one register, and with the order of b's rows
+// below a lane's NJ fragments are 4 NJ columns in a row, which it stores in 16-byte pieces.
+//   piece c of row r lies at piece c ^ key(r) of that row: lanes that read the same piece of eight rows meet eight bank groups
+template <int NJ> __device__ __forceinline__ int b_row(int i, int j) { return (i >> 2) * (4 * NJ) + j * 4 + (i & 3); }   // row of b in fragment j, place i
+__device__ __forceinline__ int a_key(int r) { return r & 7; }
+template <int NJ> __device__ __forceinline__ int b_key(int r) { return (r & 3) | (((r / (4 * NJ)) & 1) << 2); }
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Tiles in an order in which workgroups that run at the same time share rows of a and b: consecutive workgroups go to
+// different dies (8, each with its own L2), so each die takes a contiguous run of tiles, and a run walks columns of 8 tiles.
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int total = tiles_m * tiles_n, xcd = b & 7, per = total >> 3, more = total & 7;
+  const int id = xcd * per + (xcd < more ? xcd : more) + (b >> 3);
+  const int group = 8 * tiles_n, gi = id / group, first = gi * 8, in = id - gi * group;
+  const int height = tiles_m - first < 8 ? tiles_m - first : 8;
+  tm = first + in % height;
+  tn = in / height;
+}
+
+template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ>
+__global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __restrict__ a, int64_t lda, const float* __restrict__ sa,
+                                                             const uint8_t* __restrict__ b, int64_t ldb, const float* __restrict__ sb,
+                                                             const float* __restrict__ bias, int m, int n, int k, T* __restrict__ y,
+                                                             int64_t ldy, int tiles_m, int tiles_n) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  constexpr int NTH = WGM * WGN * 64, NWV = WGM * WGN;
+  constexpr int BM = WGM * MI * 16, BN = WGN * NJ * 16;
+  constexpr int STAGE = (BM + BN) * BLK;                       // bytes of codes of a step
+  constexpr int CB = BN >= BLK ? BN / BLK : 1;                 // column blocks of a tile
+  constexpr int NS = BROWS ? BM + BN : CB * BM;                // scales of a step: rows' and columns', or rows' times the block's
+  constexpr int SPT = (NS + NTH - 1) / NTH;
+  constexpr int LOADS = (BM + BN) / 8 / NWV;                   // a wavefront's instruction moves eight rows
+  static_assert((BM + BN) % (8 * NWV) == 0 && BM % 8 == 0, "whole loads");
+  __shared__ __align__(1024) uint8_t codes[2][STAGE];
+  __shared__ __align__(16) float scales[2][NS];
+  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WGN, wn = wave - wm * WGN;
+  int tm, tn;
+  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int kb = (k + BLK - 1) / BLK;
+
+  // loads: lane l of an instruction moves piece l % 8 of row l / 8 of its eight rows; rows behind the end repeat the last one
+  const uint8_t* abase = a + (int64_t)m0 * lda;
+  const uint8_t* bbase = b + (int64_t)n0 * ldb;
+  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)abase, 0, 0x7FFFFFFF, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)bbase, 0, 0x7FFFFFFF, 0x00020000);
+  unsigned off[LOADS];
+  int piece[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int r8 = (wave * LOADS + i) * 8 + (lane >> 3);       // row among the stage's BM + BN
+    const bool is_a = (wave * LOADS + i) * 8 < BM;
+    const int r = is_a ? r8 : r8 - BM;
+    piece[i] = (lane & 7) ^ (is_a ? a_key(r) : b_key<NJ>(r));
+    const int last = is_a ? m - 1 - m0 : n - 1 - n0;
+    off[i] = (unsigned)((r < last ? r : last) * (is_a ? lda : ldb)) + piece[i] * 16;
+  }
+  auto load_stage = [&](int c, int buf) {
+    const bool tail = (c + 1) * BLK > k;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const bool is_a = (wave * LOADS + i) * 8 < BM;
+      unsigned o = off[i];
+      if (tail && c * BLK + piece[i] * 16 >= k) o = 0x80000000u;                 // behind the rows' end: out of the buffer's range, zeros
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, (lds_void*)(codes[buf] + (wave * LOADS + i) * 1024), 16, o, c * BLK, 0, 0);
+    }
+  };
+  auto load_scales = [&](int c, float (&v)[SPT]) {
+#pragma unroll
+    for (int i = 0; i < SPT; ++i) {
+      const int at = t + i * NTH;
+      if (NS % NTH != 0 && at >= NS) break;
+      if constexpr (BROWS) {
+        const bool is_a = at < BM;
+        const int r = is_a ? m0 + at : n0 + at - BM, end = is_a ? m : n;
+        v[i] = (is_a ? sa : sb)[(int64_t)c * end + (r < end ? r : end - 1)];
+      } else {
+        const int cb = at / BM, r = m0 + at - cb * BM;
+        int blk = n0 / BLK + cb;
+        if (blk > (n - 1) / BLK) blk = (n - 1) / BLK;
+        v[i] = sa[(int64_t)c * m + (r < m ? r : m - 1)] * sb[(int64_t)blk * kb + c];
+      }
+    }
+  };
+  auto store_scales = [&](int buf, const float (&v)[SPT]) {
+#pragma unroll
+    for (int i = 0; i < SPT; ++i) {
+      const int at = t + i * NTH;
+      if (NS % NTH != 0 && at >= NS) break;
+      scales[buf][at] = v[i];
+    }
+  };
+
+  v4f acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = (v4f){0, 0, 0, 0};
+
+  // a lane's two 16-byte pieces of a fragment: 2 g and 2 g + 1 of its row
+  const int arow = wm * MI * 16 + l16;
+  auto frag = [&](const uint8_t* row, int key) {
+    union { uint4 h[2]; v8i v; } u;
+    u.h[0] = *reinterpret_cast<const uint4*>(row + ((2 * g) ^ key) * 16);
+    u.h[1] = *reinterpret_cast<const uint4*>(row + ((2 * g + 1) ^ key) * 16);
+    return make_frag<EXACT>(u.v);
+  };
+  auto multiply = [&](int buf) {
+    const uint8_t* as = codes[buf] + arow * BLK;
+    const uint8_t* bs = codes[buf] + BM * BLK;
+    Frag<EXACT> fb[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = wn * NJ * 16 + b_row<NJ>(l16, j);
+      fb[j] = frag(bs + r * BLK, b_key<NJ>(r));
+    }
+    v4f cs[NJ];
+    if constexpr (BROWS) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) cs[j] = *reinterpret_cast<const v4f*>(&scales[buf][BM + wn * NJ * 16 + g * 4 * NJ + j * 4]);
+    }
+    const float* rs = scales[buf] + (BROWS ? 0 : (wn * NJ * 16 / BLK) * BM) + arow;
+    Frag<EXACT> fa = frag(as, a_key(arow));
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      // the next rows' fragment is on its way while these are multiplied; no more than that, for the registers' sake
+      Frag<EXACT> next = fa;
+      if (i + 1 < MI) next = frag(as + (i + 1) * 16 * BLK, a_key(arow));
+      const float s = rs[i * 16];
+      v4f p[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) p[j] = block_product<EXACT>(fb[j], fa);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[j][e], BROWS ? s * cs[j][e] : s, acc[i][j][e]);
+      fa = next;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // vmcnt(0), then the barrier: everybody's loads of the step are in LDS, and the other stage is no longer read
+  auto arrive = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+  };
+  float sv[SPT];
+  load_scales(0, sv);
+  load_stage(0, 0);
+  store_scales(0, sv);
+  int c = 0;
+  for (; c + 1 < kb; ++c) {
+    arrive();
+    load_scales(c + 1, sv);
+    load_stage(c + 1, (c & 1) ^ 1);
+    multiply(c & 1);
+    store_scales((c & 1) ^ 1, sv);
+  }
+  arrive();
+  if ((k & 15) != 0) {                           // the piece that holds the rows' end: zeros behind it
+    const int cut = (k - c * BLK) >> 4, keep = k & 15;
+    for (int r = t; r < BM + BN; r += NTH) {
+      const int key = r < BM ? a_key(r) : b_key<NJ>(r - BM);
+      uint32_t* w = reinterpret_cast<uint32_t*>(codes[c & 1] + r * BLK + (cut ^ key) * 16);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const int left = keep - 4 * d;
+        w[d] = left >= 4 ? w[d] : left <= 0 ? 0u : w[d] & ((1u << (8 * left)) - 1u);
+      }
+    }
+    __syncthreads();
+  }
+  multiply(c & 1);
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));     // the last sums are formed here: sunk below the stores' branches, their addends need twice the registers
+  // results: lane: row l16 of each 16, columns 4 NJ g .. of the wavefront's
+  const int col = n0 + wn * NJ * 16 + g * 4 * NJ;
+  if (col >= n) return;
+  float bb[4 * NJ];
+#pragma unroll
+  for (int j = 0; j < 4 * NJ; ++j) bb[j] = bias && col + j < n ? bias[col + j] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int row = m0 + arow + i * 16;
+    if (row >= m) continue;
+    T* p = y + (int64_t)row * ldy + col;
+    float o[4 * NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[4 * j + e] = acc[i][j][e] + bb[4 * j + e];
+    if (col + 4 * NJ <= n) {
+      if constexpr (EXACT) {
+        __builtin_memcpy(p, o, sizeof(o));
+      } else {
+        uint32_t w[2 * NJ];
+#pragma unroll
+        for (int j = 0; j < 2 * NJ; ++j) w[j] = pack_bf16(o[2 * j], o[2 * j + 1]);
+        __builtin_memcpy(p, w, sizeof(w));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4 * NJ; ++j)
+        if (col + j < n) store_out<T>(p + j, o[j]);
+    }
+  }
+}
+
 bool sizes_ok(int64_t m, int64_t n, int64_t k) { return m >= 0 && n >= 0 && k >= 1 && m < 0x7FFFFFFF && n < 0x7FFFFFFF && k < 0x7FFFFFFF; }
 bool codes_ok(const void* p, int64_t ld, int64_t cols) { return ((uintptr_t)p & 15) == 0 && ld >= cols && ld % 16 == 0 && ld < ((int64_t)1 << 40); }
 
@@ -306,7 +521,32 @@ int check_product(const char* who, const Product& p) {
   return AE_OK;
 }
 
+template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ>
+int launch_tile(const Product& p, hipStream_t s) {
+  constexpr int BM = WGM * MI * 16, BN = WGN * NJ * 16;
+  const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
+  if (tm * tn > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
+  hipLaunchKernelGGL((k_fp8_tile<T, BROWS, WGM, WGN, MI, NJ>), dim3((unsigned)(tm * tn)), dim3(WGM * WGN * 64), 0, s, p.a, p.lda, p.sa, p.b, p.ldb,
+                     p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tm, (int)tn);
+  return launch_status("fp8_matmul");
+}
+template <typename T, bool BROWS>
+int launch_tiles(const Product& p, hipStream_t s) {
+  const int64_t big = ((p.m + 255) / 256) * ((p.n + 255) / 256);
+  if constexpr (sizeof(T) == 4) {
+    if (((p.m + 255) / 256) * ((p.n + 127) / 128) >= 192) return launch_tile<T, BROWS, 4, 2, 4, 4>(p, s);
+  } else {
+    if (big >= 192) return launch_tile<T, BROWS, 2, 4, 8, 4>(p, s);
+  }
+  return launch_tile<T, BROWS, 2, 2, 4, 4>(p, s);
+}
+
 int launch_product(const Product& p, hipStream_t s) {
+  // offsets inside a tile are 31 bits
+  if (p.m > 64 && p.lda < (1 << 23) && p.ldb < (1 << 23)) {
+    if (p.dtype == AE_BF16) return p.b_blocks == AE_FP8_ROWS ? launch_tiles<bf16_t, true>(p, s) : launch_tiles<bf16_t, false>(p, s);
+    return p.b_blocks == AE_FP8_ROWS ? launch_tiles<float, true>(p, s) : launch_tiles<float, false>(p, s);
+  }
   const int64_t tn = (p.n + 63) / 64, tm = (p.m + 63) / 64;
   if (tn * tm > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
 #define DIRECT(T, R)                                                                                                            \
