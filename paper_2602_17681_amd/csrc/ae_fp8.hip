@@ -6,6 +6,8 @@
 #include <float.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "ae_device.h"
 #include "ae_internal.h"
 
@@ -290,20 +292,39 @@ __global__ __launch_bounds__(256) void k_fp8_direct(const uint8_t* __restrict__ 
 // pieces) while the step before is multiplied; two such stages.  The first matrix operand is b and the second a, so that a
 // lane's results are four neighbouring columns of one row: the row's scale is one register, and with the order of b's rows
 // below a lane's NJ fragments are 4 NJ columns in a row, which it stores in 16-byte pieces.
-//   piece c of row r lies at piece c ^ key(r) of that row: lanes that read the same piece of eight rows meet eight bank groups
+//   piece c of row r lies at piece c ^ key(r) of that row, eight keys among the 16 rows of a fragment, and lane group g reads
+//   pieces g and g + 4 (any order of K will do, as long as it is b's too): 5.8 cycles a read, as for consecutive addresses;
+//   pieces 2 g and 2 g + 1 take 8.0
 template <int NJ> __device__ __forceinline__ int b_row(int i, int j) { return (i >> 2) * (4 * NJ) + j * 4 + (i & 3); }   // row of b in fragment j, place i
-__device__ __forceinline__ int a_key(int r) { return r & 7; }
-template <int NJ> __device__ __forceinline__ int b_key(int r) { return (r & 3) | (((r / (4 * NJ)) & 1) << 2); }
+__device__ __forceinline__ int a_key(int r) { return (r >> 1) & 7; }
+template <int NJ> __device__ __forceinline__ int b_key(int r) { return ((r / (4 * NJ)) & 3) << 1 | ((r >> 1) & 1); }
 
-typedef __attribute__((address_space(3))) void lds_void;
+// 16 bytes of each lane from a buffer straight into LDS: lane l writes at lds + 16 l; offsets past the buffer's range deliver
+// zeros.  In assembly, because the compiler would wait for every such load before the next read of LDS, whichever part
+// of it that reads; the kernel waits itself (vmcnt) where it needs the data.  There is no register result.  (The instruction
+// may read m0 one wait state after it was written, which the compiler does not see here: s_nop.)
+typedef int v4i __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void load_to_lds(v4i rsrc, unsigned lds, unsigned voffset, unsigned soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory", "m0");
+}
+// a raw buffer of `bytes` bytes, 0 to 2^31 - 1, from p on
+__device__ __forceinline__ v4i buffer_of(const void* p, int64_t bytes) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  const int n = bytes <= 0 ? 0 : bytes < 0x7FFFFFFF ? (int)bytes : 0x7FFFFFFF;
+  const v4i r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFF)),
+                 __builtin_amdgcn_readfirstlane(n), 0x00020000};
+  return r;
+}
 
 // Tiles in an order in which workgroups that run at the same time share rows of a and b: consecutive workgroups go to
-// different dies (8, each with its own L2), so each die takes a contiguous run of tiles, and a run walks columns of 8 tiles.
+// different dies (8, each with its own L2), so each die takes a contiguous run of tiles, and a run walks columns of 6 tiles:
+// its 32 tiles at a time read few different rows of a and of b (16 384 x 4 096 x 4 096: 250 us; columns of 4 254, of 8 258).
+constexpr int GROUP = 6;
 __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
   const int total = tiles_m * tiles_n, xcd = b & 7, per = total >> 3, more = total & 7;
   const int id = xcd * per + (xcd < more ? xcd : more) + (b >> 3);
-  const int group = 8 * tiles_n, gi = id / group, first = gi * 8, in = id - gi * group;
-  const int height = tiles_m - first < 8 ? tiles_m - first : 8;
+  const int group = GROUP * tiles_n, gi = id / group, first = gi * GROUP, in = id - gi * group;
+  const int height = tiles_m - first < GROUP ? tiles_m - first : GROUP;
   tm = first + in % height;
   tn = in / height;
 }
@@ -320,8 +341,8 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
   constexpr int CB = BN >= BLK ? BN / BLK : 1;                 // column blocks of a tile
   constexpr int NS = BROWS ? BM + BN : CB * BM;                // scales of a step: rows' and columns', or rows' times the block's
   constexpr int SPT = (NS + NTH - 1) / NTH;
-  constexpr int LOADS = (BM + BN) / 8 / NWV;                   // a wavefront's instruction moves eight rows
-  static_assert((BM + BN) % (8 * NWV) == 0 && BM % 8 == 0, "whole loads");
+  constexpr int LA = BM / 8 / NWV, LB = BN / 8 / NWV, LOADS = LA + LB;      // a wavefront's loads of a step
+  static_assert(BM % (16 * NWV) == 0 && BN % (16 * NWV) == 0 && NJ == 4, "whole loads, keys as the loads assume them");
   __shared__ __align__(1024) uint8_t codes[2][STAGE];
   __shared__ __align__(16) float scales[2][NS];
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
@@ -331,31 +352,32 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
   const int m0 = tm * BM, n0 = tn * BN;
   const int kb = (k + BLK - 1) / BLK;
 
-  // loads: lane l of an instruction moves piece l % 8 of row l / 8 of its eight rows; rows behind the end repeat the last one
-  const uint8_t* abase = a + (int64_t)m0 * lda;
-  const uint8_t* bbase = b + (int64_t)n0 * ldb;
-  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)abase, 0, 0x7FFFFFFF, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)bbase, 0, 0x7FFFFFFF, 0x00020000);
-  unsigned off[LOADS];
-  int piece[LOADS];
+  // loads: an instruction moves eight rows, lane l piece l % 8 (before the keys) of row l / 8; rows behind the end lie
+  // outside the buffer's range and become zeros.  Eight rows that begin at a multiple of 8 share all of the key but what
+  // l / 8 gives, and the two addends are bits of their own.
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&codes[0][0];
+  const int l8 = lane >> 3;
+  const int a_piece = (lane & 7) ^ a_key(l8), b_piece = (lane & 7) ^ b_key<NJ>(l8);
+  v4i ra[LA], rb[LB];
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int r8 = (wave * LOADS + i) * 8 + (lane >> 3);       // row among the stage's BM + BN
-    const bool is_a = (wave * LOADS + i) * 8 < BM;
-    const int r = is_a ? r8 : r8 - BM;
-    piece[i] = (lane & 7) ^ (is_a ? a_key(r) : b_key<NJ>(r));
-    const int last = is_a ? m - 1 - m0 : n - 1 - n0;
-    off[i] = (unsigned)((r < last ? r : last) * (is_a ? lda : ldb)) + piece[i] * 16;
+  for (int i = 0; i < LA; ++i) {
+    const int r = m0 + (wave * LA + i) * 8;
+    ra[i] = buffer_of(a + (int64_t)r * lda, (m - r) * lda);
   }
-  auto load_stage = [&](int c, int buf) {
-    const bool tail = (c + 1) * BLK > k;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const bool is_a = (wave * LOADS + i) * 8 < BM;
-      unsigned o = off[i];
-      if (tail && c * BLK + piece[i] * 16 >= k) o = 0x80000000u;                 // behind the rows' end: out of the buffer's range, zeros
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, (lds_void*)(codes[buf] + (wave * LOADS + i) * 1024), 16, o, c * BLK, 0, 0);
-    }
+  for (int i = 0; i < LB; ++i) {
+    const int r = n0 + (wave * LB + i) * 8;
+    rb[i] = buffer_of(b + (int64_t)r * ldb, (n - r) * ldb);
+  }
+  // instruction i of the loads of step c; TAIL: pieces behind the rows' end become zeros too
+  auto load_part = [&](int c, int i, bool tail) {
+    const bool is_a = i < LA;
+    const int r = is_a ? (wave * LA + i) * 8 : (wave * LB + (i - LA) / 2 * 2) * 8;       // two instructions share a key of b
+    const int piece = is_a ? a_piece ^ (i & 1 ? 4 : 0) : b_piece ^ b_key<NJ>(r);
+    unsigned o = l8 * (unsigned)(is_a ? lda : ldb) + piece * 16;
+    if (tail && c * BLK + piece * 16 >= k) o = 0x80000000u;
+    load_to_lds(is_a ? ra[i < LA ? i : 0] : rb[i < LA ? 0 : i - LA],
+                lds0 + (c & 1) * STAGE + (is_a ? wave * LA + i : BM / 8 + wave * LB + i - LA) * 1024, o, c * BLK);
   };
   auto load_scales = [&](int c, float (&v)[SPT]) {
 #pragma unroll
@@ -383,76 +405,17 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
     }
   };
 
-  v4f acc[MI][NJ];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[i][j] = (v4f){0, 0, 0, 0};
-
-  // a lane's two 16-byte pieces of a fragment: 2 g and 2 g + 1 of its row
-  const int arow = wm * MI * 16 + l16;
-  auto frag = [&](const uint8_t* row, int key) {
-    union { uint4 h[2]; v8i v; } u;
-    u.h[0] = *reinterpret_cast<const uint4*>(row + ((2 * g) ^ key) * 16);
-    u.h[1] = *reinterpret_cast<const uint4*>(row + ((2 * g + 1) ^ key) * 16);
-    return make_frag<EXACT>(u.v);
-  };
-  auto multiply = [&](int buf) {
-    const uint8_t* as = codes[buf] + arow * BLK;
-    const uint8_t* bs = codes[buf] + BM * BLK;
-    Frag<EXACT> fb[NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int r = wn * NJ * 16 + b_row<NJ>(l16, j);
-      fb[j] = frag(bs + r * BLK, b_key<NJ>(r));
-    }
-    v4f cs[NJ];
-    if constexpr (BROWS) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) cs[j] = *reinterpret_cast<const v4f*>(&scales[buf][BM + wn * NJ * 16 + g * 4 * NJ + j * 4]);
-    }
-    const float* rs = scales[buf] + (BROWS ? 0 : (wn * NJ * 16 / BLK) * BM) + arow;
-    Frag<EXACT> fa = frag(as, a_key(arow));
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      // the next rows' fragment is on its way while these are multiplied; no more than that, for the registers' sake
-      Frag<EXACT> next = fa;
-      if (i + 1 < MI) next = frag(as + (i + 1) * 16 * BLK, a_key(arow));
-      const float s = rs[i * 16];
-      v4f p[NJ];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) p[j] = block_product<EXACT>(fb[j], fa);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[j][e], BROWS ? s * cs[j][e] : s, acc[i][j][e]);
-      fa = next;
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  // vmcnt(0), then the barrier: everybody's loads of the step are in LDS, and the other stage is no longer read
+  // this wavefront's loads are in LDS, then everybody's, and nobody reads what the next ones will overwrite
   auto arrive = [&] {
-    __builtin_amdgcn_s_waitcnt(0x0F70);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  float sv[SPT];
-  load_scales(0, sv);
-  load_stage(0, 0);
-  store_scales(0, sv);
-  int c = 0;
-  for (; c + 1 < kb; ++c) {
-    arrive();
-    load_scales(c + 1, sv);
-    load_stage(c + 1, (c & 1) ^ 1);
-    multiply(c & 1);
-    store_scales((c & 1) ^ 1, sv);
-  }
-  arrive();
-  if ((k & 15) != 0) {                           // the piece that holds the rows' end: zeros behind it
-    const int cut = (k - c * BLK) >> 4, keep = k & 15;
+  // the piece that holds the end of the rows, in the last step: zeros behind it
+  auto cut_tail = [&](int buf) {
+    const int cut = (k % BLK) >> 4, keep = k & 15;
     for (int r = t; r < BM + BN; r += NTH) {
       const int key = r < BM ? a_key(r) : b_key<NJ>(r - BM);
-      uint32_t* w = reinterpret_cast<uint32_t*>(codes[c & 1] + r * BLK + (cut ^ key) * 16);
+      uint32_t* w = reinterpret_cast<uint32_t*>(codes[buf] + r * BLK + (cut ^ key) * 16);
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const int left = keep - 4 * d;
@@ -460,12 +423,123 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
       }
     }
     __syncthreads();
-  }
-  multiply(c & 1);
+  };
+
+  v4f acc[MI][NJ];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));     // the last sums are formed here: sunk below the stores' branches, their addends need twice the registers
+    for (int j = 0; j < NJ; ++j) acc[i][j] = (v4f){0, 0, 0, 0};
+
+  // a lane's two 16-byte pieces of a fragment
+  const int arow = wm * MI * 16 + l16;
+  auto raw = [&](const uint8_t* row, int key) {
+    union { uint4 h[2]; v8i v; } u;
+    u.h[0] = *reinterpret_cast<const uint4*>(row + (g ^ key) * 16);
+    u.h[1] = *reinterpret_cast<const uint4*>(row + ((g + 4) ^ key) * 16);
+    return u.v;
+  };
+  auto raw_a = [&](int buf, int i) { return raw(codes[buf] + (arow + i * 16) * BLK, a_key(arow)); };
+  auto raw_b = [&](int buf, int j) {
+    const int r = wn * NJ * 16 + b_row<NJ>(l16, j);
+    return raw(codes[buf] + (BM + r) * BLK, b_key<NJ>(r));
+  };
+  auto row_scale = [&](int buf, int i) { return scales[buf][(BROWS ? 0 : (wn * NJ * 16 / BLK) * BM) + arow + i * 16]; };
+  constexpr int AHEAD = MI > 2 ? 2 : 1;          // fragments of a that are on their way from LDS
+  Frag<EXACT> fb[NJ];
+  v4f cs[NJ];
+  v8i ahead[AHEAD];
+  float s_ahead[AHEAD];
+  auto begin_step = [&](int buf) {
+    fb[0] = make_frag<EXACT>(raw_b(buf, 0));
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      ahead[i] = raw_a(buf, i);
+      s_ahead[i] = row_scale(buf, i);
+    }
+#pragma unroll
+    for (int j = 1; j < NJ; ++j) fb[j] = make_frag<EXACT>(raw_b(buf, j));
+    if constexpr (BROWS) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) cs[j] = *reinterpret_cast<const v4f*>(&scales[buf][BM + wn * NJ * 16 + g * 4 * NJ + j * 4]);
+    }
+  };
+  auto add_scaled = [&](int i, int j, const v4f& p, float s) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], BROWS ? s * cs[j][e] : s, acc[i][j][e]);
+  };
+  // The codes of step c: rows 16 i .. + 15 are multiplied while the sums of those before are scaled and added, two fragments
+  // of a are on their way, and the next step's codes are asked for, a load beside a product (all at once they would stand in
+  // front of the reads of LDS; later ones would not be there in time).  When the last rows' products are issued, everything that the step reads from LDS has been
+  // read: the wait for the next step's codes, the barrier and the first reads of that step run beside them.
+  enum { LAST = 0, MORE = 1, MORE_TAIL = 2 };
+  auto step = [&](int c, auto what) {
+    constexpr int W = decltype(what)::value;
+    const int buf = c & 1;
+    v4f p[2][NJ];
+    float s_at[2], sv[SPT];
+    if constexpr (W != LAST) load_scales(c + 1, sv);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const Frag<EXACT> fa = make_frag<EXACT>(ahead[i % AHEAD]);
+      s_at[i & 1] = s_ahead[i % AHEAD];
+      if (i + AHEAD < MI) {
+        ahead[i % AHEAD] = raw_a(buf, i + AHEAD);
+        s_ahead[i % AHEAD] = row_scale(buf, i + AHEAD);
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        p[i & 1][j] = block_product<EXACT>(fb[j], fa);
+        if (i > 0) add_scaled(i - 1, j, p[(i - 1) & 1][j], s_at[(i - 1) & 1]);
+        if constexpr (W != LAST) {
+          if (i * NJ + j < LOADS) load_part(c + 1, i * NJ + j, W == MORE_TAIL);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    // held here: below the branches that follow, the addends would need registers of their own
+#pragma unroll
+    for (int i = 0; i + 1 < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+    if constexpr (W != LAST) {
+      store_scales(buf ^ 1, sv);
+      arrive();
+      if constexpr (W == MORE_TAIL) {
+        if ((k & 15) != 0) cut_tail(buf ^ 1);
+      }
+    }
+    float s_last = s_at[(MI - 1) & 1];
+    v4f c_last[NJ];
+    if constexpr (BROWS) {                       // the next step's column scales are read over these
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) c_last[j] = s_last * cs[j];
+    }
+    if constexpr (W != LAST) begin_step(buf ^ 1);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[MI - 1][j][e] = fmaf(p[(MI - 1) & 1][j][e], BROWS ? c_last[j][e] : s_last, acc[MI - 1][j][e]);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[MI - 1][j]));
+  };
+  {
+    float sv[SPT];
+    load_scales(0, sv);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load_part(0, i, kb == 1);
+    store_scales(0, sv);
+    arrive();
+    if (kb == 1 && (k & 15) != 0) cut_tail(0);
+    begin_step(0);
+  }
+  int c = 0;
+  for (; c + 2 < kb; ++c) step(c, std::integral_constant<int, MORE>());
+  if (c + 1 < kb) {
+    step(c, std::integral_constant<int, MORE_TAIL>());
+    ++c;
+  }
+  step(c, std::integral_constant<int, LAST>());
   // results: lane: row l16 of each 16, columns 4 NJ g .. of the wavefront's
   const int col = n0 + wn * NJ * 16 + g * 4 * NJ;
   if (col >= n) return;
@@ -533,7 +607,7 @@ int launch_tile(const Product& p, hipStream_t s) {
 template <typename T, bool BROWS>
 int launch_tiles(const Product& p, hipStream_t s) {
   const int64_t big = ((p.m + 255) / 256) * ((p.n + 255) / 256);
-  if constexpr (sizeof(T) == 4) {
+  if constexpr (sizeof(T) == 4 || BROWS) {      // bfloat16 operands, or column scales in registers: 64 rows a wavefront are what fits
     if (((p.m + 255) / 256) * ((p.n + 127) / 128) >= 192) return launch_tile<T, BROWS, 4, 2, 4, 4>(p, s);
   } else {
     if (big >= 192) return launch_tile<T, BROWS, 2, 4, 8, 4>(p, s);
