@@ -23,17 +23,22 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-// magnitude that counts for a block's scale: infinities and NaN do not
+// Infinities are rare and cost the common case nothing: the maximum over all magnitudes (which passes NaN by) tells whether
+// a block holds any.  If not, x * (1 / scale) is at most 448 (1 + 2^-23), which the conversion rounds to 448, and a NaN
+// becomes the NaN code by itself; if so, the maximum is taken again over what is finite, and the products are cut off at 448.
 __device__ __forceinline__ float finite_abs(float v) {
   const float a = fabsf(v);
   return a <= FLT_MAX ? a : 0.0f;
 }
 __device__ __forceinline__ float block_scale(float amax) { return fmaxf(amax / kCodeMax, kScaleMin); }
-// what is encoded: saturated (the conversion would make a NaN of anything over 448), NaN kept
+template <bool INF>
 __device__ __forceinline__ float code_value(float v, float inv) {
   const float y = v * inv;
+  if constexpr (!INF) return y;
   return y != y ? y : fminf(fmaxf(y, -kCodeMax), kCodeMax);
 }
+template <bool INF>
+__device__ __forceinline__ float magnitude(float v) { return INF ? finite_abs(v) : fabsf(v); }
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
@@ -67,33 +72,27 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
 // row groups, and both orientations come from one read.  Transposed codes go through LDS to be written as whole 16-byte
 // pieces of a row of x^T.
 constexpr int QT_STRIDE = BLK + 16;      // bytes of a transposed row in LDS: whole 16-byte pieces, banks shifted from row to row
-template <typename T, bool TILES, bool Q, bool QT>
-__global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, int rows, int cols, int64_t ldx, int tiles_c,
-                                                      uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
-                                                      uint8_t* __restrict__ qt, int64_t ldqt, float* __restrict__ scale_t) {
-  __shared__ float red[4 * BLK];
-  __shared__ __align__(16) uint8_t tr[QT ? BLK * QT_STRIDE : 16];
-  const int tr_i = blockIdx.x / tiles_c, tc_i = blockIdx.x - tr_i * tiles_c;
-  const int r0 = tr_i * BLK, c0 = tc_i * BLK;
+struct QuantizeArgs {
+  int rows, cols, tiles_c;
+  uint8_t* q;
+  int64_t ldq;
+  float* scale;
+  uint8_t* qt;
+  int64_t ldqt;
+  float* scale_t;
+};
+template <bool TILES, bool Q, bool QT, bool INF>
+__device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const QuantizeArgs& p, int tr_i, int tc_i, float* red, uint8_t* tr) {
+  const int r0 = tr_i * BLK, c0 = tc_i * BLK, rows = p.rows, cols = p.cols;
   const int t = threadIdx.x, cg = t & 15, rg = t >> 4, wave = t >> 6;
   const int row = r0 + rg * 8, col = c0 + cg * 8;
-  float v[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (row + i < rows) {
-      load8<T>(x + (int64_t)(row + i) * ldx + col, cols - col, v[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-    }
-  }
   float inv_r[8], inv_c[8];               // what the elements of a row / column are multiplied with
   if constexpr (TILES) {
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(v[i][j]));
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude<INF>(v[i][j]));
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
     if ((t & 63) == 0) red[wave] = m;
@@ -101,8 +100,8 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
     m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     const float s = block_scale(m), inv = 1.0f / s;
     if (t == 0) {
-      if constexpr (Q) scale[(int64_t)tr_i * tiles_c + tc_i] = s;
-      if constexpr (QT) scale_t[(int64_t)tc_i * ((rows + BLK - 1) / BLK) + tr_i] = s;
+      if constexpr (Q) p.scale[(int64_t)tr_i * p.tiles_c + tc_i] = s;
+      if constexpr (QT) p.scale_t[(int64_t)tc_i * ((rows + BLK - 1) / BLK) + tr_i] = s;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) inv_r[i] = inv_c[i] = inv;
@@ -112,12 +111,12 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
       for (int i = 0; i < 8; ++i) {
         float m = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(v[i][j]));
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude<INF>(v[i][j]));
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
         const float s = block_scale(m);
         inv_r[i] = 1.0f / s;
-        if (cg == 0 && row + i < rows) scale[(int64_t)tc_i * rows + row + i] = s;
+        if (cg == 0 && row + i < rows) p.scale[(int64_t)tc_i * rows + row + i] = s;
       }
     }
     if constexpr (QT) {
@@ -125,7 +124,7 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
       for (int j = 0; j < 8; ++j) {
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(v[i][j]));
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, magnitude<INF>(v[i][j]));
         m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
         if ((t & 63) < 16) red[wave * BLK + cg * 8 + j] = m;
@@ -136,7 +135,7 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
         const int c = cg * 8 + j;
         const float s = block_scale(fmaxf(fmaxf(red[c], red[BLK + c]), fmaxf(red[2 * BLK + c], red[3 * BLK + c])));
         inv_c[j] = 1.0f / s;
-        if (rg == 0 && c0 + c < cols) scale_t[(int64_t)tr_i * cols + c0 + c] = s;
+        if (rg == 0 && c0 + c < cols) p.scale_t[(int64_t)tr_i * cols + c0 + c] = s;
       }
     }
   }
@@ -144,15 +143,15 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (row + i >= rows || col >= cols) continue;
-      uint8_t* p = q + (int64_t)(row + i) * ldq + col;
+      uint8_t* at = p.q + (int64_t)(row + i) * p.ldq + col;
       float u[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) u[j] = code_value(v[i][j], inv_r[i]);
+      for (int j = 0; j < 8; ++j) u[j] = code_value<INF>(v[i][j], inv_r[i]);
       const uint32_t lo = codes4(u[0], u[1], u[2], u[3]), hi = codes4(u[4], u[5], u[6], u[7]);
       if (col + 8 <= cols) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
+        *reinterpret_cast<uint2*>(at) = make_uint2(lo, hi);
       } else {
-        for (int j = 0; j < cols - col; ++j) p[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+        for (int j = 0; j < cols - col; ++j) at[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
       }
     }
   }
@@ -161,7 +160,7 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
     for (int j = 0; j < 8; ++j) {
       float u[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = code_value(v[i][j], inv_c[j]);
+      for (int i = 0; i < 8; ++i) u[i] = code_value<INF>(v[i][j], inv_c[j]);
       *reinterpret_cast<uint2*>(tr + (cg * 8 + j) * QT_STRIDE + rg * 8) =
           make_uint2(codes4(u[0], u[1], u[2], u[3]), codes4(u[4], u[5], u[6], u[7]));
     }
@@ -171,21 +170,50 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
       const int c = pass * 32 + (t >> 3), ch = (t & 7) * 16;
       const int left = rows - r0 - ch;
       if (c0 + c >= cols || left <= 0) continue;
-      uint8_t* p = qt + (int64_t)(c0 + c) * ldqt + r0 + ch;
+      uint8_t* at = p.qt + (int64_t)(c0 + c) * p.ldqt + r0 + ch;
       const uint8_t* s = tr + c * QT_STRIDE + ch;
       if (left >= 16) {
-        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(s);
+        *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(s);
       } else {
-        for (int i = 0; i < left; ++i) p[i] = s[i];
+        for (int i = 0; i < left; ++i) at[i] = s[i];
       }
     }
   }
 }
+template <typename T, bool TILES, bool Q, bool QT>
+__global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, int64_t ldx, QuantizeArgs p) {
+  __shared__ float red[4 * BLK];
+  __shared__ __align__(16) uint8_t tr[QT ? BLK * QT_STRIDE : 16];
+  const int tr_i = blockIdx.x / p.tiles_c, tc_i = blockIdx.x - tr_i * p.tiles_c;
+  const int row = tr_i * BLK + (threadIdx.x >> 4) * 8, col = tc_i * BLK + (threadIdx.x & 15) * 8;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (row + i < p.rows) {
+      load8<T>(x + (int64_t)(row + i) * ldx + col, p.cols - col, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+    }
+  }
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
+  if (__syncthreads_or(m > FLT_MAX)) quantize_tile<TILES, Q, QT, true>(v, p, tr_i, tc_i, red, tr);
+  else quantize_tile<TILES, Q, QT, false>(v, p, tr_i, tc_i, red, tr);
+}
 
 // ---- product -------------------------------------------------------------------------------------------------------
-// 32 codes of a row from k0 on as a matrix operand: two aligned 16-byte loads, zeros behind the row's end k.
+// 32 codes of a row from k0 on as a matrix operand: two aligned 16-byte loads; TAIL: zeros behind the row's end k.
+template <bool TAIL>
 __device__ __forceinline__ v8i load_codes(const uint8_t* row, int k0, int k) {
   v8i r;
+  if constexpr (!TAIL) {
+    __builtin_memcpy(&r, __builtin_assume_aligned(row + k0, 16), 32);
+    return r;
+  }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int left = k - (k0 + 16 * h);
@@ -243,52 +271,198 @@ __device__ __forceinline__ v4f block_product(const Frag<EXACT>& a, const Frag<EX
 }
 
 template <typename T> __device__ __forceinline__ void store_out(T* p, float v) { Store<T>::st(p, v); }
-
-// Four wavefronts, 64 x 64 results: each takes 64 rows and 16 columns, fragments straight from global memory.  Lane l of
-// a fragment holds row l % 16 and 32 codes from 32 (l / 16) on (both operands alike, so any order of K would do); of a
-// result it holds column l % 16 and rows 4 (l / 16) .. + 3.
-template <typename T, bool BROWS>
-__global__ __launch_bounds__(256) void k_fp8_direct(const uint8_t* __restrict__ a, int64_t lda, const float* __restrict__ sa,
-                                                    const uint8_t* __restrict__ b, int64_t ldb, const float* __restrict__ sb,
-                                                    const float* __restrict__ bias, int m, int n, int k, T* __restrict__ y, int64_t ldy,
-                                                    int tiles_n) {
-  constexpr bool EXACT = sizeof(T) == 4;
-  const int tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
-  const int col = tn * 64 + (threadIdx.x >> 6) * 16 + l16;
-  const int kb = (k + BLK - 1) / BLK;
-  const uint8_t* bp = b + (int64_t)(col < n ? col : n - 1) * ldb;
-  const uint8_t* ap[4];
-  int row[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = tm * 64 + 16 * i + l16;
-    ap[i] = a + (int64_t)(r < m ? r : m - 1) * lda;
-    row[i] = tm * 64 + 16 * i + 4 * g;
-  }
-  v4f acc[4] = {};
-  for (int c = 0; c < kb; ++c) {
-    const Frag<EXACT> fb = make_frag<EXACT>(load_codes(bp, c * BLK + 32 * g, k));
-    const float s_col = BROWS ? sb[(int64_t)c * n + (col < n ? col : n - 1)] : sb[(int64_t)((col < n ? col : n - 1) / BLK) * kb + c];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const v4f p = block_product<EXACT>(make_frag<EXACT>(load_codes(ap[i], c * BLK + 32 * g, k)), fb);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(p[e], sa[(int64_t)c * m + (row[i] + e < m ? row[i] + e : m - 1)] * s_col, acc[i][e]);
+// four neighbouring results, of which `left` lie inside the row
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float (&o)[4], int left) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      __builtin_memcpy(p, o, 16);
+    } else {
+      const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+      __builtin_memcpy(p, w, 8);
     }
-  }
-  if (col >= n) return;
-  const float bb = bias ? bias[col] : 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
+  } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (row[i] + e < m) store_out<T>(y + (int64_t)(row[i] + e) * ldy + col, acc[i][e] + bb);
+      if (e < left) store_out<T>(p + e, o[e]);
+  }
+}
+
+// ---- product of few rows ---------------------------------------------------------------------------------------------
+// Bound by the reading of b.  A workgroup makes 16 MT rows x 16 NT columns, its wavefronts take every WAVES-th block of K
+// with fragments straight from memory (lane l of a fragment: row l % 16, 32 codes from 32 (l / 16) on, so four lanes read
+// the 128 bytes of a row), UNROLL blocks in flight, and add up through LDS.  b is the first matrix operand, so a lane holds
+// row l % 16 of the result and columns 4 (l / 16) .. + 3.
+// X: a is not there in codes: x is quantised on the way, each lane 32 elements of its row, the block's maximum over the
+// row's four lanes (every workgroup does so for itself: the rows are few).
+template <typename T>
+struct Elements {                        // 32 elements of a row as they lie in memory
+  uint32_t w[8 * sizeof(T)];
+};
+template <typename T, bool TAIL>
+__device__ __forceinline__ Elements<T> load_elements(const T* row, int left, bool there) {
+  Elements<T> x;
+  if constexpr (!TAIL) {
+    if (there) {
+      __builtin_memcpy(x.w, row, sizeof(x.w));
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)(8 * sizeof(T)); ++i) x.w[i] = 0u;
+    }
+  } else {
+    T e[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) e[i] = there && i < left ? row[i] : (T)0;
+    __builtin_memcpy(x.w, e, sizeof(x.w));
+  }
+  return x;
+}
+template <bool INF>
+__device__ __forceinline__ float row_maximum(const float (&v)[32]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) m = fmaxf(m, magnitude<INF>(v[i]));
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  return fmaxf(m, __shfl_xor(m, 32, 64));
+}
+template <bool INF>
+__device__ __forceinline__ v8i codes_of(const float (&v)[32], float inv) {
+  v8i c;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    c[i] = (int)codes4(code_value<INF>(v[4 * i], inv), code_value<INF>(v[4 * i + 1], inv), code_value<INF>(v[4 * i + 2], inv), code_value<INF>(v[4 * i + 3], inv));
+  return c;
+}
+template <typename T>
+__device__ __forceinline__ v8i quantize_elements(const Elements<T>& x, float& scale) {
+  float v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    v[i] = sizeof(T) == 4 ? __uint_as_float(x.w[i % (8 * sizeof(T))]) : __uint_as_float(i & 1 ? x.w[i / 2] & 0xFFFF0000u : x.w[i / 2] << 16);
+  float m = row_maximum<false>(v);
+  if (__any(m > FLT_MAX)) {
+    m = row_maximum<true>(v);
+    scale = block_scale(m);
+    return codes_of<true>(v, 1.0f / scale);
+  }
+  scale = block_scale(m);
+  return codes_of<false>(v, 1.0f / scale);
+}
+
+template <typename T, bool X, bool BROWS, int MT, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_fp8_few(const void* __restrict__ a, int64_t lda, const float* __restrict__ sa,
+                                                        const uint8_t* __restrict__ b, int64_t ldb, const float* __restrict__ sb,
+                                                        const float* __restrict__ bias, int m, int n, int k, T* __restrict__ y,
+                                                        int64_t ldy, int tiles_n) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  constexpr int UNROLL = MT * NT >= 4 ? 2 : 4;
+  __shared__ __align__(16) float red[WAVES][MT * NT][64][4];
+  const int tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
+  const int m0 = tm * 16 * MT, n0 = tn * 16 * NT;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kb = (k + BLK - 1) / BLK;
+  int64_t a_off[MT], b_off[NT];
+  int a_row[MT], n_blk[NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    a_row[i] = m0 + 16 * i + l16 < m ? m0 + 16 * i + l16 : m - 1;      // rows behind the end repeat the last one, and are not stored
+    a_off[i] = (int64_t)a_row[i] * lda;
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int r = n0 + 16 * j + l16;
+    b_off[j] = (int64_t)(r < n ? r : n - 1) * ldb;
+    n_blk[j] = (n0 + 16 * j < n ? n0 + 16 * j : n - 1) / BLK;
+  }
+  v4f acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = (v4f){0, 0, 0, 0};
+  auto blocks = [&](int c0, auto count, auto end) {
+    constexpr int U = decltype(count)::value;
+    constexpr bool TAIL = decltype(end)::value;
+    v8i rb[U][NT], rx[U][MT];
+    Elements<T> ex[X ? U : 1][MT];
+    float s[U][MT];
+    v4f cs[U][NT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * WAVES, at = c * BLK + 32 * g;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        rb[u][j] = load_codes<TAIL>(b + b_off[j], at, k);
+        if constexpr (BROWS) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int col = n0 + 16 * j + 4 * g + e;
+            cs[u][j][e] = sb[(int64_t)c * n + (col < n ? col : n - 1)];
+          }
+        } else {
+          const float f = sb[(int64_t)n_blk[j] * kb + c];
+          cs[u][j] = (v4f){f, f, f, f};
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        if constexpr (!X) {
+          rx[u][i] = load_codes<TAIL>((const uint8_t*)a + a_off[i], at, k);
+          s[u][i] = sa[(int64_t)c * m + a_row[i]];
+        } else {
+          ex[u][i] = load_elements<T, TAIL>((const T*)a + a_off[i] + at, k - at, m0 + 16 * i + l16 < m);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (X) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) rx[u][i] = quantize_elements<T>(ex[u][i], s[u][i]);
+      }
+      Frag<EXACT> fb[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fb[j] = make_frag<EXACT>(rb[u][j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const Frag<EXACT> fa = make_frag<EXACT>(rx[u][i]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const v4f p = block_product<EXACT>(fb[j], fa);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], s[u][i] * cs[u][j][e], acc[i][j][e]);
+        }
+      }
+    }
+  };
+  const int whole = k / BLK;
+  int c = wave;
+  for (; c + (UNROLL - 1) * WAVES < whole; c += UNROLL * WAVES) blocks(c, std::integral_constant<int, UNROLL>(), std::false_type());
+  if constexpr (UNROLL > 1)
+    for (; c < whole; c += WAVES) blocks(c, std::integral_constant<int, 1>(), std::false_type());
+  if (c < kb) blocks(c, std::integral_constant<int, 1>(), std::true_type());
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) *reinterpret_cast<v4f*>(red[wave][i * NT + j][lane]) = acc[i][j];
+  __syncthreads();
+  for (int at = threadIdx.x; at < MT * NT * 64; at += WAVES * 64) {
+    const int tile = at >> 6, l = at & 63;
+    v4f v = *reinterpret_cast<const v4f*>(red[0][tile][l]);
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += *reinterpret_cast<const v4f*>(red[w][tile][l]);
+    const int row = m0 + 16 * (tile / NT) + (l & 15), col = n0 + 16 * (tile % NT) + 4 * (l >> 4);
+    if (row >= m || col >= n) continue;
+    float o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = v[e] + (bias && col + e < n ? bias[col + e] : 0.0f);
+    store4<T>(y + (int64_t)row * ldy + col, o, n - col);
+  }
 }
 
 // ---- product of many rows: tiles staged in LDS -----------------------------------------------------------------------
-// A workgroup of WGM x WGN wavefronts makes a tile of BM x BN results, a wavefront 16 MI x 16 NJ of them, in steps of one
-// block (128 codes) of K.  The codes of a step go from memory straight into LDS (16 bytes a lane, a row of 128 in eight
+// A group of WGM x WGN wavefronts makes a tile of BM x BN results, a wavefront 16 MI x 16 NJ of them, in steps of one
+// block (128 codes) of K.  Where tiles are few, KG groups of a workgroup share K: more loads in flight on a compute unit.  The codes of a step go from memory straight into LDS (16 bytes a lane, a row of 128 in eight
 // pieces) while the step before is multiplied; two such stages.  The first matrix operand is b and the second a, so that a
 // lane's results are four neighbouring columns of one row: the row's scale is one register, and with the order of b's rows
 // below a lane's NJ fragments are 4 NJ columns in a row, which it stores in 16-byte pieces.
@@ -329,13 +503,13 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm
   tn = in / height;
 }
 
-template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ>
-__global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __restrict__ a, int64_t lda, const float* __restrict__ sa,
+template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ, int KG>
+__global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t* __restrict__ a, int64_t lda, const float* __restrict__ sa,
                                                              const uint8_t* __restrict__ b, int64_t ldb, const float* __restrict__ sb,
                                                              const float* __restrict__ bias, int m, int n, int k, T* __restrict__ y,
                                                              int64_t ldy, int tiles_m, int tiles_n) {
   constexpr bool EXACT = sizeof(T) == 4;
-  constexpr int NTH = WGM * WGN * 64, NWV = WGM * WGN;
+  constexpr int NTH = WGM * WGN * 64, NWV = WGM * WGN;         // threads and wavefronts of a group
   constexpr int BM = WGM * MI * 16, BN = WGN * NJ * 16;
   constexpr int STAGE = (BM + BN) * BLK;                       // bytes of codes of a step
   constexpr int CB = BN >= BLK ? BN / BLK : 1;                 // column blocks of a tile
@@ -343,19 +517,24 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
   constexpr int SPT = (NS + NTH - 1) / NTH;
   constexpr int LA = BM / 8 / NWV, LB = BN / 8 / NWV, LOADS = LA + LB;      // a wavefront's loads of a step
   static_assert(BM % (16 * NWV) == 0 && BN % (16 * NWV) == 0 && NJ == 4, "whole loads, keys as the loads assume them");
-  __shared__ __align__(1024) uint8_t codes[2][STAGE];
-  __shared__ __align__(16) float scales[2][NS];
-  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
+  static_assert(MI * NJ >= LOADS, "a load beside a product");
+  __shared__ __align__(1024) uint8_t all_codes[KG][2][STAGE];
+  __shared__ __align__(16) float all_scales[KG][2][NS];
+  const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NTH);
+  uint8_t (*codes)[STAGE] = all_codes[kg];
+  float (*scales)[NS] = all_scales[kg];
+  const int t = threadIdx.x - kg * NTH, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WGN, wn = wave - wm * WGN;
   int tm, tn;
   tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const int kb = (k + BLK - 1) / BLK;
+  const int per = (kb + KG - 1) / KG, first = kg * per;        // blocks of K of a group; behind the last one they are zeros
 
   // loads: an instruction moves eight rows, lane l piece l % 8 (before the keys) of row l / 8; rows behind the end lie
   // outside the buffer's range and become zeros.  Eight rows that begin at a multiple of 8 share all of the key but what
   // l / 8 gives, and the two addends are bits of their own.
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&codes[0][0];
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)codes[0];
   const int l8 = lane >> 3;
   const int a_piece = (lane & 7) ^ a_key(l8), b_piece = (lane & 7) ^ b_key<NJ>(l8);
   v4i ra[LA], rb[LB];
@@ -377,9 +556,10 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
     unsigned o = l8 * (unsigned)(is_a ? lda : ldb) + piece * 16;
     if (tail && c * BLK + piece * 16 >= k) o = 0x80000000u;
     load_to_lds(is_a ? ra[i < LA ? i : 0] : rb[i < LA ? 0 : i - LA],
-                lds0 + (c & 1) * STAGE + (is_a ? wave * LA + i : BM / 8 + wave * LB + i - LA) * 1024, o, c * BLK);
+                lds0 + ((c - first) & 1) * STAGE + (is_a ? wave * LA + i : BM / 8 + wave * LB + i - LA) * 1024, o, c * BLK);
   };
-  auto load_scales = [&](int c, float (&v)[SPT]) {
+  auto load_scales = [&](int at_c, float (&v)[SPT]) {
+    const int c = at_c < kb ? at_c : kb - 1;
 #pragma unroll
     for (int i = 0; i < SPT; ++i) {
       const int at = t + i * NTH;
@@ -388,11 +568,13 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
         const bool is_a = at < BM;
         const int r = is_a ? m0 + at : n0 + at - BM, end = is_a ? m : n;
         v[i] = (is_a ? sa : sb)[(int64_t)c * end + (r < end ? r : end - 1)];
+        if (KG > 1 && at_c >= kb) v[i] = 0.0f;
       } else {
         const int cb = at / BM, r = m0 + at - cb * BM;
         int blk = n0 / BLK + cb;
         if (blk > (n - 1) / BLK) blk = (n - 1) / BLK;
         v[i] = sa[(int64_t)c * m + (r < m ? r : m - 1)] * sb[(int64_t)blk * kb + c];
+        if (KG > 1 && at_c >= kb) v[i] = 0.0f;
       }
     }
   };
@@ -410,10 +592,10 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  // the piece that holds the end of the rows, in the last step: zeros behind it
-  auto cut_tail = [&](int buf) {
-    const int cut = (k % BLK) >> 4, keep = k & 15;
-    for (int r = t; r < BM + BN; r += NTH) {
+  // the piece that holds the end of the rows, in the last block: zeros behind it.  Every group comes here at the same step.
+  auto cut_tail = [&](int c) {
+    const int cut = (k % BLK) >> 4, keep = k & 15, buf = (c - first) & 1;
+    for (int r = t; r < BM + BN && c == kb - 1; r += NTH) {
       const int key = r < BM ? a_key(r) : b_key<NJ>(r - BM);
       uint32_t* w = reinterpret_cast<uint32_t*>(codes[buf] + r * BLK + (cut ^ key) * 16);
 #pragma unroll
@@ -475,7 +657,7 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
   enum { LAST = 0, MORE = 1, MORE_TAIL = 2 };
   auto step = [&](int c, auto what) {
     constexpr int W = decltype(what)::value;
-    const int buf = c & 1;
+    const int buf = (c - first) & 1;
     v4f p[2][NJ];
     float s_at[2], sv[SPT];
     if constexpr (W != LAST) load_scales(c + 1, sv);
@@ -506,7 +688,7 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
       store_scales(buf ^ 1, sv);
       arrive();
       if constexpr (W == MORE_TAIL) {
-        if ((k & 15) != 0) cut_tail(buf ^ 1);
+        if ((k & 15) != 0 && (KG == 1 || c + 1 - first == (kb - 1) % per)) cut_tail(c + 1);
       }
     }
     float s_last = s_at[(MI - 1) & 1];
@@ -525,21 +707,45 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_fp8_tile(const uint8_t* __re
   };
   {
     float sv[SPT];
-    load_scales(0, sv);
+    load_scales(first, sv);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) load_part(0, i, kb == 1);
+    for (int i = 0; i < LOADS; ++i) load_part(first, i, KG > 1 || kb == 1);
     store_scales(0, sv);
     arrive();
-    if (kb == 1 && (k & 15) != 0) cut_tail(0);
+    if ((k & 15) != 0 && (kb - 1) % per == 0) cut_tail(first);
     begin_step(0);
   }
-  int c = 0;
-  for (; c + 2 < kb; ++c) step(c, std::integral_constant<int, MORE>());
-  if (c + 1 < kb) {
-    step(c, std::integral_constant<int, MORE_TAIL>());
-    ++c;
+  int c = first;
+  const int end = first + per;
+  if constexpr (KG == 1) {
+    for (; c + 2 < end; ++c) step(c, std::integral_constant<int, MORE>());
+    if (c + 1 < end) {
+      step(c, std::integral_constant<int, MORE_TAIL>());
+      ++c;
+    }
+  } else {
+    for (; c + 1 < end; ++c) step(c, std::integral_constant<int, MORE_TAIL>());
   }
   step(c, std::integral_constant<int, LAST>());
+  if constexpr (KG > 1) {                        // the groups' sums, added up in their order through LDS
+    static_assert((KG - 1) * BM * BN * 4 <= (int)sizeof(all_codes), "room for the sums");
+    v4f* sums = reinterpret_cast<v4f*>(&all_codes[0][0][0]);
+    __syncthreads();
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) sums[((kg - 1) * MI * NJ + i * NJ + j) * NTH + t] = acc[i][j];
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int q = 0; q < KG - 1; ++q)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] += sums[(q * MI * NJ + i * NJ + j) * NTH + t];
+  }
   // results: lane: row l16 of each 16, columns 4 NJ g .. of the wavefront's
   const int col = n0 + wn * NJ * 16 + g * 4 * NJ;
   if (col >= n) return;
@@ -577,7 +783,7 @@ bool sizes_ok(int64_t m, int64_t n, int64_t k) { return m >= 0 && n >= 0 && k >=
 bool codes_ok(const void* p, int64_t ld, int64_t cols) { return ((uintptr_t)p & 15) == 0 && ld >= cols && ld % 16 == 0 && ld < ((int64_t)1 << 40); }
 
 struct Product {
-  const uint8_t* a; int64_t lda; const float* sa;
+  const void* a; int64_t lda; const float* sa;
   const uint8_t* b; int64_t ldb; const float* sb;
   int b_blocks;
   const float* bias;
@@ -595,41 +801,65 @@ int check_product(const char* who, const Product& p) {
   return AE_OK;
 }
 
-template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ>
+template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ, int KG>
 int launch_tile(const Product& p, hipStream_t s) {
   constexpr int BM = WGM * MI * 16, BN = WGN * NJ * 16;
   const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
   if (tm * tn > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
-  hipLaunchKernelGGL((k_fp8_tile<T, BROWS, WGM, WGN, MI, NJ>), dim3((unsigned)(tm * tn)), dim3(WGM * WGN * 64), 0, s, p.a, p.lda, p.sa, p.b, p.ldb,
+  hipLaunchKernelGGL((k_fp8_tile<T, BROWS, WGM, WGN, MI, NJ, KG>), dim3((unsigned)(tm * tn)), dim3(WGM * WGN * KG * 64), 0, s, (const uint8_t*)p.a, p.lda, p.sa, p.b, p.ldb,
                      p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tm, (int)tn);
   return launch_status("fp8_matmul");
 }
+// The largest tiles that still leave no compute unit idle, by the number of tiles (256 compute units; times with the quantiser):
+//   up to 256 of 64 x 64     four groups of K    200 x 4 096 x 4 096 in bfloat16 22 us (two groups 26, one 34; 128 x 128 in two groups 33)
+//   up to 512                two groups          400 x 4 096 x 4 096 30 us (four 36, one 35; 128 x 128 in two groups 33); binary32: 128 x 64, 37 us (64 x 64 54)
+//   up to 256 of 128 x 128   two groups of K     777 x 4 096 x 4 096 36 us (one 44; 64 x 64 39; 256 x 256 57)
+//   more                     one group, two workgroups to a compute unit    1 500 x 4 096 x 4 096 49 us (256 x 256 59; 64 x 64 63)
+//   from 192 of 256 x 256    1 500 x 8 192 x 2 048 41 us (128 x 128 48).  Binary32 results and b in row blocks need more registers:
+//                            256 x 128, and only where it is a whole round or many (1 500 x 4 096 x 4 096 78 us, 128 x 128 83; 1 500 x 8 192 x 2 048 88, 78)
 template <typename T, bool BROWS>
 int launch_tiles(const Product& p, hipStream_t s) {
-  const int64_t big = ((p.m + 255) / 256) * ((p.n + 255) / 256);
-  if constexpr (sizeof(T) == 4 || BROWS) {      // bfloat16 operands, or column scales in registers: 64 rows a wavefront are what fits
-    if (((p.m + 255) / 256) * ((p.n + 127) / 128) >= 192) return launch_tile<T, BROWS, 4, 2, 4, 4>(p, s);
+  auto tiles = [&](int64_t bm, int64_t bn) { return ((p.m + bm - 1) / bm) * ((p.n + bn - 1) / bn); };
+  constexpr bool WIDE = sizeof(T) == 4 || BROWS;
+  if constexpr (WIDE) {
+    const int64_t t = tiles(256, 128);
+    if ((t >= 192 && t <= 256) || (t > 448 && t <= 512) || t >= 1024) return launch_tile<T, BROWS, 4, 2, 4, 4, 1>(p, s);
   } else {
-    if (big >= 192) return launch_tile<T, BROWS, 2, 4, 8, 4>(p, s);
+    if (tiles(256, 256) >= 192) return launch_tile<T, BROWS, 2, 4, 8, 4, 1>(p, s);
   }
-  return launch_tile<T, BROWS, 2, 2, 4, 4>(p, s);
+  if (tiles(64, 64) <= 256) return launch_tile<T, BROWS, 4, 1, 1, 4, 4>(p, s);
+  if (tiles(64, 64) <= 512) return launch_tile<T, BROWS, 4, 1, WIDE ? 2 : 1, 4, 2>(p, s);
+  if (tiles(128, 128) <= 256) return launch_tile<T, BROWS, 2, 2, 4, 4, 2>(p, s);
+  return launch_tile<T, BROWS, 2, 2, 4, 4, 1>(p, s);
+}
+template <typename T, bool X, bool BROWS, int MT, int NT, int WAVES>
+int launch_few(const Product& p, hipStream_t s) {
+  const int64_t tm = (p.m + 16 * MT - 1) / (16 * MT), tn = (p.n + 16 * NT - 1) / (16 * NT);
+  if (tm * tn > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
+  hipLaunchKernelGGL((k_fp8_few<T, X, BROWS, MT, NT, WAVES>), dim3((unsigned)(tm * tn)), dim3(WAVES * 64), 0, s, (const void*)p.a, p.lda, p.sa, p.b, p.ldb,
+                     p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tn);
+  return launch_status("fp8_matmul");
+}
+// x quantised on the way: every workgroup reads and quantises all of x, so it takes as many columns as leave 256 workgroups
+constexpr int64_t kQuantizeOnTheWay = 16;        // rows
+template <typename T>
+int launch_few_elements(const Product& p, hipStream_t s) {
+  if (p.n >= 64 * 256) return launch_few<T, true, false, 1, 4, 8>(p, s);
+  if (p.n >= 32 * 256) return launch_few<T, true, false, 1, 2, 8>(p, s);
+  return launch_few<T, true, false, 1, 1, 8>(p, s);
+}
+template <typename T, bool BROWS>
+int launch_rows(const Product& p, hipStream_t s) {
+  // offsets inside a tile are 31 bits
+  if (p.m > 64 && p.lda < (1 << 23) && p.ldb < (1 << 23)) return launch_tiles<T, BROWS>(p, s);
+  if (p.m <= 16) return launch_few<T, false, BROWS, 1, 1, 8>(p, s);
+  if (p.m <= 32) return launch_few<T, false, BROWS, 2, 1, 8>(p, s);
+  return launch_few<T, false, BROWS, 4, 1, 8>(p, s);
 }
 
 int launch_product(const Product& p, hipStream_t s) {
-  // offsets inside a tile are 31 bits
-  if (p.m > 64 && p.lda < (1 << 23) && p.ldb < (1 << 23)) {
-    if (p.dtype == AE_BF16) return p.b_blocks == AE_FP8_ROWS ? launch_tiles<bf16_t, true>(p, s) : launch_tiles<bf16_t, false>(p, s);
-    return p.b_blocks == AE_FP8_ROWS ? launch_tiles<float, true>(p, s) : launch_tiles<float, false>(p, s);
-  }
-  const int64_t tn = (p.n + 63) / 64, tm = (p.m + 63) / 64;
-  if (tn * tm > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
-#define DIRECT(T, R)                                                                                                            \
-  hipLaunchKernelGGL((k_fp8_direct<T, R>), dim3((unsigned)(tn * tm)), dim3(256), 0, s, p.a, p.lda, p.sa, p.b, p.ldb, p.sb, p.bias, \
-                     (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tn)
-  if (p.dtype == AE_BF16) { if (p.b_blocks == AE_FP8_ROWS) DIRECT(bf16_t, true); else DIRECT(bf16_t, false); }
-  else { if (p.b_blocks == AE_FP8_ROWS) DIRECT(float, true); else DIRECT(float, false); }
-#undef DIRECT
-  return launch_status("fp8_matmul");
+  if (p.dtype == AE_BF16) return p.b_blocks == AE_FP8_ROWS ? launch_rows<bf16_t, true>(p, s) : launch_rows<bf16_t, false>(p, s);
+  return p.b_blocks == AE_FP8_ROWS ? launch_rows<float, true>(p, s) : launch_rows<float, false>(p, s);
 }
 
 template <typename T>
@@ -637,9 +867,9 @@ int launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
                     int64_t ldqt, float* scale_t, hipStream_t s) {
   const int64_t tr = (rows + BLK - 1) / BLK, tc = (cols + BLK - 1) / BLK;
   if (tr * tc > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_quantize: matrix too large");
+  const QuantizeArgs p = {(int)rows, (int)cols, (int)tc, (uint8_t*)q, ldq, scale, (uint8_t*)qt, ldqt, scale_t};
 #define QUANT(TI, A, B)                                                                                                         \
-  hipLaunchKernelGGL((k_fp8_quantize<T, TI, A, B>), dim3((unsigned)(tr * tc)), dim3(256), 0, s, (const T*)x, (int)rows, (int)cols, ldx, \
-                     (int)tc, (uint8_t*)q, ldq, scale, (uint8_t*)qt, ldqt, scale_t)
+  hipLaunchKernelGGL((k_fp8_quantize<T, TI, A, B>), dim3((unsigned)(tr * tc)), dim3(256), 0, s, (const T*)x, ldx, p)
   if (blocks == AE_FP8_TILES) {
     if (q && qt) QUANT(true, true, true);
     else if (q) QUANT(true, true, false);
@@ -693,7 +923,7 @@ extern "C" int model_fp8_matmul(const void* a, int64_t lda, const float* a_scale
   if (m == 0 || n == 0) return AE_OK;
   if (!a || !a_scale) return fail(AE_EINVAL, "model_fp8_matmul: null argument");
   if (!codes_ok(a, lda, k) || ((uintptr_t)a_scale & 3)) return fail(AE_EINVAL, "model_fp8_matmul: rows of codes must begin on 16-byte borders and not overlap, scales must not be misaligned");
-  const Product p = {(const uint8_t*)a, lda, a_scale, (const uint8_t*)b, ldb, b_scale, b_blocks, bias, m, n, k, dtype, y, ldy};
+  const Product p = {a, lda, a_scale, (const uint8_t*)b, ldb, b_scale, b_blocks, bias, m, n, k, dtype, y, ldy};
   AE_TRY(check_product("model_fp8_matmul", p));
   return launch_product(p, (hipStream_t)stream);
 }
@@ -701,7 +931,7 @@ extern "C" int model_fp8_matmul(const void* a, int64_t lda, const float* a_scale
 extern "C" int model_fp8_linear_workspace(int64_t m, int64_t n, int64_t k, int64_t* bytes) {
   using namespace ae;
   if (!bytes || !sizes_ok(m, n, k)) return fail(AE_EINVAL, "model_fp8_linear_workspace: bad argument");
-  *bytes = m * align16(k) + align16(m * ((k + BLK - 1) / BLK) * 4);
+  *bytes = m <= kQuantizeOnTheWay ? 0 : m * align16(k) + align16(m * ((k + BLK - 1) / BLK) * 4);
   return AE_OK;
 }
 
@@ -720,6 +950,12 @@ extern "C" int model_fp8_linear(const void* x, int64_t ldx, const void* w, int64
   float* sx = (float*)(q + m * align16(k));
   const Product p = {q, align16(k), sx, (const uint8_t*)w, ldw, w_scale, AE_FP8_TILES, bias, m, n, k, dtype, y, ldy};
   AE_TRY(check_product("model_fp8_linear", p));
+  if (m <= kQuantizeOnTheWay) {
+    Product f = p;
+    f.a = x;
+    f.lda = ldx;
+    return dtype == AE_BF16 ? launch_few_elements<bf16_t>(f, (hipStream_t)stream) : launch_few_elements<float>(f, (hipStream_t)stream);
+  }
   AE_TRY(model_fp8_quantize(x, m, k, ldx, dtype, AE_FP8_ROWS, q, align16(k), sx, nullptr, 0, nullptr, stream));
   return launch_product(p, (hipStream_t)stream);
 }
