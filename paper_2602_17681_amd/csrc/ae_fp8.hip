@@ -71,7 +71,26 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
 // in registers, so that a block maximum along a row is a reduction over 16 neighbouring lanes, along a column over the 16
 // row groups, and both orientations come from one read.  Transposed codes go through LDS to be written as whole 16-byte
 // pieces of a row of x^T.
-constexpr int QT_STRIDE = BLK + 16;      // bytes of a transposed row in LDS: whole 16-byte pieces, banks shifted from row to row
+constexpr int QT_STRIDE = BLK / 4 + 1;    // words of a transposed row in LDS: eight rows on, as far as neighbouring lanes write, are 8 banks on
+// maximum over the 16 lanes of a row of lanes, in all of them
+__device__ __forceinline__ float max16(float v) {
+  auto turned = [](float x, auto by) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(by)::value, 0xF, 0xF, false));      // row_ror
+  };
+  v = fmaxf(v, turned(v, std::integral_constant<int, 8>()));
+  v = fmaxf(v, turned(v, std::integral_constant<int, 4>()));
+  v = fmaxf(v, turned(v, std::integral_constant<int, 2>()));
+  return fmaxf(v, turned(v, std::integral_constant<int, 1>()));
+}
+// maximum over lanes l, l + 16, l + 32, l + 48 (mod 64)
+__device__ __forceinline__ float max_rows(float v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  const u2 h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+  const u2 q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
 struct QuantizeArgs {
   int rows, cols, tiles_c;
   uint8_t* q;
@@ -82,7 +101,7 @@ struct QuantizeArgs {
   float* scale_t;
 };
 template <bool TILES, bool Q, bool QT, bool INF>
-__device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const QuantizeArgs& p, int tr_i, int tc_i, float* red, uint8_t* tr) {
+__device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const QuantizeArgs& p, int tr_i, int tc_i, float* red, uint32_t* tr) {
   const int r0 = tr_i * BLK, c0 = tc_i * BLK, rows = p.rows, cols = p.cols;
   const int t = threadIdx.x, cg = t & 15, rg = t >> 4, wave = t >> 6;
   const int row = r0 + rg * 8, col = c0 + cg * 8;
@@ -93,8 +112,7 @@ __device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const Quan
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude<INF>(v[i][j]));
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    m = max_rows(max16(m));
     if ((t & 63) == 0) red[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
@@ -112,9 +130,7 @@ __device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const Quan
         float m = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude<INF>(v[i][j]));
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-        const float s = block_scale(m);
+        const float s = block_scale(max16(m));
         inv_r[i] = 1.0f / s;
         if (cg == 0 && row + i < rows) p.scale[(int64_t)tc_i * rows + row + i] = s;
       }
@@ -125,8 +141,7 @@ __device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const Quan
         float m = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = fmaxf(m, magnitude<INF>(v[i][j]));
-        m = fmaxf(m, __shfl_xor(m, 16, 64));
-        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        m = max_rows(m);
         if ((t & 63) < 16) red[wave * BLK + cg * 8 + j] = m;
       }
       __syncthreads();
@@ -161,8 +176,9 @@ __device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const Quan
       float u[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] = code_value<INF>(v[i][j], inv_c[j]);
-      *reinterpret_cast<uint2*>(tr + (cg * 8 + j) * QT_STRIDE + rg * 8) =
-          make_uint2(codes4(u[0], u[1], u[2], u[3]), codes4(u[4], u[5], u[6], u[7]));
+      uint32_t* w = tr + (cg * 8 + j) * QT_STRIDE + rg * 2;
+      w[0] = codes4(u[0], u[1], u[2], u[3]);
+      w[1] = codes4(u[4], u[5], u[6], u[7]);
     }
     __syncthreads();
 #pragma unroll
@@ -171,11 +187,11 @@ __device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const Quan
       const int left = rows - r0 - ch;
       if (c0 + c >= cols || left <= 0) continue;
       uint8_t* at = p.qt + (int64_t)(c0 + c) * p.ldqt + r0 + ch;
-      const uint8_t* s = tr + c * QT_STRIDE + ch;
+      const uint32_t* s = tr + c * QT_STRIDE + ch / 4;
       if (left >= 16) {
-        *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(s);
+        *reinterpret_cast<uint4*>(at) = make_uint4(s[0], s[1], s[2], s[3]);
       } else {
-        for (int i = 0; i < left; ++i) at[i] = s[i];
+        for (int i = 0; i < left; ++i) at[i] = (uint8_t)(s[i >> 2] >> (8 * (i & 3)));
       }
     }
   }
@@ -183,7 +199,7 @@ __device__ __forceinline__ void quantize_tile(const float (&v)[8][8], const Quan
 template <typename T, bool TILES, bool Q, bool QT>
 __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, int64_t ldx, QuantizeArgs p) {
   __shared__ float red[4 * BLK];
-  __shared__ __align__(16) uint8_t tr[QT ? BLK * QT_STRIDE : 16];
+  __shared__ uint32_t tr[QT ? BLK * QT_STRIDE : 1];
   const int tr_i = blockIdx.x / p.tiles_c, tc_i = blockIdx.x - tr_i * p.tiles_c;
   const int row = tr_i * BLK + (threadIdx.x >> 4) * 8, col = tc_i * BLK + (threadIdx.x & 15) * 8;
   float v[8][8];
@@ -203,6 +219,54 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
     for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
   if (__syncthreads_or(m > FLT_MAX)) quantize_tile<TILES, Q, QT, true>(v, p, tr_i, tc_i, red, tr);
   else quantize_tile<TILES, Q, QT, false>(v, p, tr_i, tc_i, red, tr);
+}
+
+// Codes in row blocks alone need no tile: 16 lanes take a block, a workgroup 16 R rows of one column of blocks, so that
+// also few rows make many workgroups.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void k_fp8_quantize_rows(const T* __restrict__ x, int64_t ldx, QuantizeArgs p) {
+  const int rt = blockIdx.x / p.tiles_c, tc = blockIdx.x - rt * p.tiles_c;
+  const int row = rt * 16 * R + (threadIdx.x >> 4), cg = threadIdx.x & 15, col = tc * BLK + cg * 8;
+  float v[R][8], m[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = row + 16 * i;
+    if (r < p.rows) {
+      load8<T>(x + (int64_t)r * ldx + col, p.cols - col, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    m[i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m[i] = fmaxf(m[i], fabsf(v[i][j]));
+    m[i] = max16(m[i]);
+    const bool inf = __any(m[i] > FLT_MAX);
+    if (inf) {
+      m[i] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m[i] = fmaxf(m[i], finite_abs(v[i][j]));
+      m[i] = max16(m[i]);
+    }
+    const float s = block_scale(m[i]), inv = 1.0f / s;
+    const int r = row + 16 * i;
+    float u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = inf ? code_value<true>(v[i][j], inv) : code_value<false>(v[i][j], inv);
+    if (r >= p.rows) continue;
+    if (cg == 0) p.scale[(int64_t)tc * p.rows + r] = s;
+    if (col >= p.cols) continue;
+    uint8_t* at = p.q + (int64_t)r * p.ldq + col;
+    const uint32_t lo = codes4(u[0], u[1], u[2], u[3]), hi = codes4(u[4], u[5], u[6], u[7]);
+    if (col + 8 <= p.cols) {
+      *reinterpret_cast<uint2*>(at) = make_uint2(lo, hi);
+    } else {
+      for (int j = 0; j < p.cols - col; ++j) at[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+    }
+  }
 }
 
 // ---- product -------------------------------------------------------------------------------------------------------
@@ -322,8 +386,7 @@ __device__ __forceinline__ float row_maximum(const float (&v)[32]) {
   float m = 0.0f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) m = fmaxf(m, magnitude<INF>(v[i]));
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  return fmaxf(m, __shfl_xor(m, 32, 64));
+  return max_rows(m);
 }
 template <bool INF>
 __device__ __forceinline__ v8i codes_of(const float (&v)[32], float inv) {
@@ -866,7 +929,8 @@ template <typename T>
 int launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int blocks, void* q, int64_t ldq, float* scale, void* qt,
                     int64_t ldqt, float* scale_t, hipStream_t s) {
   const int64_t tr = (rows + BLK - 1) / BLK, tc = (cols + BLK - 1) / BLK;
-  if (tr * tc > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_quantize: matrix too large");
+  constexpr int QROWS = 2;                       // 16 384 x 4 096 in bfloat16: 37 us, 5.4 TB/s (one 38, four 45; 128 x 128 tiles 46)
+  if (tr * tc * 8 > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_quantize: matrix too large");
   const QuantizeArgs p = {(int)rows, (int)cols, (int)tc, (uint8_t*)q, ldq, scale, (uint8_t*)qt, ldqt, scale_t};
 #define QUANT(TI, A, B)                                                                                                         \
   hipLaunchKernelGGL((k_fp8_quantize<T, TI, A, B>), dim3((unsigned)(tr * tc)), dim3(256), 0, s, (const T*)x, ldx, p)
@@ -876,7 +940,7 @@ int launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
     else QUANT(true, false, true);
   } else {
     if (q && qt) QUANT(false, true, true);
-    else if (q) QUANT(false, true, false);
+    else if (q) hipLaunchKernelGGL((k_fp8_quantize_rows<T, QROWS>), dim3((unsigned)((rows + 16 * QROWS - 1) / (16 * QROWS) * tc)), dim3(256), 0, s, (const T*)x, ldx, p);
     else QUANT(false, false, true);
   }
 #undef QUANT
