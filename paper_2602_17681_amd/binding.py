@@ -7,6 +7,7 @@ Nothing is computed here and there is no fallback: if the library is missing the
 import fails.
 """
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -133,14 +134,21 @@ def _ptr(t, dtype=None):
     return C.c_void_p(t.data_ptr())
 
 
+def _raw_stream():
+    """The current stream of the current device as a number: what _stream() wraps, without the Stream object in between."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
 def _mat(t, rows, cols, dtype=None):
     """(data pointer, row stride) of a device matrix whose rows are contiguous; (null, 0) for None."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, "device-resident [%d][%d] matrix required" % (rows, cols)
+    assert t.is_cuda and t.shape == (rows, cols), "device-resident [%d][%d] matrix required" % (rows, cols)
     assert dtype is None or t.dtype == dtype, (t.dtype, dtype)
-    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
-    assert (cols <= 1 or t.stride(1) == 1) and ld >= cols, "rows must be contiguous and must not overlap"
+    ld, step = t.stride()
+    if rows <= 1:
+        ld = max(cols, ld)                          # the stride of a single row plays no part
+    assert (step == 1 or cols <= 1) and ld >= cols, "rows must be contiguous and must not overlap"
     return t.data_ptr(), ld
 
 
@@ -150,7 +158,8 @@ def _codes(t, rows, cols):
         return None, 0
     assert t.dtype == torch.float8_e4m3fn or t.dtype == torch.uint8, t.dtype
     p, ld = _mat(t, rows, cols)
-    ld = -(-ld // 16) * 16 if rows == 1 else ld     # the stride of a single row plays no part
+    if rows == 1:
+        ld = -(-ld // 16) * 16
     assert rows == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= rows * ld, "all rows * stride bytes must be there"
     return p, ld
 
@@ -168,7 +177,7 @@ def _room(t, nbytes):
     if t is None:
         assert nbytes == 0, "a workspace of %d bytes is needed" % nbytes
         return None
-    assert t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes
+    assert t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes, "a workspace of %d bytes is needed" % nbytes
     return t.data_ptr()
 
 
@@ -531,9 +540,10 @@ def model_fp8_quantize(x, rows, cols, blocks, q=None, scale=None, qt=None, scale
     qp, ldq = _codes(q, rows, cols)
     tp, ldt = _codes(qt, cols, rows)
     _check(lib.model_fp8_quantize(xp, rows, cols, ldx, _dtype_of(x), FP8_BLOCKS[blocks], qp, ldq, _fp8_scales(scale, rows, cols, blocks),
-                                  tp, ldt, _fp8_scales(scale_t, cols, rows, blocks), _stream()))
+                                  tp, ldt, _fp8_scales(scale_t, cols, rows, blocks), _raw_stream()))
 
 
+@functools.lru_cache(maxsize=1024)                # by sizes alone
 def model_fp8_matmul_workspace(m, n, k):
     b = C.c_int64()
     _check(lib.model_fp8_matmul_workspace(m, n, k, C.byref(b)))
@@ -547,9 +557,10 @@ def model_fp8_matmul(a, a_scale, b, b_scale, b_blocks, bias, m, n, k, y, workspa
     yp, ldy = _mat(y, m, n)
     _check(lib.model_fp8_matmul(ap, lda, _fp8_scales(a_scale, m, k, "rows"), bp, ldb, _fp8_scales(b_scale, n, k, b_blocks),
                                 FP8_BLOCKS[b_blocks], _vec(bias, n), m, n, k, _dtype_of(y), yp, ldy,
-                                _room(workspace, model_fp8_matmul_workspace(m, n, k)), _stream()))
+                                _room(workspace, model_fp8_matmul_workspace(m, n, k)), _raw_stream()))
 
 
+@functools.lru_cache(maxsize=1024)                # by sizes alone
 def model_fp8_linear_workspace(m, n, k):
     b = C.c_int64()
     _check(lib.model_fp8_linear_workspace(m, n, k, C.byref(b)))
@@ -562,9 +573,10 @@ def model_fp8_linear(x, w, w_scale, bias, m, n, k, y, workspace=None):
     wp, ldw = _codes(w, n, k)
     yp, ldy = _mat(y, m, n, x.dtype)
     _check(lib.model_fp8_linear(xp, ldx, wp, ldw, _fp8_scales(w_scale, n, k, "tiles"), _vec(bias, n), m, n, k, _dtype_of(x), yp, ldy,
-                                _room(workspace, model_fp8_linear_workspace(m, n, k)), _stream()))
+                                _room(workspace, model_fp8_linear_workspace(m, n, k)), _raw_stream()))
 
 
+@functools.lru_cache(maxsize=1024)                # by sizes alone
 def model_token_logprobs_workspace(rows, vocab, top_k, dtype):
     b = C.c_int64()
     _check(lib.model_token_logprobs_workspace(rows, vocab, top_k, dtype, C.byref(b)))
@@ -580,9 +592,10 @@ def model_token_logprobs(logits, rows, vocab, tokens, top_k, logprob, entropy, l
     _check(lib.model_token_logprobs(zp, rows, vocab, ld, dtype, temperature, _vec(tokens, rows * n_tokens, torch.int32), n_tokens, top_k,
                                     _vec(logprob, rows * n_tokens), _vec(entropy, rows), _vec(lse, rows), _vec(top_id, rows * top_k, torch.int32),
                                     _vec(top_logit, rows * top_k), _vec(top_logprob, rows * top_k),
-                                    _room(workspace, model_token_logprobs_workspace(rows, vocab, top_k, dtype)), _stream()))
+                                    _room(workspace, model_token_logprobs_workspace(rows, vocab, top_k, dtype)), _raw_stream()))
 
 
+@functools.lru_cache(maxsize=1024)                # by sizes alone
 def model_loss_distill_workspace(rows, vocab, dtype):
     b = C.c_int64()
     _check(lib.model_loss_distill_workspace(rows, vocab, dtype, C.byref(b)))
@@ -598,7 +611,7 @@ def model_loss_distill(logits, rows, vocab, top_id, top_logit, loss_rows, loss, 
     top_k = top_id.shape[1]
     _check(lib.model_loss_distill(zp, rows, vocab, ld, dtype, temperature, _vec(top_id, rows * top_k, torch.int32), _vec(top_logit, rows * top_k),
                                   top_k, _vec(teacher_lse, rows), _vec(weight, rows), _vec(loss_rows, rows), _vec(loss, 1), gp, ldd,
-                                  _room(workspace, model_loss_distill_workspace(rows, vocab, dtype)), _stream()))
+                                  _room(workspace, model_loss_distill_workspace(rows, vocab, dtype)), _raw_stream()))
 
 
 def model_calibrate_mfma(lds_reads, random_data=0, iters=4000):

@@ -65,6 +65,39 @@ template <typename T> __device__ __forceinline__ float round_to_storage(float v)
 template <> __device__ __forceinline__ float round_to_storage<float>(float v) { return v; }
 template <> __device__ __forceinline__ float round_to_storage<bf16_t>(float v) { return bf16_to_f32(f32_to_bf16(v)); }
 
+// Reductions over lanes without a trip through LDS; every lane receives the result.
+// over the 16 lanes of a row of lanes: rotations by 8, 4, 2, 1
+template <int BY> __device__ __forceinline__ float row_turned(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + BY, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float max16(float v) {
+  v = fmaxf(v, row_turned<8>(v));
+  v = fmaxf(v, row_turned<4>(v));
+  v = fmaxf(v, row_turned<2>(v));
+  return fmaxf(v, row_turned<1>(v));
+}
+__device__ __forceinline__ float sum16(float v) {
+  v += row_turned<8>(v);
+  v += row_turned<4>(v);
+  v += row_turned<2>(v);
+  return v + row_turned<1>(v);
+}
+// over lanes l, l + 16, l + 32, l + 48 (mod 64): halves, then rows, change places with themselves
+__device__ __forceinline__ float max_rows(float v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  const u2 h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+  const u2 q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float sum_rows(float v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  const u2 h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  const u2 q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
 // Sum over the 64 lanes of a wavefront; every lane receives the total.
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

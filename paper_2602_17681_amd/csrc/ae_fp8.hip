@@ -72,25 +72,6 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
 // row groups, and both orientations come from one read.  Transposed codes go through LDS to be written as whole 16-byte
 // pieces of a row of x^T.
 constexpr int QT_STRIDE = BLK / 4 + 1;    // words of a transposed row in LDS: eight rows on, as far as neighbouring lanes write, are 8 banks on
-// maximum over the 16 lanes of a row of lanes, in all of them
-__device__ __forceinline__ float max16(float v) {
-  auto turned = [](float x, auto by) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(by)::value, 0xF, 0xF, false));      // row_ror
-  };
-  v = fmaxf(v, turned(v, std::integral_constant<int, 8>()));
-  v = fmaxf(v, turned(v, std::integral_constant<int, 4>()));
-  v = fmaxf(v, turned(v, std::integral_constant<int, 2>()));
-  return fmaxf(v, turned(v, std::integral_constant<int, 1>()));
-}
-// maximum over lanes l, l + 16, l + 32, l + 48 (mod 64)
-__device__ __forceinline__ float max_rows(float v) {
-  typedef unsigned u2 __attribute__((ext_vector_type(2)));
-  const u2 h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
-  const u2 q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-
 struct QuantizeArgs {
   int rows, cols, tiles_c;
   uint8_t* q;

@@ -61,6 +61,10 @@ __device__ __forceinline__ uint32_t order_key(float z) {
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 __device__ __forceinline__ uint64_t order_key(float z, int index) { return ((uint64_t)order_key(z) << 32) | (0xFFFFFFFFu - (uint32_t)index); }
+__device__ __forceinline__ float key_logit(uint64_t k) {
+  const uint32_t u = (uint32_t)(k >> 32);
+  return u == 0 ? __uint_as_float(0x7FC00000u) : __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
 __device__ __forceinline__ int key_index(uint64_t k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
 
 // running statistics of a set of logits: maximum, sum of e_j, sum of e_j (z_j - m)
@@ -81,22 +85,29 @@ __device__ __forceinline__ Stats join(const Stats& x, const Stats& y, float c2) 
   return r;
 }
 __device__ __forceinline__ Stats wave_join(Stats v, float c2) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const Stats o = {__shfl_xor(v.m, off, 64), __shfl_xor(v.s, off, 64), __shfl_xor(v.a, off, 64)};
-    v = join(v, o, c2);
-  }
-  return v;
+  Stats r;
+  r.m = max_rows(max16(v.m));
+  const float d = fmaxf(v.m - reference(r.m), -FLT_MAX), f = fast_exp2(d * c2);
+  r.s = sum_rows(sum16(f * v.s));
+  r.a = sum_rows(sum16(shifted(v.a, v.s, d, f)));
+  return r;
 }
 __device__ __forceinline__ Stats block_join(Stats v, float c2, Stats* sm /* NW */) {
   v = wave_join(v, c2);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = sm[0];
+  float m = sm[0].m;
 #pragma unroll
-  for (int i = 1; i < NW; ++i) v = join(v, sm[i], c2);
-  return v;
+  for (int i = 1; i < NW; ++i) m = fmaxf(m, sm[i].m);
+  Stats r = {m, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    const float d = fmaxf(sm[i].m - reference(m), -FLT_MAX), f = fast_exp2(d * c2);
+    r.s += f * sm[i].s;
+    r.a += shifted(sm[i].a, sm[i].s, d, f);
+  }
+  return r;
 }
 
 constexpr int UNROLL = 4;                // vectors in flight
@@ -123,107 +134,216 @@ __device__ __forceinline__ void for_vectors(const T* p, int n, F f) {
 }
 
 // ---- top list ------------------------------------------------------------------------------------------------------
+constexpr int GROUPS = 8;                // parts of a thread's share whose maxima are kept
 struct TopShared {
   uint64_t cand[CAND];
   uint32_t tmax[NT];
+  uint16_t gmax[GROUPS][NT];             // upper halves of the keys of the parts' maxima, 0: no elements
+  uint32_t pairs[CAND];
   int hist[256];
-  int count, digit, before;
+  int sums[NW];
+  int count, n_pairs, digit, before;
   uint32_t threshold;
 };
 
-// Leaves in sh.cand the sh.count >= min(k, all) largest keys, unordered, at most CAND.  `each(f)` calls f(key) for the
-// thread's share of the keys; tmax is the upper half of the share's largest key, 0 for an empty share.
-// The k-th largest of the threads' maxima is a lower bound of the k-th largest key, since those maxima are k keys
-// themselves; as the largest keys lie in different shares for the most part, few others pass it.  Only threads whose
-// maximum passes go over their share again.  Where more keys pass than LDS holds (long runs of equal logits, maxima in
-// one share), the bound is sharpened by digits of the whole key.
-template <typename E>
-__device__ void top_select(TopShared& sh, int k, uint32_t tmax, E each) {
+// adds the keys of the lanes that want it; lanes of a wavefront take their places with one atomic
+__device__ __forceinline__ void push(TopShared& sh, bool want, uint64_t key) {
+  const uint64_t m = __ballot(want);
+  if (!want) return;
+  const int lane = threadIdx.x & 63, first = __ffsll((unsigned long long)m) - 1;
+  int at = 0;
+  if (lane == first) at = atomicAdd(&sh.count, __popcll(m));
+  at = __shfl(at, first, 64) + __popcll(m & ((1ull << lane) - 1));
+  if (at < CAND) sh.cand[at] = key;
+}
+
+// The k-th largest of the threads' maxima, which is at most the k-th largest key, since those maxima are k keys
+// themselves, and not much less, since the largest keys lie in different shares for the most part.  The leading bits will
+// do: all that a positive bfloat16 has, nine of a binary32 number's fraction.
+constexpr int BOUND_BITS = 18;
+__device__ uint32_t top_bound(TopShared& sh, int k, uint32_t tmax) {
   const int t = threadIdx.x, lane = t & 63;
   __syncthreads();
   sh.tmax[t] = tmax;
-  if (t == 0) sh.count = 0;
+  if (t == 0) sh.count = sh.n_pairs = 0;
   __syncthreads();
   if (t < 64) {
-    uint32_t v[NT / 64];
+    uint32_t v[NW];
 #pragma unroll
-    for (int i = 0; i < NT / 64; ++i) v[i] = sh.tmax[lane + 64 * i];
+    for (int i = 0; i < NW; ++i) v[i] = sh.tmax[lane + 64 * i];
     uint32_t bound = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31; bit >= 32 - BOUND_BITS; --bit) {
       const uint32_t c = bound | (1u << bit);
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < NT / 64; ++i) n += __popcll(__ballot(v[i] >= c));
+      for (int i = 0; i < NW; ++i) n += __popcll(__ballot(v[i] >= c));
       if (n >= k) bound = c;
       if (n == k) break;
     }
     if (lane == 0) sh.threshold = bound;
   }
   __syncthreads();
-  const uint32_t bound = sh.threshold;
-  if (tmax >= bound) {
-    each([&](uint64_t key) {
-      if ((uint32_t)(key >> 32) >= bound) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < CAND) sh.cand[at] = key;
-      }
-    });
+  return sh.threshold;
+}
+
+// Where more keys reach the bound than LDS holds (long runs of equal logits, many large ones in one share): the exact value
+// of the k-th largest, by its digits if the bound is not it already; then what is larger, in any order, and of what
+// is equal the first ones in the order of the index.  (A share of nothing but NaN counts as -infinity in the bound, which
+// may then be too high.)  A source gives its keys in steps of W to a thread, in that order.
+template <typename Src>
+__device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, const Src& src) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  constexpr int W = Src::W;
+  uint64_t key[W];
+  __syncthreads();
+  if (t == 0) sh.count = 0;
+  __syncthreads();
+  for (int s = 0; s < src.steps(); ++s) {
+    const int n = src.load(s, key);
+    int more = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) more += i < n && (uint32_t)(key[i] >> 32) > bound ? 1 : 0;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) more += __shfl_xor(more, off, 64);
+    if (lane == 0 && more) atomicAdd(&sh.count, more);
   }
   __syncthreads();
-  int count = sh.count;
-  if (count >= k && count <= CAND) return;
-  uint64_t prefix = 0;
-  int want = k;                          // how many of the keys that share the prefix belong to the list
-  for (int d = 7; d >= 0; --d) {
-    __syncthreads();
-    if (t < 256) sh.hist[t] = 0;
-    __syncthreads();
-    each([&](uint64_t key) {
-      if (d == 7 || (key >> (8 * d + 8)) == (prefix >> (8 * d + 8))) {
-        const int digit = (int)(key >> (8 * d)) & 255;
-        const int first = __builtin_amdgcn_readfirstlane(digit);
-        const uint64_t same = __ballot(digit == first);          // lanes of equal digits add once, not one after the other
-        if (digit == first) {
-          if (lane == __ffsll((unsigned long long)same) - 1) atomicAdd(&sh.hist[digit], __popcll(same));
-        } else {
-          atomicAdd(&sh.hist[digit], 1);
+  uint32_t value = bound;
+  int larger = sh.count;
+  if (larger >= k || too_high) {
+    value = 0;
+    larger = 0;                          // keys known to be larger than every one with the prefix `value`
+    for (int d = 3; d >= 0; --d) {
+      __syncthreads();
+      if (t < 256) sh.hist[t] = 0;
+      __syncthreads();
+      for (int s = 0; s < src.steps(); ++s) {
+        const int n = src.load(s, key);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const uint32_t v = (uint32_t)(key[i] >> 32);
+          if (i < n && (d == 3 || (v >> (8 * d + 8)) == (value >> (8 * d + 8)))) {
+            const int digit = (int)(v >> (8 * d)) & 255;
+            const int first = __builtin_amdgcn_readfirstlane(digit);
+            const uint64_t same = __ballot(digit == first);        // lanes of equal digits add once, not one after the other
+            if (digit != first) atomicAdd(&sh.hist[digit], 1);
+            else if (lane == __ffsll((unsigned long long)same) - 1) atomicAdd(&sh.hist[digit], __popcll(same));
+          }
         }
       }
-    });
-    __syncthreads();
-    if (t == 0) {
-      int above = 0, at = 255;
-      while (at > 0 && above + sh.hist[at] < want) above += sh.hist[at--];
-      sh.digit = at;
-      sh.before = above;
+      __syncthreads();
+      if (t == 0) {
+        int above = larger, at = 255;
+        while (at > 0 && above + sh.hist[at] < k) above += sh.hist[at--];
+        sh.digit = at;
+        sh.before = above;
+      }
+      __syncthreads();
+      value |= (uint32_t)sh.digit << (8 * d);
+      larger = sh.before;
     }
-    __syncthreads();
-    prefix |= (uint64_t)sh.digit << (8 * d);
-    want -= sh.before;
-    if (k - want + sh.hist[sh.digit] <= CAND) break;             // everything from the prefix on fits
   }
   __syncthreads();
   if (t == 0) sh.count = 0;
   __syncthreads();
-  each([&](uint64_t key) {
-    if (key >= prefix) {
-      const int at = atomicAdd(&sh.count, 1);
-      if (at < CAND) sh.cand[at] = key;
+  if (larger > 0) {
+    for (int s = 0; s < src.steps(); ++s) {
+      const int n = src.load(s, key);
+#pragma unroll
+      for (int i = 0; i < W; ++i) push(sh, i < n && (uint32_t)(key[i] >> 32) > value, key[i]);
     }
-  });
+  }
+  __syncthreads();
+  int have = larger;                     // fewer than k <= CAND
+  for (int s = 0; s < src.steps() && have < k; ++s) {
+    const int n = src.load(s, key);
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) mine += i < n && (uint32_t)(key[i] >> 32) == value ? 1 : 0;
+    int upto = mine;                     // in the lanes up to this one
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int o = __shfl_up(upto, off, 64);
+      if (lane >= off) upto += o;
+    }
+    if (lane == 63) sh.sums[wave] = upto;
+    __syncthreads();
+    int at = have + upto - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      if (w < wave) at += sh.sums[w];
+      total += sh.sums[w];
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (i < n && (uint32_t)(key[i] >> 32) == value) {
+        if (at < k) sh.cand[at] = key[i];
+        ++at;
+      }
+    have += total;
+    __syncthreads();
+  }
+  if (t == 0) sh.count = have < k ? have : k;
   __syncthreads();
 }
-// Calls f(rank, key) for the k largest candidates; keys differ, so a key's rank is the number of larger ones.
+
+// Calls f(rank, key) for the k largest candidates; keys differ, so a key's rank is the number of larger ones.  A few lanes
+// share a candidate while there are more lanes than candidates.
 template <typename F>
-__device__ void top_ranked(const TopShared& sh, int k, F f) {
-  const int count = sh.count < CAND ? sh.count : CAND;
-  for (int i = threadIdx.x; i < count; i += NT) {
-    const uint64_t key = sh.cand[i];
+__device__ void top_ranked(TopShared& sh, int k, F f) {
+  const int count = sh.count, t = threadIdx.x;
+  const int lanes = count <= NT / 8 ? 8 : count <= NT / 4 ? 4 : count <= NT / 2 ? 2 : 1;
+  const int step = 4 * lanes, whole = (count + step - 1) / step * step;
+  for (int i = count + t; i < whole; i += NT) sh.cand[i] = 0;          // room for them: CAND is a multiple of 32
+  __syncthreads();
+  for (int i0 = 0; i0 < count; i0 += NT / lanes) {
+    const int i = i0 + t / lanes;
+    const uint64_t key = i < count ? sh.cand[i] : ~0ull;
     int rank = 0;
-    for (int j = 0; j < count; ++j) rank += sh.cand[j] > key ? 1 : 0;
-    if (rank < k) f(rank, key);
+    for (int j = 4 * (t & (lanes - 1)); j < whole; j += step) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) rank += sh.cand[j + u] > key ? 1 : 0;
+    }
+    for (int off = 1; off < lanes; off <<= 1) rank += __shfl_xor(rank, off, 64);
+    if (i < count && rank < k && (t & (lanes - 1)) == 0) f(rank, key);
   }
 }
+
+// the logits of a row piece as a source of keys
+template <typename T>
+struct RowKeys {
+  static constexpr int W = Store<T>::VEC;
+  const T* z;
+  int n, c0;
+  __device__ int steps() const { return (n + NT * W - 1) / (NT * W); }
+  __device__ int load(int s, uint64_t (&key)[W]) const {
+    const int c = (s * NT + (int)threadIdx.x) * W, left = n - c;
+    float v[W];
+    if (left >= W) load_vec<T>(z + c, v);
+    else load_vec_tail<T>(z + c, left, v);
+#pragma unroll
+    for (int i = 0; i < W; ++i) key[i] = order_key(v[i], c0 + c + i);
+    return left < 0 ? 0 : left < W ? left : W;
+  }
+};
+// the lists of a row's pieces, each in falling order
+struct ListKeys {
+  static constexpr int W = 1;
+  const uint64_t* keys;
+  int n, lists, len;
+  // a thread's share: one list, every (NT / lists)-th rank of it, so that the largest keys are maxima of different shares
+  __device__ int rounds() const { return (len + NT / lists - 1) / (NT / lists); }
+  __device__ uint64_t share(int j) const {
+    const int ranks = NT / lists, t = threadIdx.x, list = t % lists, rank = t / lists + j * ranks;
+    return t < ranks * lists && rank < len ? keys[list * len + rank] : 0;
+  }
+  __device__ int steps() const { return (n + NT - 1) / NT; }
+  __device__ int load(int s, uint64_t (&key)[1]) const {
+    const int i = s * NT + (int)threadIdx.x;
+    key[0] = i < n ? keys[i] : 0;
+    return key[0] != 0 ? 1 : 0;
+  }
+};
 
 struct LogprobArgs {
   const void* logits;
@@ -260,35 +380,48 @@ __device__ void write_row(const LogprobArgs& p, int64_t row, const Stats& st) {
     p.logprob[row * p.n_tokens + i] = id >= 0 && id < p.vocab ? log_prob(Store<T>::ld(z + id), r, p.temp) : 0.0f;
   }
 }
-template <typename T>
-__device__ void write_top(const LogprobArgs& p, int64_t row, const RowLog& r, int rank, uint64_t key) {
-  const int id = key_index(key);
-  const float z = Store<T>::ld((const T*)p.logits + row * p.ld + id);
+__device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const RowLog& r, int rank, uint64_t key) {
+  const float z = key_logit(key);
   const int64_t at = row * p.top_k + rank;
-  if (p.top_id) p.top_id[at] = id;
+  if (p.top_id) p.top_id[at] = key_index(key);
   if (p.top_logit) p.top_logit[at] = z;
   if (p.top_logprob) p.top_logprob[at] = log_prob(z, r, p.temp);
 }
 
 // One workgroup per row piece; with one piece per row it writes the results, otherwise what k_logprob_join needs.
-template <typename T, bool TOP>
-__global__ __launch_bounds__(NT) void k_logprob(LogprobArgs p) {
-  constexpr int V = Store<T>::VEC;
+template <typename T, bool TOP, bool ENT>
+__global__ __launch_bounds__(NT, 4) void k_logprob(LogprobArgs p) {
+  constexpr int V = Store<T>::VEC, STEP = NT * V;
   __shared__ Stats sm[NW];
   __shared__ TopShared sh;
   const int64_t row = blockIdx.x / p.splits;
-  const int split = (int)(blockIdx.x - row * p.splits);
+  const int split = (int)(blockIdx.x - row * p.splits), t = threadIdx.x;
   const int c0 = split * p.chunk;
   const int n = p.vocab - c0 < p.chunk ? p.vocab - c0 : p.chunk;
   const T* z = (const T*)p.logits + row * p.ld + c0;
   const float c2 = kLog2e / p.temp;
+  const int rounds = (n + UNROLL * STEP - 1) / (UNROLL * STEP), per = (rounds + GROUPS - 1) / GROUPS;      // rounds of loads, and to a group
   Stats st = {-INFINITY, 0.0f, 0.0f};
-  bool some = false;
-  for_vectors<T>(z, n, [&](const float (&v)[V], int, int) {
-    float cm = v[0];
+  float gm = -INFINITY;
+  for (int r = 0; r < rounds; ++r) {
+    const int base = r * UNROLL * STEP + t * V;
+    float v[UNROLL][V];
+    if ((r + 1) * UNROLL * STEP <= n) {
 #pragma unroll
-    for (int i = 1; i < V; ++i) cm = fmaxf(cm, v[i]);
-    some = true;
+      for (int u = 0; u < UNROLL; ++u) load_vec<T>(z + base + u * STEP, v[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        const int c = base + u * STEP;
+        if (c + V <= n) load_vec<T>(z + c, v[u]);
+        else load_vec_tail<T>(z + c, n - c, v[u]);
+      }
+    }
+    float cm = v[0][0];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+      for (int i = 0; i < V; ++i) cm = fmaxf(cm, v[u][i]);
     if (cm > st.m) {
       const float d = fmaxf(st.m - cm, -FLT_MAX), f = fast_exp2(d * c2);
       st.a = shifted(st.a, st.s, d, f);
@@ -296,35 +429,78 @@ __global__ __launch_bounds__(NT) void k_logprob(LogprobArgs p) {
       st.m = cm;
     }
     const float ref = reference(st.m);
+    float a = 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float d = v[i] - ref, e = fast_exp2(d * c2);
-      st.s += e;
-      st.a += e * fmaxf(d, -FLT_MAX);
+    for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = v[u][i] - ref, e = fast_exp2(d * c2);
+        st.s += e;
+        if constexpr (ENT) a = fmaf(e, d, a);
+      }
+    if constexpr (ENT) {
+      if (a != a) {                      // 0 times -infinity among them: those have no part in the sum
+        a = 0.0f;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float d = v[u][i] - ref, e = fast_exp2(d * c2);
+            a = fmaf(e, fmaxf(d, -FLT_MAX), a);
+          }
+      }
+      st.a += a;
     }
-  });
-  const uint32_t tmax = some ? order_key(st.m) : 0u;
+    if constexpr (TOP) {
+      gm = fmaxf(gm, cm);
+      if (r % per == per - 1 || r == rounds - 1) {
+        sh.gmax[r / per][t] = r / per * per * UNROLL * STEP + t * V < n ? (uint16_t)(order_key(gm) >> 16) : (uint16_t)0;
+        gm = -INFINITY;
+      }
+    }
+  }
+  const uint32_t tmax = t * V < n ? order_key(st.m) : 0u;
   const Stats all = block_join(st, c2, sm);
-  if (p.splits == 1) write_row<T>(p, row, all);
-  else if (threadIdx.x == 0) p.part[row * p.splits + split] = all;
+  if (p.splits > 1 && t == 0) p.part[row * p.splits + split] = all;
   if constexpr (TOP) {
     const int k = p.top_k < n ? p.top_k : n;
-    top_select(sh, k, tmax, [&](auto f) {
-      for_vectors<T>(z, n, [&](const float (&v)[V], int c, int len) {
+    const uint32_t bound = top_bound(sh, k, tmax);
+    // the parts of shares that reach the bound, then their vectors, one to a thread
+    if (tmax >= bound) {
+      for (int g = 0; g * per < rounds; ++g)
+        if (sh.gmax[g][t] >= (bound >> 16)) {
+          const int at = atomicAdd(&sh.n_pairs, 1);
+          if (at < CAND) sh.pairs[at] = (uint32_t)(g << 16 | t);
+        }
+    }
+    __syncthreads();
+    const int pairs = sh.n_pairs, width = per * UNROLL;
+    if (pairs <= CAND) {
+      for (int i = t; i < pairs * width; i += NT) {
+        const int pair = i / width;
+        const uint32_t g = sh.pairs[pair] >> 16, owner = sh.pairs[pair] & 0xFFFF;
+        const int c = ((int)g * width + (i - pair * width)) * STEP + (int)owner * V, left = n - c;
+        if (left <= 0) continue;
+        float v[V];
+        if (left >= V) load_vec<T>(z + c, v);
+        else load_vec_tail<T>(z + c, left, v);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < len) f(order_key(v[i], c0 + c + i));
-      });
-    });
+        for (int j = 0; j < V; ++j) push(sh, j < left && order_key(v[j]) >= bound, order_key(v[j], c0 + c + j));
+      }
+    }
+    __syncthreads();
+    const int found = sh.count;
+    if (pairs > CAND || found < k || found > CAND) top_exact(sh, k, bound, pairs <= CAND && found < k, RowKeys<T>{z, n, c0});
     if (p.splits == 1) {
       const RowLog r = row_log(all);
-      top_ranked(sh, k, [&](int rank, uint64_t key) { write_top<T>(p, row, r, rank, key); });
+      top_ranked(sh, k, [&](int rank, uint64_t key) { write_top(p, row, r, rank, key); });
     } else {
       uint64_t* out = p.part_top + (row * p.splits + split) * p.top_k;
       top_ranked(sh, k, [&](int rank, uint64_t key) { out[rank] = key; });
-      for (int i = k + (int)threadIdx.x; i < p.top_k; i += NT) out[i] = 0;
+      for (int i = k + t; i < p.top_k; i += NT) out[i] = 0;
     }
   }
+  if (p.splits == 1) write_row<T>(p, row, all);
 }
 
 // One workgroup per row: joins its pieces.
@@ -334,6 +510,14 @@ __global__ __launch_bounds__(NT) void k_logprob_join(LogprobArgs p) {
   __shared__ TopShared sh;
   const int64_t row = blockIdx.x;
   const float c2 = kLog2e / p.temp;
+  const ListKeys src = {p.part_top + row * p.splits * p.top_k, p.splits * p.top_k, p.splits, p.top_k};
+  uint32_t tmax = 0;
+  if constexpr (TOP) {
+    for (int j = 0; j < src.rounds(); ++j) {
+      const uint32_t h = (uint32_t)(src.share(j) >> 32);
+      tmax = h > tmax ? h : tmax;
+    }
+  }
   if (threadIdx.x < 64) {
     Stats st = {-INFINITY, 0.0f, 0.0f};
     if ((int)threadIdx.x < p.splits) st = p.part[row * p.splits + threadIdx.x];
@@ -342,24 +526,21 @@ __global__ __launch_bounds__(NT) void k_logprob_join(LogprobArgs p) {
   }
   __syncthreads();
   const Stats all = sm;
-  write_row<T>(p, row, all);
   if constexpr (TOP) {
-    const uint64_t* keys = p.part_top + row * p.splits * p.top_k;
-    const int n = p.splits * p.top_k;
-    uint32_t tmax = 0;
-    for (int i = threadIdx.x; i < n; i += NT) {
-      const uint32_t h = (uint32_t)(keys[i] >> 32);
-      tmax = h > tmax ? h : tmax;
-    }
-    top_select(sh, p.top_k, tmax, [&](auto f) {
-      for (int i = threadIdx.x; i < n; i += NT) {
-        const uint64_t key = keys[i];
-        if (key != 0) f(key);
+    const uint32_t bound = top_bound(sh, p.top_k, tmax);
+    if (tmax >= bound) {
+      for (int j = 0; j < src.rounds(); ++j) {
+        const uint64_t key = src.share(j);
+        push(sh, key != 0 && (uint32_t)(key >> 32) >= bound, key);
       }
-    });
+    }
+    __syncthreads();
+    const int found = sh.count;
+    if (found < p.top_k || found > CAND) top_exact(sh, p.top_k, bound, found < p.top_k, src);
     const RowLog r = row_log(all);
-    top_ranked(sh, p.top_k, [&](int rank, uint64_t key) { write_top<T>(p, row, r, rank, key); });
+    top_ranked(sh, p.top_k, [&](int rank, uint64_t k) { write_top(p, row, r, rank, k); });
   }
+  write_row<T>(p, row, all);
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------
@@ -654,7 +835,8 @@ extern "C" int model_token_logprobs(const void* logits, int64_t rows, int64_t vo
   const dim3 grid((unsigned)(rows * p.splits)), grid_j((unsigned)rows);
 #define LOGPROB(T, TOP)                                                        \
   do {                                                                         \
-    hipLaunchKernelGGL((k_logprob<T, TOP>), grid, dim3(NT), 0, s, p);          \
+    if (entropy) hipLaunchKernelGGL((k_logprob<T, TOP, true>), grid, dim3(NT), 0, s, p);      \
+    else hipLaunchKernelGGL((k_logprob<T, TOP, false>), grid, dim3(NT), 0, s, p);             \
     if (p.splits > 1) hipLaunchKernelGGL((k_logprob_join<T, TOP>), grid_j, dim3(NT), 0, s, p); \
   } while (0)
   if (dtype == AE_BF16) { if (top) LOGPROB(bf16_t, true); else LOGPROB(bf16_t, false); }
