@@ -82,6 +82,27 @@ __device__ __forceinline__ float sum16(float v) {
   v += row_turned<2>(v);
   return v + row_turned<1>(v);
 }
+template <int BY> __device__ __forceinline__ double row_turned(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, 0x120 + BY, 0xF, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), 0x120 + BY, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sum16(double v) {
+  v += row_turned<8>(v);
+  v += row_turned<4>(v);
+  v += row_turned<2>(v);
+  return v + row_turned<1>(v);
+}
+// of N <= 16 values in LDS, one to a lane (a loop over them would hold them all in registers)
+template <int N> __device__ __forceinline__ float max_of(const float* sm) {
+  const int i = threadIdx.x & 15;
+  return max16(sm[i < N ? i : 0]);
+}
+template <int N, typename F> __device__ __forceinline__ F sum_of(const F* sm) {
+  const int i = threadIdx.x & 15;
+  return sum16(i < N ? sm[i] : F(0));
+}
 // over lanes l, l + 16, l + 32, l + 48 (mod 64): halves, then rows, change places with themselves
 __device__ __forceinline__ float max_rows(float v) {
   typedef unsigned u2 __attribute__((ext_vector_type(2)));

@@ -557,7 +557,7 @@ struct DistillArgs {
   const float* top_logit;
   int top_k;
   const float *teacher_lse, *weight;
-  float* loss_rows;
+  float *loss_rows, *loss;               // loss: null where another launch adds up the rows
   void* d_logits;
   int64_t ldd;
   DistillPart* part;                     // [rows][splits]
@@ -576,36 +576,54 @@ __device__ __forceinline__ DistillPart join(const DistillPart& x, const DistillP
   return r;
 }
 
+// exp(x) to binary32 precision of an x in binary64 (whose binary32 rounding would cost |x| 2^-24): whole powers of two taken
+// out.  The teacher's binary32 numbers define its probabilities no better.
+__device__ __forceinline__ double exp_of(double x) {
+  const double y = x * 1.4426950408889634074, i = rint(y);
+  const float f = (float)(y - i);                // |f| <= 1/2; NaN for infinities
+  const float e = fast_exp2(f == f ? f : x < 0.0 ? -INFINITY : (float)x);
+  return (double)ldexpf(e, (int)fmaxf(fminf((float)i, 300.0f), -300.0f));
+}
+
+// log(x) of an x in binary64, likewise: off by binary32 roundings of a number below 0.35, not of the logarithm's size
+__device__ __forceinline__ double log_of(double x) {
+  int i;
+  const double h = frexp(x, &i);                 // in [1/2, 1)
+  const bool low = h < 0.70710678118654752440;
+  return (double)logf((float)(low ? 2.0 * h : h)) + (double)(low ? i - 1 : i) * 0.69314718055994530942;
+}
+
 // the logarithm of the sum that the teacher's probabilities are divided by
-__device__ double list_norm(const DistillArgs& p, int64_t row, double* sm /* NW + 1 */) {
+template <int NTH>
+__device__ double list_norm(const DistillArgs& p, int64_t row, double* sm /* NTH / 64 + 1 */) {
   if (p.teacher_lse) return (double)p.teacher_lse[row];
   const int* id = p.top_id + row * p.top_k;
   const float* t = p.top_logit + row * p.top_k;
   float m = -INFINITY;
-  for (int i = threadIdx.x; i < p.top_k; i += NT)
+  for (int i = threadIdx.x; i < p.top_k; i += NTH)
     if (id[i] >= 0 && id[i] < p.vocab) m = fmaxf(m, t[i]);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  m = max_rows(max16(m));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = (double)m;
   __syncthreads();
   double dm = sm[0];
-  for (int i = 1; i < NW; ++i) dm = sm[i] > dm ? sm[i] : dm;
+  for (int i = 1; i < NTH / 64; ++i) dm = sm[i] > dm ? sm[i] : dm;
   if (dm == -INFINITY) dm = 0.0;
   double s = 0.0;
-  for (int i = threadIdx.x; i < p.top_k; i += NT)
-    if (id[i] >= 0 && id[i] < p.vocab) s += exp(((double)t[i] - dm) / (double)p.temp);
+  for (int i = threadIdx.x; i < p.top_k; i += NTH)
+    if (id[i] >= 0 && id[i] < p.vocab) s += exp_of(((double)t[i] - dm) / (double)p.temp);
   __syncthreads();
-  s = block_sum<NT>(s, sm);
-  return dm / (double)p.temp + log(s);
+  s = block_sum<NTH>(s, sm);
+  return dm / (double)p.temp + log_of(s);
 }
 __device__ __forceinline__ double list_log_p(const DistillArgs& p, int64_t at, double norm) { return (double)p.top_logit[at] / (double)p.temp - norm; }
 
 // marks the list's tokens that lie in columns [c0, c0 + n): a bit for each column
+template <int NTH>
 __device__ void mark_list(const DistillArgs& p, int64_t row, int c0, int n, uint32_t* bits) {
-  for (int i = threadIdx.x; i < (n + 31) / 32; i += NT) bits[i] = 0u;
+  for (int i = threadIdx.x; i < (n + 31) / 32; i += NTH) bits[i] = 0u;
   __syncthreads();
-  for (int i = threadIdx.x; i < p.top_k; i += NT) {
+  for (int i = threadIdx.x; i < p.top_k; i += NTH) {
     const int id = p.top_id[row * p.top_k + i];
     if (id >= c0 && id < c0 + n) atomicOr(&bits[(id - c0) >> 5], 1u << ((id - c0) & 31));
   }
@@ -648,7 +666,7 @@ __device__ DistillPart piece_stats(const DistillArgs& p, int64_t row, int c0, in
   for (int i = threadIdx.x; i < p.top_k; i += NT) {
     const int id = p.top_id[row * p.top_k + i];
     if (id < c0 || id >= c0 + n) continue;
-    const double lp = list_log_p(p, row * p.top_k + i, norm), pi = exp(lp);
+    const double lp = list_log_p(p, row * p.top_k + i, norm), pi = exp_of(lp);
     st.p += pi;
     if (pi != 0.0) st.l += pi * (lp - (double)Store<T>::ld(z + id - c0) / (double)p.temp);
   }
@@ -666,51 +684,83 @@ __device__ DistillPart piece_stats(const DistillArgs& p, int64_t row, int c0, in
   return st;
 }
 
-// The loss of a row and the gradient of columns [c0, c0 + n) from the statistics of the whole row.
-template <typename T>
-__device__ void piece_gradient(const DistillArgs& p, int64_t row, int c0, int n, const uint32_t* bits, double norm, float c2, float w,
-                               const DistillPart& st, bool write_loss) {
-  constexpr int V = Store<T>::VEC;
+// What the statistics of a whole row give.  The loss, with its logarithms in binary64, is for one wavefront to compute.
+struct RowGrad {
+  float ref, f_out, s_all;               // what exponents are relative to; the gradient outside the list is f_out e_j; sum of e_j
+  double mass, rest, scale;              // P, p_r, w / T
+  bool empty;
+};
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillPart& st, float w) {
+  RowGrad r;
+  r.ref = reference(st.m);
+  r.s_all = st.s_out + st.s_in;
+  r.empty = r.s_all == 0.0f;
+  r.rest = p.teacher_lse ? 1.0 - st.p : 0.0;
+  if (!(r.rest > 0.0) && r.rest == r.rest) r.rest = 0.0;
+  if (st.s_out == 0.0f) r.rest = 0.0;
+  r.mass = st.p + r.rest;
+  const float scale = w / p.temp;
+  r.scale = (double)scale;
+  // P - p_r / q_r, over the sum
+  const float outside = r.rest != 0.0 ? (float)(r.mass - r.rest * (double)(r.s_all / st.s_out)) : (float)r.mass;
+  r.f_out = r.empty ? 0.0f : outside * scale / r.s_all;
+  return r;
+}
+__device__ float row_loss(const DistillArgs& p, const DistillPart& st, const RowGrad& r) {
+  if (r.empty) return 0.0f;
   const double s_all = (double)st.s_out + (double)st.s_in;
-  const bool empty = s_all == 0.0;
-  const double q_out = (double)st.s_out / s_all;
-  double rest = p.teacher_lse ? 1.0 - st.p : 0.0;
-  if (!(rest > 0.0) && rest == rest) rest = 0.0;
-  if (st.s_out == 0.0f) rest = 0.0;
-  const double mass = st.p + rest;
-  if (write_loss && threadIdx.x == 0) {
-    const double lse = (double)st.m / (double)p.temp + log(s_all);
-    double loss = st.l + (st.p != 0.0 ? st.p * lse : 0.0);
-    if (rest != 0.0) loss += rest * (log(rest) - log(q_out));
-    p.loss_rows[row] = empty ? 0.0f : (float)loss;
+  double loss = st.l + (st.p != 0.0 ? st.p * ((double)st.m / (double)p.temp + log_of(s_all)) : 0.0);
+  if (r.rest != 0.0) loss += r.rest * log_of(r.rest * s_all / (double)st.s_out);
+  return (float)loss;
+}
+// stores the gradient of a vector's columns: those of the list are left as they are, since g may be z, which they still need
+template <typename T>
+__device__ __forceinline__ void store_outside(T* g, const float (&o)[Store<T>::VEC], uint32_t marks, int len) {
+  if (marks == 0 && len >= Store<T>::VEC) {
+    store_vec<T>(g, o);
+  } else {
+#pragma unroll
+    for (int i = 0; i < Store<T>::VEC; ++i)
+      if (i < len && !(marks >> i & 1)) Store<T>::st(g + i, o[i]);
   }
-  if (!p.d_logits) return;
+}
+// the gradient of the list's entries in columns [c0, c0 + n)
+template <typename T, int NTH>
+__device__ void list_gradient(const DistillArgs& p, int64_t row, int c0, int n, double norm, float c2, const RowGrad& r) {
+  const T* z = (const T*)p.logits + row * p.ld;
+  T* g = (T*)p.d_logits + row * p.ldd;
+  for (int i = threadIdx.x; i < p.top_k; i += NTH) {
+    const int id = p.top_id[row * p.top_k + i];
+    if (id < c0 || id >= c0 + n) continue;
+    const double q = (double)(fast_exp2((Store<T>::ld(z + id) - r.ref) * c2) / r.s_all);
+    const double pi = exp_of(list_log_p(p, row * p.top_k + i, norm));
+    Store<T>::st(g + id, r.empty ? 0.0f : (float)((r.mass * q - pi) * r.scale));
+  }
+}
+
+// The gradient of columns [c0, c0 + n) from the statistics of the whole row.
+template <typename T>
+__device__ void piece_gradient(const DistillArgs& p, int64_t row, int c0, int n, const uint32_t* bits, double norm, float c2, const RowGrad& r) {
+  constexpr int V = Store<T>::VEC;
   const T* z = (const T*)p.logits + row * p.ld + c0;
   T* g = (T*)p.d_logits + row * p.ldd + c0;
-  const double scale = (double)w / (double)p.temp;
-  const float f_out = empty ? 0.0f : (float)((mass - (rest != 0.0 ? rest / q_out : 0.0)) * scale / s_all);
-  const float ref = reference(st.m);
   for_vectors<T>(z, n, [&](const float (&v)[V], int c, int len) {
     float o[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = f_out * fast_exp2((v[i] - ref) * c2);
-    const uint32_t mk = marks_of<V>(bits, c);
-    if (mk == 0 && len == V) {
-      store_vec<T>(g + c, o);
-    } else {
-      // the list's entries are left as they are: g may be z, which they still need
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < len && !(mk >> i & 1)) Store<T>::st(g + c + i, o[i]);
-    }
+    for (int i = 0; i < V; ++i) o[i] = r.f_out * fast_exp2((v[i] - r.ref) * c2);
+    store_outside<T>(g + c, o, marks_of<V>(bits, c), len);
   });
-  for (int i = threadIdx.x; i < p.top_k; i += NT) {
-    const int id = p.top_id[row * p.top_k + i];
-    if (id < c0 || id >= c0 + n) continue;
-    const double q = (double)fast_exp2((Store<T>::ld(z + id - c0) - ref) * c2) / s_all;
-    const double pi = exp(list_log_p(p, row * p.top_k + i, norm));
-    Store<T>::st(g + id - c0, empty ? 0.0f : (float)((mass * q - pi) * scale));
-  }
+  list_gradient<T, NT>(p, row, c0, n, norm, c2, r);
+}
+
+// The statistics of a row from those of its pieces, one to a lane; in every lane.
+__device__ DistillPart joined(const DistillArgs& p, int64_t row, float c2) {
+  const int lane = threadIdx.x & 63;
+  DistillPart v = {-INFINITY, 0.0f, 0.0f, 0.0f, 0.0, 0.0};
+  if (lane < p.splits) v = p.part[row * p.splits + lane];
+  const float m = max_rows(max16(v.m));
+  const float f = fast_exp2((v.m - reference(m)) * c2);
+  return {m, sum_rows(sum16(f * v.s_out)), sum_rows(sum16(f * v.s_in)), 0.0f, wave_sum(v.p), wave_sum(v.l)};
 }
 
 template <typename T>
@@ -725,6 +775,20 @@ __device__ void piece_zero(const DistillArgs& p, int64_t row, int c0, int n) {
   }
 }
 
+// The weighted sum of the losses of a few rows in pieces, by one workgroup: it forms every row's loss for itself.
+constexpr int64_t kTotalHere = 2 * NW;           // rows: two to a wavefront
+__device__ void total_of_pieces(const DistillArgs& p, float c2, double* sm /* NW + 1 */) {
+  double acc = 0.0;
+  for (int64_t row = threadIdx.x >> 6; row < p.rows; row += NW) {
+    const float w = p.weight ? p.weight[row] : 1.0f;
+    if (w == 0.0f) continue;
+    const DistillPart st = joined(p, row, c2);
+    if ((threadIdx.x & 63) == 0) acc += (double)w * (double)row_loss(p, st, row_grad(p, st, w));
+  }
+  acc = block_sum<NT>(acc, sm);
+  if (threadIdx.x == 0) *p.loss = (float)acc;
+}
+
 // MODE 0: statistics and gradient of whole rows; 1: statistics of row pieces; 2: gradient of row pieces from joined statistics
 template <typename T, int MODE>
 __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
@@ -736,16 +800,17 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   const int c0 = split * p.chunk;
   const int n = p.vocab - c0 < p.chunk ? p.vocab - c0 : p.chunk;
   const float w = p.weight ? p.weight[row] : 1.0f;
+  const float c2 = kLog2e / p.temp;
   if (w == 0.0f) {
     if (MODE != 1) {
       if (threadIdx.x == 0 && split == 0) p.loss_rows[row] = 0.0f;
+      if (MODE == 2 && p.loss && blockIdx.x == gridDim.x - 1) total_of_pieces(p, c2, smd);
       if (p.d_logits) piece_zero<T>(p, row, c0, n);
     }
     return;
   }
-  const float c2 = kLog2e / p.temp;
-  mark_list(p, row, c0, n, bits);
-  const double norm = list_norm(p, row, smd);
+  mark_list<NT>(p, row, c0, n, bits);
+  const double norm = list_norm<NT>(p, row, smd);
   DistillPart st;
   if constexpr (MODE != 2) {
     st = piece_stats<T>(p, row, c0, n, bits, norm, c2, sm);
@@ -754,10 +819,194 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
       return;
     }
   } else {
-    st = p.part[row * p.splits];
-    for (int i = 1; i < p.splits; ++i) st = join(st, p.part[row * p.splits + i], c2);
+    st = joined(p, row, c2);
   }
-  piece_gradient<T>(p, row, c0, n, bits, norm, c2, w, st, split == 0);
+  const RowGrad r = row_grad(p, st, w);
+  if (threadIdx.x == 0 && split == 0) p.loss_rows[row] = row_loss(p, st, r);
+  if (MODE == 2 && p.loss && blockIdx.x == gridDim.x - 1) total_of_pieces(p, c2, smd);
+  if (p.d_logits) piece_gradient<T>(p, row, c0, n, bits, norm, c2, r);
+}
+
+// Whole rows that fit the registers: a workgroup of NTH threads holds a row, NV vectors to a thread, so that it is read
+// once: 16 vectors in 1 024 threads are 256 KiB, half of a compute unit's registers.  As no more than one or a few
+// workgroups then fit a compute unit, they stay, and ask for a vector of their next row as soon as the gradient of the
+// present one's is stored.  A thread also holds its entry of the list, which is no longer than there are threads.
+template <typename T, int NTH, int NV>
+__global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
+  constexpr int V = Store<T>::VEC, STEP = NTH * V, NWV = NTH / 64;
+  extern __shared__ uint32_t bits[];
+  __shared__ float smf[4][NWV];
+  __shared__ double smd[3][NWV];
+  const int n = p.vocab, k = p.top_k, t = threadIdx.x, wave = t >> 6;
+  const float c2 = kLog2e / p.temp;
+  const double inv_t = 1.0 / (double)p.temp;
+  const int whole = n / V * V;                   // whole vectors, and what is left an element to a thread
+  const int c_tail = whole + t;
+  auto valid = [&](int id) { return id >= 0 && id < n; };
+  auto weight_of = [&](int64_t row) { return row >= p.rows ? 0.0f : p.weight ? p.weight[row] : 1.0f; };
+  int tv = t * V;
+  uint32_t raw[NV][4];
+  // the compiler must not keep what it makes of the row, or of its columns, in one pass for the next: that would take twice
+  // the registers and more
+  auto forget = [&] {
+    asm volatile("" : "+v"(tv));
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(raw[u][i]));
+  };
+  auto load_vector = [&](const T* z, int u, int limit) {
+    const int c = u * STEP + tv;
+    if (c < limit) {
+      __builtin_memcpy(raw[u], reinterpret_cast<const char*>(z) + (uint32_t)c * (uint32_t)sizeof(T), 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[u][i] = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;      // -infinity
+    }
+  };
+  auto element = [&](int u, int i) {
+    return sizeof(T) == 4 ? __uint_as_float(raw[u][i % 4]) : __uint_as_float(i & 1 ? raw[u][i / 2] & 0xFFFF0000u : raw[u][i / 2] << 16);
+  };
+  int id_next = -1;
+  float top_next = 0.0f, tail_next = 0.0f, lse_next = 0.0f;
+  auto ask_for_rest = [&](int64_t r) {           // what a row needs beside its vectors
+    const T* z = (const T*)p.logits + r * p.ld;
+    id_next = t < k ? p.top_id[r * k + t] : -1;
+    top_next = t < k ? p.top_logit[r * k + t] : 0.0f;
+    tail_next = c_tail < n ? Store<T>::ld(z + c_tail) : -INFINITY;
+    lse_next = p.teacher_lse ? p.teacher_lse[r] : 0.0f;
+  };
+  float w = weight_of(blockIdx.x);
+  if (w != 0.0f) ask_for_rest(blockIdx.x);
+  {
+    const T* z = (const T*)p.logits + (int64_t)blockIdx.x * p.ld;
+    const int limit = w != 0.0f ? whole : 0;     // a row without weight is not read
+#pragma unroll
+    for (int u = 0; u < NV; ++u) load_vector(z, u, limit);
+  }
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const T* z = (const T*)p.logits + row * p.ld;
+    T* g = (T*)p.d_logits + row * p.ldd;
+    const float w_next = weight_of(row + gridDim.x);
+    const T* z_next = z + (int64_t)gridDim.x * p.ld;
+    const int limit = w_next != 0.0f ? whole : 0;
+    if (w == 0.0f) {
+      if (t == 0) p.loss_rows[row] = 0.0f;
+      const float o[V] = {};
+      for (int c = t * V; c < n; c += STEP) store_outside<T>(g + c, o, 0u, n - c);
+      if (w_next != 0.0f) ask_for_rest(row + gridDim.x);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) load_vector(z_next, u, limit);
+      w = w_next;
+      continue;
+    }
+    const int id0 = id_next;
+    const float top0 = top_next, z_tail = tail_next;
+    const float z0 = valid(id0) ? Store<T>::ld(z + id0) : 0.0f;
+    for (int i = t; i < (n + 31) / 32; i += NTH) bits[i] = 0u;
+    float tm = valid(id0) ? top0 : -INFINITY;
+    tm = max_rows(max16(tm));
+    if ((t & 63) == 0) smf[0][wave] = tm;
+    __syncthreads();
+    if (valid(id0)) atomicOr(&bits[id0 >> 5], 1u << (id0 & 31));
+    // the logarithm of what the teacher's probabilities are divided by
+    double norm = (double)lse_next;
+    if (!p.teacher_lse) {
+      tm = max_of<NWV>(smf[0]);
+      const double ref_t = tm == -INFINITY ? 0.0 : (double)tm;
+      double s = 0.0;
+      if (valid(id0)) s = exp_of(((double)top0 - ref_t) * inv_t);
+      s = wave_sum(s);
+      if ((t & 63) == 0) smd[0][wave] = s;
+      norm = ref_t * inv_t;                      // and the sum's logarithm, below
+    }
+    float m = z_tail;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) m = fmaxf(m, element(u, i));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    m = max_rows(max16(m));
+    forget();
+    if ((t & 63) == 0) smf[1][wave] = m;
+    __syncthreads();
+    if (!p.teacher_lse && wave * 64 < k) norm += log_of(sum_of<NWV>(smd[0]));      // for wavefronts with entries of the list
+    m = max_of<NWV>(smf[1]);
+    const float ref = reference(m);
+    // e_j of a vector's columns
+    auto exponentials = [&](int u, float (&e)[V]) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = fast_exp2((element(u, i) - ref) * c2);
+    };
+    float s_out = 0.0f, s_in = 0.0f;
+    const float e_tail = fast_exp2((z_tail - ref) * c2);
+    const bool in_tail = c_tail < n && (bits[c_tail >> 5] >> (c_tail & 31) & 1);
+    (in_tail ? s_in : s_out) = e_tail;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = u * STEP + tv;
+      if (u * STEP < whole) {
+        const uint32_t mk = c < whole ? marks_of<V>(bits, c) : 0u;
+        float e[V];
+        exponentials(u, e);
+        if (mk) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            s_in += mk >> i & 1 ? e[i] : 0.0f;
+            e[i] = mk >> i & 1 ? 0.0f : e[i];
+          }
+        }
+        float sum = e[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) sum += e[i];
+        s_out += sum;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    forget();
+    double pi0 = 0.0, sp, sl = 0.0;
+    if (valid(id0)) {
+      const double lp = (double)top0 * inv_t - norm;
+      pi0 = exp_of(lp);
+      if (pi0 != 0.0) sl = pi0 * (lp - (double)z0 * inv_t);
+    }
+    s_out = sum_rows(sum16(s_out));
+    s_in = sum_rows(sum16(s_in));
+    sp = wave_sum(pi0);
+    sl = wave_sum(sl);
+    if ((t & 63) == 0) {
+      smf[2][wave] = s_out;
+      smf[3][wave] = s_in;
+      smd[1][wave] = sp;
+      smd[2][wave] = sl;
+    }
+    __syncthreads();
+    const DistillPart st = {m, sum_of<NWV>(smf[2]), sum_of<NWV>(smf[3]), 0.0f, sum_of<NWV>(smd[1]), sum_of<NWV>(smd[2])};
+    const RowGrad r = row_grad(p, st, w);
+    if (w_next != 0.0f) ask_for_rest(row + gridDim.x);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = u * STEP + tv;
+      if (c < whole) {
+        float o[V];
+        exponentials(u, o);
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] *= r.f_out;
+        store_outside<T>(g + c, o, marks_of<V>(bits, c), V);
+      }
+      load_vector(z_next, u, limit);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (c_tail < n && !in_tail) Store<T>::st(g + c_tail, r.f_out * e_tail);
+    if (valid(id0)) {
+      const double q = (double)(fast_exp2((z0 - ref) * c2) / r.s_all);
+      Store<T>::st(g + id0, r.empty ? 0.0f : (float)((r.mass * q - pi0) * r.scale));
+    }
+    if (t == NTH - 64) p.loss_rows[row] = row_loss(p, st, r);      // the last wavefront: the list is the first ones'
+    w = w_next;
+    __syncthreads();                             // the marks and sums have been read
+  }
 }
 
 // loss = sum of w_r L_r in a fixed order
@@ -773,15 +1022,53 @@ __global__ __launch_bounds__(NT) void k_distill_total(const float* __restrict__ 
   if (threadIdx.x == 0) *loss = (float)acc;
 }
 
-// Pieces of a row: enough workgroups for the chip where rows alone are too few, none shorter than 4 096 columns.
+template <typename T, int NTH, int NV>
+int launch_distill_row(const DistillArgs& p, size_t lds, hipStream_t s) {
+  // 16 vectors: workgroups that stay, as many as the registers of 256 compute units hold (128 to a thread).  Fewer: a row each, since more
+  // of them run at a time (4 096 x 32 000 in bfloat16 124 us, with staying ones 145; 8 192 x 131 072 1 020, a row each 1 090)
+  const int64_t stay = NV == 16 ? 256 * (1024 / NTH) : p.rows;
+  hipLaunchKernelGGL((k_distill_row<T, NTH, NV>), dim3((unsigned)(p.rows < stay ? p.rows : stay)), dim3(NTH), lds, s, p);
+  return launch_status("loss_distill");
+}
+template <typename T>
+int launch_distill_rows(const DistillArgs& p, size_t lds, hipStream_t s) {
+  const int vecs = (p.vocab + Store<T>::VEC - 1) / Store<T>::VEC;
+  if (p.d_logits && p.top_k <= 256) {
+    if (vecs <= 256 * 4) return launch_distill_row<T, 256, 4>(p, lds, s);
+    if (vecs <= 256 * 8) return launch_distill_row<T, 256, 8>(p, lds, s);
+    if (vecs <= 512 * 8) return launch_distill_row<T, 512, 8>(p, lds, s);
+    if (vecs <= 512 * 16) return launch_distill_row<T, 512, 16>(p, lds, s);
+    if (vecs <= 1024 * 16) return launch_distill_row<T, 1024, 16>(p, lds, s);
+  }
+  hipLaunchKernelGGL((k_distill<T, 0>), dim3((unsigned)p.rows), dim3(NT), lds, s, p);
+  return launch_status("loss_distill");
+}
+template <typename T>
+int launch_distill_pieces(const DistillArgs& p, size_t lds, hipStream_t s) {
+  const dim3 grid((unsigned)(p.rows * p.splits));
+  hipLaunchKernelGGL((k_distill<T, 1>), grid, dim3(NT), lds, s, p);
+  hipLaunchKernelGGL((k_distill<T, 2>), grid, dim3(NT), lds, s, p);
+  return launch_status("loss_distill");
+}
+
+// Rows in pieces of at least 4 096 columns, where whole rows would leave compute units idle for longer than the second launch takes.
 constexpr int64_t kMaxVocab = 1 << 20;
-void cut_rows(int64_t rows, int64_t vocab, int* splits, int* chunk) {
-  int64_t want = rows >= 256 ? 1 : (512 + rows - 1) / rows, most = (vocab + 4095) / 4096;
+void cut_rows(int64_t rows, int64_t vocab, bool cut, int* splits, int* chunk) {
+  int64_t want = cut ? ((rows < 64 ? 256 : 512) + rows - 1) / rows : 1, most = (vocab + 4095) / 4096;
   if (want > most) want = most;
   if (want > MAX_SPLITS) want = MAX_SPLITS;
   const int64_t c = ((vocab + want - 1) / want + 63) / 64 * 64;
   *chunk = (int)c;
   *splits = (int)((vocab + c - 1) / c);
+}
+// log probabilities: 131 072 bfloat16 columns, 4 rows 16 us in pieces, 20 whole; 50 021 binary32 14 and 14; 8 000 15 and 10; 100 rows of
+// 131 072 24 and 20
+void cut_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 65536, splits, chunk); }
+// distillation: 64 rows of 131 072 17 us in pieces, 28 whole; 130 of 50 021 23 and 20; 8 000 columns 10 and 8.  Rows that fill a compute
+// unit's registers take twice as long from 257 rows on: 300 rows of 131 072 57 and 72 us, 511 91 and 78
+void cut_distill(int64_t rows, int64_t vocab, int dtype, int* splits, int* chunk) {
+  const bool alone = vocab > 512 * 16 * (dtype == AE_BF16 ? 8 : 4);
+  cut_rows(rows, vocab, (rows < 128 && vocab > 16384) || (alone && rows > 256 && rows <= 384), splits, chunk);
 }
 int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
 
@@ -804,7 +1091,7 @@ extern "C" int model_token_logprobs_workspace(int64_t rows, int64_t vocab, int t
   *bytes = 0;
   if (rows == 0) return AE_OK;
   int splits, chunk;
-  cut_rows(rows, vocab, &splits, &chunk);
+  cut_logprob(rows, vocab, &splits, &chunk);
   if (splits > 1) *bytes = align16(rows * splits * (int64_t)sizeof(Stats)) + rows * splits * (int64_t)top_k * 8;
   return AE_OK;
 }
@@ -827,7 +1114,7 @@ extern "C" int model_token_logprobs(const void* logits, int64_t rows, int64_t vo
   p.logits = logits; p.rows = rows; p.ld = ld; p.vocab = (int)vocab; p.temp = temperature;
   p.tokens = tokens; p.n_tokens = n_tokens; p.top_k = top_k;
   p.logprob = logprob; p.entropy = entropy; p.lse = lse; p.top_id = top_id; p.top_logit = top_logit; p.top_logprob = top_logprob;
-  cut_rows(rows, vocab, &p.splits, &p.chunk);
+  cut_logprob(rows, vocab, &p.splits, &p.chunk);
   p.part = (Stats*)workspace;
   p.part_top = (uint64_t*)((char*)workspace + align16(rows * p.splits * (int64_t)sizeof(Stats)));
   const bool top = top_k > 0 && (top_id || top_logit || top_logprob);
@@ -852,7 +1139,7 @@ extern "C" int model_loss_distill_workspace(int64_t rows, int64_t vocab, int dty
   *bytes = 0;
   if (rows == 0) return AE_OK;
   int splits, chunk;
-  cut_rows(rows, vocab, &splits, &chunk);
+  cut_distill(rows, vocab, dtype, &splits, &chunk);
   *bytes = align16(rows * 4) + (splits > 1 ? rows * splits * (int64_t)sizeof(DistillPart) : 0);
   return AE_OK;
 }
@@ -880,23 +1167,15 @@ extern "C" int model_loss_distill(const void* logits, int64_t rows, int64_t voca
     p.top_id = top_id; p.top_logit = top_logit; p.top_k = top_k; p.teacher_lse = teacher_lse; p.weight = weight;
     p.loss_rows = loss_rows = loss_rows ? loss_rows : (float*)workspace;
     p.d_logits = d_logits; p.ldd = ldd;
-    cut_rows(rows, vocab, &p.splits, &p.chunk);
+    cut_distill(rows, vocab, dtype, &p.splits, &p.chunk);
     p.part = (DistillPart*)((char*)workspace + align16(rows * 4));
-    const dim3 grid((unsigned)(rows * p.splits));
     const size_t lds = (size_t)(p.chunk + 31) / 32 * 4;
-#define DISTILL(T)                                                                   \
-  do {                                                                               \
-    if (p.splits == 1) {                                                             \
-      hipLaunchKernelGGL((k_distill<T, 0>), grid, dim3(NT), lds, s, p);              \
-    } else {                                                                         \
-      hipLaunchKernelGGL((k_distill<T, 1>), grid, dim3(NT), lds, s, p);              \
-      hipLaunchKernelGGL((k_distill<T, 2>), grid, dim3(NT), lds, s, p);              \
-    }                                                                                \
-  } while (0)
-    if (dtype == AE_BF16) DISTILL(bf16_t);
-    else DISTILL(float);
-#undef DISTILL
-    AE_TRY(launch_status("loss_distill"));
+    if (p.splits > 1 && rows <= kTotalHere) {
+      p.loss = loss;
+      loss = nullptr;
+    }
+    if (p.splits == 1) AE_TRY(dtype == AE_BF16 ? launch_distill_rows<bf16_t>(p, lds, s) : launch_distill_rows<float>(p, lds, s));
+    else AE_TRY(dtype == AE_BF16 ? launch_distill_pieces<bf16_t>(p, lds, s) : launch_distill_pieces<float>(p, lds, s));
   }
   if (loss) hipLaunchKernelGGL(k_distill_total, dim3(1), dim3(NT), 0, s, loss_rows, weight, rows, loss);
   return launch_status("loss_distill");
