@@ -161,26 +161,31 @@ __device__ __forceinline__ void push(TopShared& sh, bool want, uint64_t key) {
 // themselves, and not much less, since the largest keys lie in different shares for the most part.  The leading bits will
 // do: all that a positive bfloat16 has, nine of a binary32 number's fraction.
 constexpr int BOUND_BITS = 18;
+// by the first wavefront: the largest number that k of the maxima reach, its bits from `high` to `low` found, those above given
+__device__ uint32_t bound_bits(const TopShared& sh, int k, uint32_t bound, int high, int low) {
+  const int lane = threadIdx.x & 63;
+  uint32_t v[NW];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) v[i] = sh.tmax[lane + 64 * i];
+  for (int bit = high; bit >= low; --bit) {
+    const uint32_t c = bound | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) n += __popcll(__ballot(v[i] >= c));
+    if (n >= k) bound = c;
+    if (n == k) break;
+  }
+  return bound;
+}
 __device__ uint32_t top_bound(TopShared& sh, int k, uint32_t tmax) {
-  const int t = threadIdx.x, lane = t & 63;
+  const int t = threadIdx.x;
   __syncthreads();
   sh.tmax[t] = tmax;
   if (t == 0) sh.count = sh.n_pairs = 0;
   __syncthreads();
   if (t < 64) {
-    uint32_t v[NW];
-#pragma unroll
-    for (int i = 0; i < NW; ++i) v[i] = sh.tmax[lane + 64 * i];
-    uint32_t bound = 0;
-    for (int bit = 31; bit >= 32 - BOUND_BITS; --bit) {
-      const uint32_t c = bound | (1u << bit);
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) n += __popcll(__ballot(v[i] >= c));
-      if (n >= k) bound = c;
-      if (n == k) break;
-    }
-    if (lane == 0) sh.threshold = bound;
+    const uint32_t bound = bound_bits(sh, k, 0, 31, 32 - BOUND_BITS);
+    if (t == 0) sh.threshold = bound;
   }
   __syncthreads();
   return sh.threshold;
@@ -190,23 +195,39 @@ __device__ uint32_t top_bound(TopShared& sh, int k, uint32_t tmax) {
 // of the k-th largest, by its digits if the bound is not it already; then what is larger, in any order, and of what
 // is equal the first ones in the order of the index.  (A share of nothing but NaN counts as -infinity in the bound, which
 // may then be too high.)  A source gives its keys in steps of W to a thread, in that order.
+template <typename Src, typename F>
+__device__ __forceinline__ void for_steps(const Src& src, F f) {          // f(keys, how many) for the thread's steps, four loads in flight
+  constexpr int W = Src::W;
+  for (int s = 0; s < src.steps(); s += 4) {
+    uint64_t key[4][W];
+    int n[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) n[u] = src.load(s + u, key[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) f(key[u], n[u]);
+  }
+}
 template <typename Src>
 __device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, const Src& src) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   constexpr int W = Src::W;
   uint64_t key[W];
   __syncthreads();
+  if (t < 64) {                          // the bound to its last bit: one that equals the k-th largest saves its search
+    const uint32_t b = bound_bits(sh, k, bound, 31 - BOUND_BITS, 0);
+    if (t == 0) sh.threshold = b;
+  }
   if (t == 0) sh.count = 0;
   __syncthreads();
-  for (int s = 0; s < src.steps(); ++s) {
-    const int n = src.load(s, key);
-    int more = 0;
+  bound = sh.threshold;
+  int more = 0;
+  for_steps(src, [&](const uint64_t (&v)[W], int n) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) more += i < n && (uint32_t)(key[i] >> 32) > bound ? 1 : 0;
+    for (int i = 0; i < W; ++i) more += i < n && (uint32_t)(v[i] >> 32) > bound ? 1 : 0;
+  });
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) more += __shfl_xor(more, off, 64);
-    if (lane == 0 && more) atomicAdd(&sh.count, more);
-  }
+  for (int off = 32; off > 0; off >>= 1) more += __shfl_xor(more, off, 64);
+  if (lane == 0) atomicAdd(&sh.count, more);
   __syncthreads();
   uint32_t value = bound;
   int larger = sh.count;
@@ -217,11 +238,10 @@ __device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, c
       __syncthreads();
       if (t < 256) sh.hist[t] = 0;
       __syncthreads();
-      for (int s = 0; s < src.steps(); ++s) {
-        const int n = src.load(s, key);
+      for_steps(src, [&](const uint64_t (&keys)[W], int n) {
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          const uint32_t v = (uint32_t)(key[i] >> 32);
+          const uint32_t v = (uint32_t)(keys[i] >> 32);
           if (i < n && (d == 3 || (v >> (8 * d + 8)) == (value >> (8 * d + 8)))) {
             const int digit = (int)(v >> (8 * d)) & 255;
             const int first = __builtin_amdgcn_readfirstlane(digit);
@@ -230,7 +250,7 @@ __device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, c
             else if (lane == __ffsll((unsigned long long)same) - 1) atomicAdd(&sh.hist[digit], __popcll(same));
           }
         }
-      }
+      });
       __syncthreads();
       if (t == 0) {
         int above = larger, at = 255;
@@ -247,11 +267,10 @@ __device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, c
   if (t == 0) sh.count = 0;
   __syncthreads();
   if (larger > 0) {
-    for (int s = 0; s < src.steps(); ++s) {
-      const int n = src.load(s, key);
+    for_steps(src, [&](const uint64_t (&v)[W], int n) {
 #pragma unroll
-      for (int i = 0; i < W; ++i) push(sh, i < n && (uint32_t)(key[i] >> 32) > value, key[i]);
-    }
+      for (int i = 0; i < W; ++i) push(sh, i < n && (uint32_t)(v[i] >> 32) > value, v[i]);
+    });
   }
   __syncthreads();
   int have = larger;                     // fewer than k <= CAND
