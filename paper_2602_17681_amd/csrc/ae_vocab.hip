@@ -565,7 +565,7 @@ __global__ __launch_bounds__(NT) void k_logprob_join(LogprobArgs p) {
 // ---- distillation --------------------------------------------------------------------------------------------------
 struct DistillPart {                     // of a row piece
   float m, s_out, s_in, pad;             // maximum; sums of e_j outside and inside the teacher's list
-  double p, l;                           // sums over the list's entries in the piece: p_i, and p_i (log p_i - z_i / T)
+  double p, l;                           // sums over the list's entries in the piece: p_i, and p_i (log p_i - (z_i - m) / T)
 };
 struct DistillArgs {
   const void* logits;
@@ -581,19 +581,6 @@ struct DistillArgs {
   int64_t ldd;
   DistillPart* part;                     // [rows][splits]
 };
-
-__device__ __forceinline__ DistillPart join(const DistillPart& x, const DistillPart& y, float c2) {
-  DistillPart r;
-  r.m = fmaxf(x.m, y.m);
-  const float ref = reference(r.m);
-  const float fx = fast_exp2((x.m - ref) * c2), fy = fast_exp2((y.m - ref) * c2);
-  r.s_out = fx * x.s_out + fy * y.s_out;
-  r.s_in = fx * x.s_in + fy * y.s_in;
-  r.pad = 0.0f;
-  r.p = x.p + y.p;
-  r.l = x.l + y.l;
-  return r;
-}
 
 // exp(x) to binary32 precision of an x in binary64 (whose binary32 rounding would cost |x| 2^-24): whole powers of two taken
 // out.  The teacher's binary32 numbers define its probabilities no better.
@@ -652,7 +639,7 @@ template <int V> __device__ __forceinline__ uint32_t marks_of(const uint32_t* bi
 
 template <typename T>
 __device__ DistillPart piece_stats(const DistillArgs& p, int64_t row, int c0, int n, const uint32_t* bits, double norm, float c2,
-                                   DistillPart* sm /* NW */) {
+                                   float (*smf)[NW] /* 3 */, double (*smd)[NW] /* 2 */) {
   constexpr int V = Store<T>::VEC;
   const T* z = (const T*)p.logits + row * p.ld + c0;
   DistillPart st = {-INFINITY, 0.0f, 0.0f, 0.0f, 0.0, 0.0};
@@ -682,24 +669,42 @@ __device__ DistillPart piece_stats(const DistillArgs& p, int64_t row, int c0, in
       for (int i = 0; i < V; ++i) st.s_out += e[i];
     }
   });
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  float m = max_rows(max16(st.m));
+  float f = fast_exp2((st.m - reference(m)) * c2);
+  const float w_out = sum_rows(sum16(f * st.s_out)), w_in = sum_rows(sum16(f * st.s_in));
+  __syncthreads();
+  if (lane == 0) {
+    smf[0][wave] = m;
+    smf[1][wave] = w_out;
+    smf[2][wave] = w_in;
+  }
+  __syncthreads();
+  const int i8 = lane & 15;
+  const float m_i = i8 < NW ? smf[0][i8] : -INFINITY;
+  m = max16(m_i);
+  f = fast_exp2((m_i - reference(m)) * c2);
+  st = {m, sum16(i8 < NW ? f * smf[1][i8] : 0.0f), sum16(i8 < NW ? f * smf[2][i8] : 0.0f), 0.0f, 0.0, 0.0};
+  const double ref = (double)reference(m), inv_t = 1.0 / (double)p.temp;
+  double sp = 0.0, sl = 0.0;
   for (int i = threadIdx.x; i < p.top_k; i += NT) {
     const int id = p.top_id[row * p.top_k + i];
     if (id < c0 || id >= c0 + n) continue;
     const double lp = list_log_p(p, row * p.top_k + i, norm), pi = exp_of(lp);
-    st.p += pi;
-    if (pi != 0.0) st.l += pi * (lp - (double)Store<T>::ld(z + id - c0) / (double)p.temp);
+    sp += pi;
+    if (pi != 0.0) sl += pi * (lp - ((double)Store<T>::ld(z + id - c0) - ref) * inv_t);
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const DistillPart o = {__shfl_xor(st.m, off, 64), __shfl_xor(st.s_out, off, 64), __shfl_xor(st.s_in, off, 64), 0.0f,
-                           __shfl_xor(st.p, off, 64), __shfl_xor(st.l, off, 64)};
-    st = join(st, o, c2);
+  if (p.top_k > 64 || wave == 0) {               // whose lanes have entries
+    sp = wave_sum(sp);
+    sl = wave_sum(sl);
+  }
+  if (lane == 0) {
+    smd[0][wave] = sp;
+    smd[1][wave] = sl;
   }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = st;
-  __syncthreads();
-  st = sm[0];
-  for (int i = 1; i < NW; ++i) st = join(st, sm[i], c2);
+  st.p = sum_of<NW>(smd[0]);
+  st.l = sum_of<NW>(smd[1]);
   return st;
 }
 
@@ -725,10 +730,11 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillP
   r.f_out = r.empty ? 0.0f : outside * scale / r.s_all;
   return r;
 }
-__device__ float row_loss(const DistillArgs& p, const DistillPart& st, const RowGrad& r) {
+// off: the sums are 2^off times those of exponents relative to the maximum
+__device__ float row_loss(const DistillArgs& p, const DistillPart& st, const RowGrad& r, float off = 0.0f) {
   if (r.empty) return 0.0f;
   const double s_all = (double)st.s_out + (double)st.s_in;
-  double loss = st.l + (st.p != 0.0 ? st.p * ((double)st.m / (double)p.temp + log_of(s_all)) : 0.0);
+  double loss = st.l + (st.p != 0.0 ? st.p * (log_of(s_all) - (double)off * 0.69314718055994530942) : 0.0);
   if (r.rest != 0.0) loss += r.rest * log_of(r.rest * s_all / (double)st.s_out);
   return (float)loss;
 }
@@ -779,6 +785,8 @@ __device__ DistillPart joined(const DistillArgs& p, int64_t row, float c2) {
   if (lane < p.splits) v = p.part[row * p.splits + lane];
   const float m = max_rows(max16(v.m));
   const float f = fast_exp2((v.m - reference(m)) * c2);
+  // the piece's own maximum in the terms of l becomes the row's
+  if (v.p != 0.0) v.l -= v.p * ((double)reference(v.m) - (double)reference(m)) / (double)p.temp;
   return {m, sum_rows(sum16(f * v.s_out)), sum_rows(sum16(f * v.s_in)), 0.0f, wave_sum(v.p), wave_sum(v.l)};
 }
 
@@ -812,8 +820,8 @@ __device__ void total_of_pieces(const DistillArgs& p, float c2, double* sm /* NW
 template <typename T, int MODE>
 __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   extern __shared__ uint32_t bits[];
-  __shared__ DistillPart sm[NW];
-  __shared__ double smd[NW + 1];
+  __shared__ float smf[3][NW];
+  __shared__ double smp[2][NW], smd[NW + 1];
   const int64_t row = blockIdx.x / p.splits;
   const int split = (int)(blockIdx.x - row * p.splits);
   const int c0 = split * p.chunk;
@@ -832,7 +840,7 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   const double norm = list_norm<NT>(p, row, smd);
   DistillPart st;
   if constexpr (MODE != 2) {
-    st = piece_stats<T>(p, row, c0, n, bits, norm, c2, sm);
+    st = piece_stats<T>(p, row, c0, n, bits, norm, c2, smf, smp);
     if constexpr (MODE == 1) {
       if (threadIdx.x == 0) p.part[row * p.splits + split] = st;
       return;
@@ -952,14 +960,22 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     __syncthreads();
     if (!p.teacher_lse && wave * 64 < k) norm += log_of(sum_of<NWV>(smd[0]));      // for wavefronts with entries of the list
     m = max_of<NWV>(smf[1]);
-    const float ref = reference(m);
+    // e_j = 2^(z_j ce + k2) in one operation, k2 = -m ce.  What k2 is rounded by is a factor of all e_j, of their sums too;
+    // the loss takes it out again (`off`).  Beyond 2^100 neighbouring numbers are 2^76 apart: e_j is 1 at the maximum and 0
+    // elsewhere, with any factor, and 1 leaves m as it is.
+    float ce = c2, k2 = -reference(m) * c2;
+    if (!(fabsf(k2) < 0x1p100f)) {
+      ce = 1.0f;
+      k2 = -reference(m);
+    }
+    const float off = fmaf(reference(m), ce, k2);
     // e_j of a vector's columns
     auto exponentials = [&](int u, float (&e)[V]) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) e[i] = fast_exp2((element(u, i) - ref) * c2);
+      for (int i = 0; i < V; ++i) e[i] = fast_exp2(fmaf(element(u, i), ce, k2));
     };
     float s_out = 0.0f, s_in = 0.0f;
-    const float e_tail = fast_exp2((z_tail - ref) * c2);
+    const float e_tail = fast_exp2(fmaf(z_tail, ce, k2));
     const bool in_tail = c_tail < n && (bits[c_tail >> 5] >> (c_tail & 31) & 1);
     (in_tail ? s_in : s_out) = e_tail;
 #pragma unroll
@@ -988,7 +1004,7 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     if (valid(id0)) {
       const double lp = (double)top0 * inv_t - norm;
       pi0 = exp_of(lp);
-      if (pi0 != 0.0) sl = pi0 * (lp - (double)z0 * inv_t);
+      if (pi0 != 0.0) sl = pi0 * (lp - ((double)z0 - (double)reference(m)) * inv_t);
     }
     s_out = sum_rows(sum16(s_out));
     s_in = sum_rows(sum16(s_in));
@@ -1019,10 +1035,10 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     }
     if (c_tail < n && !in_tail) Store<T>::st(g + c_tail, r.f_out * e_tail);
     if (valid(id0)) {
-      const double q = (double)(fast_exp2((z0 - ref) * c2) / r.s_all);
+      const double q = (double)(fast_exp2(fmaf(z0, ce, k2)) / r.s_all);
       Store<T>::st(g + id0, r.empty ? 0.0f : (float)((r.mass * q - pi0) * r.scale));
     }
-    if (t == NTH - 64) p.loss_rows[row] = row_loss(p, st, r);      // the last wavefront: the list is the first ones'
+    if (t == NTH - 64) p.loss_rows[row] = row_loss(p, st, r, off);      // the last wavefront: the list is the first ones'
     w = w_next;
     __syncthreads();                             // the marks and sums have been read
   }

@@ -164,3 +164,51 @@ def test_distill_rows(rows, vocab, dtype, masked):
         ae.model_loss_distill(z, rows, vocab, i32, t, lr2, None, z, ws, teacher_lse=lse, weight=w, temperature=temperature)
         assert torch.equal(z, g) and torch.equal(lr2, lr)
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(5, 20001), (140, 20001), (260, 900), (300, 40001), (140, 131090)])
+def test_distill_of_extreme_rows(rows, vocab, dtype):
+    """A row of the type's lowest number only, one of numbers near the largest, one of large ones, one whose logits are all
+    alike: differences to the maximum are what counts, and they are exact."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    z, gen = make(rows, vocab, dtype, 5, False)
+    low = torch.finfo(z.dtype).min
+    z[0] = low
+    z[1] = 2e38
+    z[1, ::7] = -2e38
+    z[2] *= 1e6
+    z[3] = 1.5
+    k = 12
+    ids = torch.arange(k, device="cuda").repeat(rows, 1) * 7 + 3
+    ids[1, :3] = torch.arange(3, device="cuda") * 7
+    t = (torch.randn((rows, k), generator=gen, device="cuda") + 3).sort(1, descending=True).values
+    t[1, :3] = -math.inf                                   # tokens that the student all but rules out, and the teacher does
+    lse = (torch.logsumexp(t.double(), 1) + 0.3).float()
+    ws = torch.empty(ae.model_loss_distill_workspace(rows, vocab, ae.AE_BF16 if dtype == "bf16" else ae.AE_F32), dtype=torch.uint8, device="cuda")
+    lr, g = torch.empty(rows, device="cuda"), torch.empty_like(z)
+    ae.model_loss_distill(z, rows, vocab, ids.to(torch.int32), t, lr, None, g, ws, teacher_lse=lse)
+    for r in (0, 1, 2, 3):
+        zr, at = z[r].double(), ids[r]
+        d = zr - zr.max()
+        s = torch.exp(d).sum()
+        logq = d - torch.log(s)
+        q = torch.exp(logq)
+        logp = t[r].double() - lse[r].double()
+        p = torch.exp(logp)
+        outside = torch.ones(vocab, dtype=torch.bool, device="cuda")
+        outside[at] = False
+        q_out = q[outside].sum()
+        rest = 1 - p.sum() if q_out > 0 else torch.zeros((), dtype=torch.float64, device="cuda")
+        loss = torch.where(p > 0, p * (logp - logq[at]), 0.0).sum() + (rest * (torch.log(rest) - torch.log(q_out)) if rest > 0 else 0.0)
+        e = sum_error(vocab, 1.0, 30.0)
+        # logits of a million: the terms p (z_i - m) of the loss are binary32 products of that size at most
+        assert abs(lr[r].item() - loss.item()) <= 3 * e + 8 * U * (abs(loss.item()) + 1)
+        mass = p.sum() + rest
+        grad = q * (mass - (rest / q_out if rest > 0 else 0.0))
+        grad[at] = mass * q[at] - p
+        tol = (mass + (rest / q_out if rest > 0 else 0.0)) * q * (3 * e + 16 * U) + 4 * U * grad.abs() + 1e-37
+        if dtype == "bf16":
+            tol = tol + 2.0 ** -8 * grad.abs()
+        assert bool(((g[r].double() - grad).abs() <= tol).all())
