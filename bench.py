@@ -514,6 +514,80 @@ def bench_fold(torch, ae, args):
     }
 
 
+def build_output_layer(torch, ae, tokens, d, vocab, seed, top_k=64, temperature=1.5):
+    """A calibration step of a quantised output layer: hidden states under a transformation T(x) = A x + v, whose inverse is
+    folded into the layer (model_fold_linear), the layer in 8 bits with a scale for each 128 x 128 tile, a teacher's
+    logits in bfloat16 (of the unquantised layer).  All device tensors the step needs, and the host copies of what it starts from."""
+    rng = np.random.default_rng(seed)
+    a, v, a_inv = wl.make_transform(d, seed=seed, bf16=True, kind="affine")
+    w_h = (rng.standard_normal((vocab, d)) * 2.5 / np.sqrt(d)).astype(np.float32)
+    h = rng.standard_normal((tokens, d)).astype(np.float32)
+    dev = lambda t, dt=torch.bfloat16: torch.from_numpy(np.ascontiguousarray(t, dtype=np.float32)).cuda().to(dt).contiguous()      # noqa: E731
+    f32 = lambda *sh: torch.empty(sh, device="cuda")      # noqa: E731
+    pad = lambda n: -(-n // 16) * 16      # noqa: E731
+    codes = lambda r, c: torch.empty((r, pad(c)), dtype=torch.float8_e4m3fn, device="cuda")[:, :c]      # noqa: E731
+    blocks = lambda n: -(-n // ae.FP8_BLOCK)      # noqa: E731
+    st = dict(tokens=tokens, d=d, vocab=vocab, top_k=top_k, temperature=temperature)
+    w, w_fold, bias = dev(w_h), torch.empty((vocab, d), dtype=torch.bfloat16, device="cuda"), f32(vocab)
+    ws = torch.empty(ae.model_fold_workspace(vocab, d, 0, d, ae.AE_BF16), dtype=torch.uint8, device="cuda")
+    ae.model_fold_linear(w, None, vocab, d, None, None, dev(a_inv), dev(v, torch.float32), w_fold, bias, ws)
+    st["x"] = dev(h @ a.T + v)                                     # transformed hidden states
+    st["teacher"] = torch.matmul(dev(h), w.t())                    # the unquantised layer's logits
+    st["w"], st["w_s"] = codes(vocab, d), f32(blocks(vocab), blocks(d))
+    st["wt"], st["wt_s"] = codes(d, vocab), f32(blocks(d), blocks(vocab))
+    ae.model_fp8_quantize(w_fold, vocab, d, "tiles", st["w"], st["w_s"], st["wt"], st["wt_s"])
+    st["bias"], st["target"] = bias, torch.from_numpy(rng.integers(0, vocab, (tokens, 1)).astype(np.int32)).cuda()
+    st["logits"] = torch.empty((tokens, vocab), dtype=torch.bfloat16, device="cuda")
+    st["top_id"] = torch.empty((tokens, top_k), dtype=torch.int32, device="cuda")
+    st["top_logit"], st["teacher_lse"], st["weight"] = f32(tokens, top_k), f32(tokens), torch.full((tokens,), 1.0 / tokens, device="cuda")
+    st["logprob"], st["entropy"], st["loss"] = f32(tokens, 1), f32(tokens), f32(1)
+    st["g"], st["g_s"], st["gt"], st["gt_s"] = codes(tokens, vocab), f32(blocks(vocab), tokens), codes(vocab, tokens), f32(blocks(tokens), vocab)
+    st["xt"], st["xt_s"] = codes(d, tokens), f32(blocks(tokens), d)
+    st["dx"], st["dw"] = torch.empty((tokens, d), dtype=torch.bfloat16, device="cuda"), f32(vocab, d)
+    room = max(ae.model_fp8_linear_workspace(tokens, vocab, d), ae.model_fp8_matmul_workspace(tokens, d, vocab), ae.model_fp8_matmul_workspace(vocab, d, tokens),
+               ae.model_token_logprobs_workspace(tokens, vocab, top_k, ae.AE_BF16), ae.model_loss_distill_workspace(tokens, vocab, ae.AE_BF16))
+    st["ws"] = torch.empty(max(16, room), dtype=torch.uint8, device="cuda")
+    return st
+
+
+def output_layer_step(st, ae):
+    """teacher's top logits -> 8-bit layer -> log probabilities of the targets -> distillation loss, gradient in the logits' place
+    -> input and weight gradient, both as 8-bit products."""
+    n, d, v, k, temp, ws = st["tokens"], st["d"], st["vocab"], st["top_k"], st["temperature"], st["ws"]
+    ae.model_token_logprobs(st["teacher"], n, v, None, k, None, None, st["teacher_lse"], st["top_id"], st["top_logit"], None, ws, temperature=temp)
+    ae.model_fp8_linear(st["x"], st["w"], st["w_s"], st["bias"], n, v, d, st["logits"], ws)
+    ae.model_token_logprobs(st["logits"], n, v, st["target"], 0, st["logprob"], st["entropy"], None, None, None, None, ws)
+    ae.model_loss_distill(st["logits"], n, v, st["top_id"], st["top_logit"], None, st["loss"], st["logits"], ws,
+                          teacher_lse=st["teacher_lse"], weight=st["weight"], temperature=temp)
+    ae.model_fp8_quantize(st["logits"], n, v, "rows", st["g"], st["g_s"], st["gt"], st["gt_s"])
+    ae.model_fp8_quantize(st["x"], n, d, "rows", None, None, st["xt"], st["xt_s"])
+    ae.model_fp8_matmul(st["g"], st["g_s"], st["wt"], st["wt_s"], "tiles", None, n, d, v, st["dx"], ws)
+    ae.model_fp8_matmul(st["gt"], st["gt_s"], st["xt"], st["xt_s"], "rows", None, v, d, n, st["dw"], ws)
+
+
+def bench_output_layer(torch, ae, args):
+    """The step above for 2 048 tokens, hidden width 4 096 and 32 768 tokens of vocabulary."""
+    tokens, d, vocab = 2048, 4096, 32768
+    st = build_output_layer(torch, ae, tokens, d, vocab, seed=31)
+    for _ in range(args.warmup):
+        output_layer_step(st, ae)
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(args.steps):
+        output_layer_step(st, ae)
+    torch.cuda.synchronize()
+    dt = time.perf_counter() - t0
+    flops = 6.0 * tokens * d * vocab
+    ms = dt / args.steps * 1e3
+    return {
+        "metric": "tokens/sec, calibration step of an 8-bit output layer (teacher's top 64, layer, log probabilities, distillation, both gradients)",
+        "value": tokens * args.steps / dt, "unit": "tokens/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "ms_per_step": ms, "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "fp8", "data": "synthetic",
+        "config": {"workload": "output_layer", "tokens": tokens, "d": d, "vocab": vocab, "top_k": 64, "temperature": 1.5},
+        "loss": st["loss"].item(), "mean_nll": -st["logprob"].mean().item(), "tflops_of_the_three_products": flops / ms / 1e9,
+    }
+
+
 # measured HBM bytes per product launch of the QR parametrisation (profiles/qr_param.md)
 QR_TRAFFIC_BYTES = {"f32": 8.56e8}
 
@@ -735,6 +809,9 @@ def main():
     ap.add_argument("--fold", action="store_true",
                     help="benchmark the folding of two affine transformations into the four projections of one attention block "
                          "(d = 4096) instead of a network: one JSON line with roofline and cpu_baseline")
+    ap.add_argument("--output-layer", action="store_true",
+                    help="benchmark a calibration step of an 8-bit output layer (teacher's top logits, 8-bit products, log probabilities, "
+                         "distillation loss and gradients) instead of a network: one JSON line")
     ap.add_argument("--mx-elem", default="fp4", choices=["fp4", "fp8", "int4"],
                     help="element format of --mx-quant (FP4 E2M1, FP8 E4M3, or the 4-bit integer reading)")
     ap.add_argument("--calibrate-mfma", action="store_true",
@@ -770,6 +847,9 @@ def main():
         return
     if args.fold:
         print(json.dumps(bench_fold(torch, ae, args)))
+        return
+    if args.output_layer:
+        print(json.dumps(bench_output_layer(torch, ae, args)))
         return
     if args.qr_param:
         print(json.dumps(bench_qr_param(torch, ae, args)))
