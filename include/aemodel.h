@@ -411,13 +411,17 @@ int model_fold_embedding(const void* e, int64_t vocab, int64_t d, const void* a,
  *   AE_FP8_TILES the same codes and scales transposed.  Both orientations take one pass over x.
  * model_fp8_matmul    y[i][j] = bias[j] + sum over blocks c of a_scale[c][i] * b_scale[c; j] * sum over k in c of a[i][k] * b[j][k]:
  *   a [m][k] in AE_FP8_ROWS, b [n][k] in either form (b_blocks), so that y = a b^T; bias binary32 [n], nullable; y [m][n]
- *   in dtype, row stride ldy elements.  Sums are binary32 on the matrix cores, scaled block by block, rounded to dtype
- *   once.  With the codes of x and W (tiles) it is a layer's forward pass; with those of dY and W^T its input gradient;
+ *   in dtype, row stride ldy elements.  a_scale * b_scale is one binary32 product; the blocks are added up in binary32 and
+ *   rounded to dtype once.  The sum over a block: for binary32 y the codes are multiplied as bfloat16, which holds them
+ *   exactly, and added in binary32 (an error of about 2^-23 of the block's largest sums); for bfloat16 y the 8-bit matrix
+ *   instruction multiplies them at twice the rate and keeps, of each eight neighbouring products, 14 bits below the largest
+ *   (about 2^-16, against 2^-9 of the result's rounding).  With the codes of x and W (tiles) it is a layer's forward pass; with those of dY and W^T its input gradient;
  *   with those of dY^T and X^T (rows) its weight gradient.
  * model_fp8_linear    y = x W^T + bias with x [m][k] in dtype quantised by the call as above (AE_FP8_ROWS) and W [n][k] in
  *   AE_FP8_TILES: the values are those of model_fp8_quantize followed by model_fp8_matmul.
- * workspace: the matching _workspace bytes (0 for many shapes: then it may be null), 16-byte aligned; its contents need
- * not be kept.  Sizes up to 2^31 - 1 each; m or n of zero is no work; k at least 1. */
+ * workspace: the matching _workspace bytes (0 for model_fp8_matmul, and for model_fp8_linear of 16 rows or fewer, which
+ * quantises on the way: then it may be null), 16-byte aligned; its contents need not be kept.  Sizes up to 2^31 - 513
+ * each; m or n of zero is no work; k at least 1. */
 enum ae_fp8_blocks { AE_FP8_ROWS = 0, AE_FP8_TILES = 1 };
 int model_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int blocks, void* q, int64_t ldq,
                        float* scale, void* qt, int64_t ldqt, float* scale_t, void* stream);
@@ -430,11 +434,12 @@ int model_fp8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, con
                      int64_t n, int64_t k, int dtype, void* y, int64_t ldy, void* workspace, void* stream);
 
 /* ---- log probabilities and distillation over a vocabulary --------------------------------------------------------
- * logits z [rows][vocab] in dtype (row stride ld elements, no alignment beyond the element's own); temperature T > 0:
- * every row is the distribution q_j = exp(z_j / T - lse), lse = log sum_j exp(z_j / T).  Logits of -infinity are
- * outcomes that cannot occur.  A row in which all are is empty: its lse and log probabilities are -infinity, its
- * entropy, loss and gradient zero.  A row that holds a NaN or +infinity gives NaN for its own results only.  All sums
- * are binary32 or wider; a row's results do not depend on the other rows.  1 <= vocab <= 2^20.
+ * logits z [rows][vocab] in dtype (row stride ld elements, no alignment beyond the element's own); temperature T, a
+ * positive normal number: every row is the distribution q_j = exp(z_j / T - lse), lse = log sum_j exp(z_j / T).  Logits
+ * of -infinity are outcomes that cannot occur.  A row in which all are is empty: its lse and log probabilities are
+ * -infinity, its entropy, loss and gradient zero.  A row that holds a NaN or +infinity gives NaN for its own results only.
+ * All sums are binary32 or wider; a row's results do not depend on what the other rows hold (their number decides how rows
+ * are divided among workgroups, and so last bits).  The same call gives the same bits.  1 <= vocab <= 2^20.
  *
  * model_token_logprobs  for every row
  *   logprob [rows][n_tokens]: log q of the given tokens [rows][n_tokens] (int32); an index outside 0 .. vocab - 1 marks a

@@ -73,20 +73,10 @@ struct Stats {
 };
 // the sum a after the maximum has grown by -d; f = the factor of the sums.  Nothing is left of what f = 0 scales (s d may overflow)
 __device__ __forceinline__ float shifted(float a, float s, float d, float f) { return f == 0.0f ? 0.0f : f * (a + s * d); }
-__device__ __forceinline__ Stats join(const Stats& x, const Stats& y, float c2) {
-  Stats r;
-  r.m = fmaxf(x.m, y.m);
-  const float ref = reference(r.m);
-  // differences of -infinity (a side without entries) are cut off at the lowest number, so that 0 times them is 0
-  const float dx = fmaxf(x.m - ref, -FLT_MAX), dy = fmaxf(y.m - ref, -FLT_MAX);
-  const float fx = fast_exp2(dx * c2), fy = fast_exp2(dy * c2);
-  r.s = fx * x.s + fy * y.s;
-  r.a = shifted(x.a, x.s, dx, fx) + shifted(y.a, y.s, dy, fy);
-  return r;
-}
 __device__ __forceinline__ Stats wave_join(Stats v, float c2) {
   Stats r;
   r.m = max_rows(max16(v.m));
+  // the difference of -infinity (a side without entries) is cut off at the lowest number, so that 0 times it is 0
   const float d = fmaxf(v.m - reference(r.m), -FLT_MAX), f = fast_exp2(d * c2);
   r.s = sum_rows(sum16(f * v.s));
   r.a = sum_rows(sum16(shifted(v.a, v.s, d, f)));
@@ -407,9 +397,12 @@ __device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, con
   if (p.top_logprob) p.top_logprob[at] = log_prob(z, r, p.temp);
 }
 
-// One workgroup per row piece; with one piece per row it writes the results, otherwise what k_logprob_join needs.
+// One workgroup per row piece; with one piece per row it writes the results, otherwise what k_logprob_join needs.  Bound by
+// reading the logits: 2 048 x 131 072 in bfloat16 93 us without entropy and list, 5.8 TB/s, 99 with entropy.  A list costs
+// what its threads do while a row's loads have ended and the next row's have not begun: 116 us with 64 entries.  Three
+// workgroups to a compute unit, so that others load meanwhile: 80 registers (4 096 x 32 000 with 64 entries 93 us, two 118).
 template <typename T, bool TOP, bool ENT>
-__global__ __launch_bounds__(NT, 4) void k_logprob(LogprobArgs p) {
+__global__ __launch_bounds__(NT, 6) void k_logprob(LogprobArgs p) {
   constexpr int V = Store<T>::VEC, STEP = NT * V;
   __shared__ Stats sm[NW];
   __shared__ TopShared sh;
@@ -816,6 +809,8 @@ __device__ void total_of_pieces(const DistillArgs& p, float c2, double* sm /* NW
   if (threadIdx.x == 0) *p.loss = (float)acc;
 }
 
+// Rows that the registers do not hold, or without a gradient, or with long lists: a row is read once for its statistics and
+// again for its gradient (1 024 x 131 072 in binary32 332 us, 3.2 TB/s of one reading and one writing; loss alone 104, 5.2).
 // MODE 0: statistics and gradient of whole rows; 1: statistics of row pieces; 2: gradient of row pieces from joined statistics
 template <typename T, int MODE>
 __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
@@ -857,7 +852,9 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
 // Whole rows that fit the registers: a workgroup of NTH threads holds a row, NV vectors to a thread, so that it is read
 // once: 16 vectors in 1 024 threads are 256 KiB, half of a compute unit's registers.  As no more than one or a few
 // workgroups then fit a compute unit, they stay, and ask for a vector of their next row as soon as the gradient of the
-// present one's is stored.  A thread also holds its entry of the list, which is no longer than there are threads.
+// present one's is stored.  Bound by memory: 8 192 x 131 072 in bfloat16 1 007 us, 4.3 TB/s read and written (a copy: 4.9),
+// the difference being barriers that nothing is loaded beside.  A thread also holds its entry of the list, which is no
+// longer than there are threads.
 template <typename T, int NTH, int NV>
 __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
   constexpr int V = Store<T>::VEC, STEP = NTH * V, NWV = NTH / 64;
@@ -1059,8 +1056,9 @@ __global__ __launch_bounds__(NT) void k_distill_total(const float* __restrict__ 
 
 template <typename T, int NTH, int NV>
 int launch_distill_row(const DistillArgs& p, size_t lds, hipStream_t s) {
-  // 16 vectors: workgroups that stay, as many as the registers of 256 compute units hold (128 to a thread).  Fewer: a row each, since more
-  // of them run at a time (4 096 x 32 000 in bfloat16 124 us, with staying ones 145; 8 192 x 131 072 1 020, a row each 1 090)
+  // 16 vectors: workgroups that stay, as many as the registers of 256 compute units hold (128 to a thread).  Fewer: a row
+  // each, since more of them run at a time (4 096 x 32 000 in bfloat16 124 us, with staying ones 145; 8 192 x 131 072 1 007, a
+  // row each 1 071; 4 096 x 50 021 230 and 243)
   const int64_t stay = NV == 16 ? 256 * (1024 / NTH) : p.rows;
   hipLaunchKernelGGL((k_distill_row<T, NTH, NV>), dim3((unsigned)(p.rows < stay ? p.rows : stay)), dim3(NTH), lds, s, p);
   return launch_status("loss_distill");
@@ -1096,9 +1094,11 @@ void cut_rows(int64_t rows, int64_t vocab, bool cut, int* splits, int* chunk) {
   *chunk = (int)c;
   *splits = (int)((vocab + c - 1) / c);
 }
-// log probabilities: 131 072 bfloat16 columns, 4 rows 16 us in pieces, 20 whole; 50 021 binary32 14 and 14; 8 000 15 and 10; 100 rows of
-// 131 072 24 and 20
+// log probabilities with a list of 20, 4 rows: 131 072 bfloat16 columns 16 us in pieces, 20 whole; 65 536 17 and 13; 50 021 binary32
+// 15 and 13; 100 rows of 131 072 24 and 20
 void cut_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 65536, splits, chunk); }
+// room for the pieces of rows is asked for from 32 769 columns on, so that the rule above is not the callers' concern
+void room_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 32768, splits, chunk); }
 // distillation: 64 rows of 131 072 17 us in pieces, 28 whole; 130 of 50 021 23 and 20; 8 000 columns 10 and 8.  Rows that fill a compute
 // unit's registers take twice as long from 257 rows on: 300 rows of 131 072 57 and 72 us, 511 91 and 78
 void cut_distill(int64_t rows, int64_t vocab, int dtype, int* splits, int* chunk) {
@@ -1113,7 +1113,7 @@ int check_rows(const char* who, int64_t rows, int64_t vocab, int dtype) {
   if (vocab < 1 || vocab > kMaxVocab) return fail(AE_EINVAL, "%s: vocab must be 1 .. 2^20", who);
   return AE_OK;
 }
-bool temp_ok(float t) { return t > 0.0f && t <= FLT_MAX; }
+bool temp_ok(float t) { return t >= FLT_MIN && t <= FLT_MAX; }          // log2 e / t is finite
 
 }  // namespace
 }  // namespace ae
@@ -1126,7 +1126,7 @@ extern "C" int model_token_logprobs_workspace(int64_t rows, int64_t vocab, int t
   *bytes = 0;
   if (rows == 0) return AE_OK;
   int splits, chunk;
-  cut_logprob(rows, vocab, &splits, &chunk);
+  room_logprob(rows, vocab, &splits, &chunk);
   if (splits > 1) *bytes = align16(rows * splits * (int64_t)sizeof(Stats)) + rows * splits * (int64_t)top_k * 8;
   return AE_OK;
 }
@@ -1138,7 +1138,7 @@ extern "C" int model_token_logprobs(const void* logits, int64_t rows, int64_t vo
   int64_t need = 0;
   AE_TRY(check_rows("model_token_logprobs", rows, vocab, dtype));
   if (ld < vocab || ld >= ((int64_t)1 << 40)) return fail(AE_EINVAL, "model_token_logprobs: rows must not overlap");
-  if (!temp_ok(temperature)) return fail(AE_EINVAL, "model_token_logprobs: the temperature must be positive and finite");
+  if (!temp_ok(temperature)) return fail(AE_EINVAL, "model_token_logprobs: the temperature must be a positive normal number");
   if (n_tokens < 0 || n_tokens > 1024) return fail(AE_EINVAL, "model_token_logprobs: n_tokens must be 0 .. 1024");
   AE_TRY(model_token_logprobs_workspace(rows, vocab, top_k, dtype, &need));
   if (rows == 0) return AE_OK;
@@ -1187,7 +1187,7 @@ extern "C" int model_loss_distill(const void* logits, int64_t rows, int64_t voca
   int64_t need = 0;
   AE_TRY(check_rows("model_loss_distill", rows, vocab, dtype));
   if (ld < vocab || ld >= ((int64_t)1 << 40) || (d_logits && (ldd < vocab || ldd >= ((int64_t)1 << 40)))) return fail(AE_EINVAL, "model_loss_distill: rows must not overlap");
-  if (!temp_ok(temperature)) return fail(AE_EINVAL, "model_loss_distill: the temperature must be positive and finite");
+  if (!temp_ok(temperature)) return fail(AE_EINVAL, "model_loss_distill: the temperature must be a positive normal number");
   if (top_k < 1 || top_k > vocab) return fail(AE_EINVAL, "model_loss_distill: top_k must be 1 .. vocab");
   if (!loss_rows && !loss && !d_logits) return fail(AE_EINVAL, "model_loss_distill: no output");
   hipStream_t s = (hipStream_t)stream;

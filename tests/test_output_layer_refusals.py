@@ -134,3 +134,17 @@ def test_binding_refuses_wrong_tensors(ae):
         ae.model_token_logprobs(x, 4, 64, None, 0, None, None, None, None, None, None, None)
     with pytest.raises(AssertionError):
         ae.model_loss_distill(x, 4, 64, torch.zeros((4, 1), dtype=torch.int32), torch.zeros((4, 1)), None, None, None, None)
+
+
+@pytest.mark.parametrize("temp", [1e-39, float.fromhex("0x1.fffffcp-127"), -1.0, float("nan"), float("inf")])
+def test_temperature_is_a_positive_normal_number(ae, temp):
+    refused(ae, ae.lib.model_token_logprobs(P, 4, 64, 64, ae.AE_BF16, temp, None, 0, 1, None, P, P, P, P, P, P, None), "temperature")
+    refused(ae, ae.lib.model_loss_distill(P, 4, 64, 64, ae.AE_BF16, temp, P, P, 4, None, None, P, P, None, 0, P, None), "temperature")
+
+
+def test_sizes_end_below_the_largest_int(ae):
+    room = C.c_int64()
+    assert ae.lib.model_fp8_matmul_workspace((1 << 31) - 513, 1, 1, C.byref(room)) == 0 and room.value == 0
+    refused(ae, ae.lib.model_fp8_matmul_workspace((1 << 31) - 512, 1, 1, C.byref(room)), "bad argument")
+    refused(ae, ae.lib.model_fp8_matmul_workspace(1, (1 << 31) - 512, 1, C.byref(room)), "bad argument")
+    refused(ae, ae.lib.model_fp8_linear_workspace(1, 1, (1 << 31) - 512, C.byref(room)), "bad argument")
