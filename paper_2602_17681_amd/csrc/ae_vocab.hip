@@ -1046,9 +1046,18 @@ __global__ __launch_bounds__(NT) void k_distill_total(const float* __restrict__ 
                                                       float* __restrict__ loss) {
   __shared__ double sm[NW + 1];
   double acc = 0.0;
-  for (int64_t r = threadIdx.x; r < rows; r += NT) {
-    const float w = weight ? weight[r] : 1.0f;
-    if (w != 0.0f) acc += (double)w * (double)loss_rows[r];
+  constexpr int U = 8;                           // loads in flight: 8 192 rows 24 us one by one
+  for (int64_t r0 = threadIdx.x; r0 < rows; r0 += NT * U) {
+    float w[U], l[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r0 + u * NT;
+      l[u] = r < rows ? loss_rows[r] : 0.0f;
+      w[u] = r >= rows ? 0.0f : weight ? weight[r] : 1.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (w[u] != 0.0f) acc += (double)w[u] * (double)l[u];
   }
   acc = block_sum<NT>(acc, sm);
   if (threadIdx.x == 0) *loss = (float)acc;
@@ -1099,11 +1108,12 @@ void cut_rows(int64_t rows, int64_t vocab, bool cut, int* splits, int* chunk) {
 void cut_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 65536, splits, chunk); }
 // room for the pieces of rows is asked for from 32 769 columns on, so that the rule above is not the callers' concern
 void room_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 32768, splits, chunk); }
-// distillation: 64 rows of 131 072 17 us in pieces, 28 whole; 130 of 50 021 23 and 20; 8 000 columns 10 and 8.  Rows that fill a compute
+// distillation: 64 rows of 131 072 17 us in pieces, 28 whole; 100 of 50 021 16 and 19, 130 23 and 20; 4 rows
+// of 32 768 in binary32 with the sum 11 and 14, of 17 000 11 and 9; 8 000 columns 10 and 8.  Rows that fill a compute
 // unit's registers take twice as long from 257 rows on: 300 rows of 131 072 57 and 72 us, 511 91 and 78
 void cut_distill(int64_t rows, int64_t vocab, int dtype, int* splits, int* chunk) {
   const bool alone = vocab > 512 * 16 * (dtype == AE_BF16 ? 8 : 4);
-  cut_rows(rows, vocab, (rows < 128 && vocab > 16384) || (alone && rows > 256 && rows <= 384), splits, chunk);
+  cut_rows(rows, vocab, (rows < 128 && vocab > 24576) || (alone && rows > 256 && rows <= 384), splits, chunk);
 }
 int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
 
