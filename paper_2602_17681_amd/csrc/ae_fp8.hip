@@ -286,18 +286,22 @@ template <>
 struct Frag<true> {
   v8bf w[4];                             // the same, in eights
 };
+__device__ __forceinline__ v8bf exact_eight(const v8i& c, int s) {
+  v8bf w;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const v2bf lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + h], 1.0f, false);
+    const v2bf hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + h], 1.0f, true);
+    w[4 * h] = lo[0]; w[4 * h + 1] = lo[1]; w[4 * h + 2] = hi[0]; w[4 * h + 3] = hi[1];
+  }
+  return w;
+}
 template <bool EXACT>
 __device__ __forceinline__ Frag<EXACT> make_frag(v8i c) {
   Frag<EXACT> f;
   if constexpr (EXACT) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const v2bf lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + h], 1.0f, false);
-        const v2bf hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + h], 1.0f, true);
-        f.w[s][4 * h] = lo[0]; f.w[s][4 * h + 1] = lo[1]; f.w[s][4 * h + 2] = hi[0]; f.w[s][4 * h + 3] = hi[1];
-      }
+    for (int s = 0; s < 4; ++s) f.w[s] = exact_eight(c, s);
   } else {
     f.c = c;
   }
@@ -518,7 +522,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_fp8_few(const void* __restrict__
 // Bound by the matrix cores and by what of a tile's first load and last store nothing runs beside (one workgroup of
 // 256 x 256 fills a compute unit): 16 384 x 4 096 x 4 096 in bfloat16 250 us, 2 200 TFLOP/s; 4 096 x 4 096 x 4 096 62.
 // Binary32 results: by turning codes into bfloat16 (an instruction of half rate for two codes, 16 times a fragment) beside
-// the bfloat16 products: 4 096 x 4 096 x 4 096 150 us, 920 TFLOP/s.
+// the bfloat16 products: 4 096 x 4 096 x 4 096 140 us, 980 TFLOP/s, b in row blocks 156.
 template <int NJ> __device__ __forceinline__ int b_row(int i, int j) { return (i >> 2) * (4 * NJ) + j * 4 + (i & 3); }   // row of b in fragment j, place i
 __device__ __forceinline__ int a_key(int r) { return (r >> 1) & 7; }
 template <int NJ> __device__ __forceinline__ int b_key(int r) { return ((r / (4 * NJ)) & 3) << 1 | ((r >> 1) & 1); }
@@ -528,9 +532,12 @@ template <int NJ> __device__ __forceinline__ int b_key(int r) { return ((r / (4 
 // of it that reads; the kernel waits itself (vmcnt) where it needs the data.  There is no register result.  (The instruction
 // may read m0 one wait state after it was written, which the compiler does not see here: s_nop.)
 typedef int v4i __attribute__((ext_vector_type(4)));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      // m0 is a reserved register: the compiler keeps nothing in it from one of its own instructions to another
 __device__ __forceinline__ void load_to_lds(v4i rsrc, unsigned lds, unsigned voffset, unsigned soffset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // a raw buffer of `bytes` bytes, at most 2^31 - 1 of them, from p on
 __device__ __forceinline__ v4i buffer_of(const void* p, int64_t bytes) {
   const uint64_t a = (uint64_t)(uintptr_t)p;
@@ -680,19 +687,28 @@ __global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t*
   };
   auto row_scale = [&](int buf, int i) { return scales[buf][(BROWS ? 0 : (wn * NJ * 16 / BLK) * BM) + arow + i * 16]; };
   constexpr int AHEAD = MI > 2 ? 2 : 1;          // fragments of a that are on their way from LDS
-  Frag<EXACT> fb[NJ];
+  // Binary32 results: the next fragment of a is turned into bfloat16 a quarter at a time beside the products of the present
+  // one (fn), a fragment of b before the first product that takes it (LATE_B).  All where a step begins they took 551 us at
+  // 16 384 x 4 096 x 4 096, so 522, and held registers for longer (1 000 x 1 000 x 1 024, b in row blocks, 13.2 and 10.1).  Only
+  // 256 x 128 tiles with b in row blocks gain nothing (4 096 x 4 096 x 4 096 167 and, late, 169).
+  constexpr bool LATE_B = EXACT && !(BROWS && NWV == 8);
+  Frag<EXACT> fb[NJ], fn;
   v4f cs[NJ];
-  v8i ahead[AHEAD];
+  v8i ahead[AHEAD], raw_fb[LATE_B ? NJ : 1];
   float s_ahead[AHEAD];
   auto begin_step = [&](int buf) {
-    fb[0] = make_frag<EXACT>(raw_b(buf, 0));
+    if constexpr (LATE_B) raw_fb[0] = raw_b(buf, 0);
+    else fb[0] = make_frag<EXACT>(raw_b(buf, 0));
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       ahead[i] = raw_a(buf, i);
       s_ahead[i] = row_scale(buf, i);
     }
 #pragma unroll
-    for (int j = 1; j < NJ; ++j) fb[j] = make_frag<EXACT>(raw_b(buf, j));
+    for (int j = 1; j < NJ; ++j) {
+      if constexpr (LATE_B) raw_fb[j] = raw_b(buf, j);
+      else fb[j] = make_frag<EXACT>(raw_b(buf, j));
+    }
     if constexpr (BROWS) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) cs[j] = *reinterpret_cast<const v4f*>(&scales[buf][BM + wn * NJ * 16 + g * 4 * NJ + j * 4]);
@@ -716,7 +732,7 @@ __global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t*
     if constexpr (W != LAST) load_scales(c + 1, sv);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const Frag<EXACT> fa = make_frag<EXACT>(ahead[i % AHEAD]);
+      const Frag<EXACT> fa = EXACT && i > 0 ? fn : make_frag<EXACT>(ahead[i % AHEAD]);
       s_at[i & 1] = s_ahead[i % AHEAD];
       if (i + AHEAD < MI) {
         ahead[i % AHEAD] = raw_a(buf, i + AHEAD);
@@ -724,7 +740,13 @@ __global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t*
       }
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
+        if constexpr (LATE_B) {
+          if (i == 0) fb[j] = make_frag<EXACT>(raw_fb[j]);
+        }
         p[i & 1][j] = block_product<EXACT>(fb[j], fa);
+        if constexpr (EXACT) {
+          if (i + 1 < MI) fn.w[j] = exact_eight(ahead[(i + 1) % AHEAD], j);
+        }
         if (i > 0) add_scaled(i - 1, j, p[(i - 1) & 1][j], s_at[(i - 1) & 1]);
         if constexpr (W != LAST) {
           if (i * NJ + j < LOADS) load_part(c + 1, i * NJ + j, W == MORE_TAIL);
