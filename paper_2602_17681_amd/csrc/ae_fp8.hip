@@ -888,7 +888,7 @@ int launch_tile(const Product& p, hipStream_t s) {
 }
 // The largest tiles that still leave no compute unit idle, by the number of tiles (256 compute units; times with the quantiser):
 //   up to 256 of 64 x 64     four groups of K    200 x 4 096 x 4 096 in bfloat16 22 us (two groups 26, one 34; 128 x 128 in two groups 33)
-//   up to 512                two groups          400 x 4 096 x 4 096 30 us (four 36, one 35; 128 x 128 in two groups 33); binary32: 128 x 64, 37 us (64 x 64 54)
+//   up to 512                two groups          400 x 4 096 x 4 096 30 us (four 36, one 35; 128 x 128 in two groups 33); binary32: 128 x 64, the product 32.8 us (64 x 64 34.2)
 //   up to 256 of 128 x 128   two groups of K     777 x 4 096 x 4 096 36 us (one 44; 64 x 64 39; 256 x 256 57)
 //   more                     one group, two workgroups to a compute unit    1 500 x 4 096 x 4 096 49 us (256 x 256 59; 64 x 64 63)
 //   from 192 of 256 x 256    1 500 x 8 192 x 2 048 41 us (128 x 128 48).  Binary32 results and b in row blocks need more registers:
