@@ -957,22 +957,31 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     __syncthreads();
     if (!p.teacher_lse && wave * 64 < k) norm += log_of(sum_of<NWV>(smd[0]));      // for wavefronts with entries of the list
     m = max_of<NWV>(smf[1]);
-    // e_j = 2^(z_j ce + k2) in one operation, k2 = -m ce.  What k2 is rounded by is a factor of all e_j, of their sums too;
-    // the loss takes it out again (`off`).  Beyond 2^100 neighbouring numbers are 2^76 apart: e_j is 1 at the maximum and 0
-    // elsewhere, with any factor, and 1 leaves m as it is.
-    float ce = c2, k2 = -reference(m) * c2;
-    if (!(fabsf(k2) < 0x1p100f)) {
-      ce = 1.0f;
-      k2 = -reference(m);
+    // e_j = 2^(z_j c2 + k2) in one operation, k2 = -m c2.  What k2 is rounded by, |k2| 2^-25 at most, is a factor of all e_j, of
+    // their sums too; the loss takes it out again (`off`).  That will do while the factor is near 1.  From |k2| = 2^20 on (a
+    // large maximum, a low temperature; the same for all threads) the row becomes z_j - m before that, with k2 = 0: a
+    // difference that the type does not hold is off by its last place, but of bfloat16 numbers it is then 0 or over
+    // 2^20 2^-8 / c2, of which nothing is left anyway.  (A choice in every exponent takes 2 % longer.)
+    float k2 = -reference(m) * c2, shift = 0.0f;
+    if (!(fabsf(k2) < 0x1p20f)) {
+      shift = reference(m);
+      k2 = 0.0f;
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (sizeof(T) == 4) raw[u][i] = __float_as_uint(element(u, i) - shift);
+          else raw[u][i] = pack_bf16(element(u, 2 * i) - shift, element(u, 2 * i + 1) - shift);
+        }
     }
-    const float off = fmaf(reference(m), ce, k2);
+    const float off = fmaf(reference(m) - shift, c2, k2);
     // e_j of a vector's columns
     auto exponentials = [&](int u, float (&e)[V]) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) e[i] = fast_exp2(fmaf(element(u, i), ce, k2));
+      for (int i = 0; i < V; ++i) e[i] = fast_exp2(fmaf(element(u, i), c2, k2));
     };
     float s_out = 0.0f, s_in = 0.0f;
-    const float e_tail = fast_exp2(fmaf(z_tail, ce, k2));
+    const float e_tail = fast_exp2(fmaf(z_tail - shift, c2, k2));
     const bool in_tail = c_tail < n && (bits[c_tail >> 5] >> (c_tail & 31) & 1);
     (in_tail ? s_in : s_out) = e_tail;
 #pragma unroll
@@ -1032,7 +1041,7 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     }
     if (c_tail < n && !in_tail) Store<T>::st(g + c_tail, r.f_out * e_tail);
     if (valid(id0)) {
-      const double q = (double)(fast_exp2(fmaf(z0, ce, k2)) / r.s_all);
+      const double q = (double)(fast_exp2(fmaf(z0 - shift, c2, k2)) / r.s_all);
       Store<T>::st(g + id0, r.empty ? 0.0f : (float)((r.mass * q - pi0) * r.scale));
     }
     if (t == NTH - 64) p.loss_rows[row] = row_loss(p, st, r, off);      // the last wavefront: the list is the first ones'
