@@ -183,8 +183,8 @@ __device__ uint32_t top_bound(TopShared& sh, int k, uint32_t tmax) {
 
 // Where more keys reach the bound than LDS holds (long runs of equal logits, many large ones in one share): the exact value
 // of the k-th largest, by its digits if the bound is not it already; then what is larger, in any order, and of what
-// is equal the first ones in the order of the index.  (A share of nothing but NaN counts as -infinity in the bound, which
-// may then be too high.)  A source gives its keys in steps of W to a thread, in that order.
+// is equal the first ones in the order of the index.  There are enough of them, since k maxima of shares, which are keys, reach
+// the bound.  A source gives its keys in steps of W to a thread, in that order.
 template <typename Src, typename F>
 __device__ __forceinline__ void for_steps(const Src& src, F f) {          // f(keys, how many) for the thread's steps, four loads in flight
   constexpr int W = Src::W;
@@ -198,7 +198,7 @@ __device__ __forceinline__ void for_steps(const Src& src, F f) {          // f(k
   }
 }
 template <typename Src>
-__device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, const Src& src) {
+__device__ void top_exact(TopShared& sh, int k, uint32_t bound, const Src& src) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   constexpr int W = Src::W;
   uint64_t key[W];
@@ -221,7 +221,7 @@ __device__ void top_exact(TopShared& sh, int k, uint32_t bound, bool too_high, c
   __syncthreads();
   uint32_t value = bound;
   int larger = sh.count;
-  if (larger >= k || too_high) {
+  if (larger >= k) {
     value = 0;
     larger = 0;                          // keys known to be larger than every one with the prefix `value`
     for (int d = 3; d >= 0; --d) {
@@ -471,12 +471,13 @@ __global__ __launch_bounds__(NT, 6) void k_logprob(LogprobArgs p) {
       }
     }
   }
-  const uint32_t tmax = t * V < n ? order_key(st.m) : 0u;
+  // the share's largest key; -infinity is none of its keys for sure if there are NaN, so for the bound such a share has the lowest
+  const uint32_t tmax = t * V < n ? order_key(st.m) : 0u, sure = st.m == -INFINITY && st.s != st.s ? 0u : tmax;
   const Stats all = block_join(st, c2, sm);
   if (p.splits > 1 && t == 0) p.part[row * p.splits + split] = all;
   if constexpr (TOP) {
     const int k = p.top_k < n ? p.top_k : n;
-    const uint32_t bound = top_bound(sh, k, tmax);
+    const uint32_t bound = top_bound(sh, k, sure);
     // the parts of shares that reach the bound, then their vectors, one to a thread
     if (tmax >= bound) {
       for (int g = 0; g * per < rounds; ++g)
@@ -502,7 +503,7 @@ __global__ __launch_bounds__(NT, 6) void k_logprob(LogprobArgs p) {
     }
     __syncthreads();
     const int found = sh.count;
-    if (pairs > CAND || found < k || found > CAND) top_exact(sh, k, bound, pairs <= CAND && found < k, RowKeys<T>{z, n, c0});
+    if (pairs > CAND || found > CAND) top_exact(sh, k, bound, RowKeys<T>{z, n, c0});
     if (p.splits == 1) {
       const RowLog r = row_log(all);
       top_ranked(sh, k, [&](int rank, uint64_t key) { write_top(p, row, r, rank, key); });
@@ -548,7 +549,7 @@ __global__ __launch_bounds__(NT) void k_logprob_join(LogprobArgs p) {
     }
     __syncthreads();
     const int found = sh.count;
-    if (found < p.top_k || found > CAND) top_exact(sh, p.top_k, bound, found < p.top_k, src);
+    if (found > CAND) top_exact(sh, p.top_k, bound, src);
     const RowLog r = row_log(all);
     top_ranked(sh, p.top_k, [&](int rank, uint64_t k) { write_top(p, row, r, rank, k); });
   }
