@@ -453,7 +453,8 @@ int model_fp8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, con
  *     teacher_lse null: p_i = exp(t_i / T) / sum over the list, no rest (p_r = 0);
  *     teacher_lse [rows] (the teacher's lse over its whole vocabulary, at the same T): p_i = exp(t_i / T - teacher_lse),
  *       p_r = max(0, 1 - sum p_i), the probability of all other tokens as one outcome (left out where the student has
- *       none: q_r = 0).
+ *       none: no other logit within 708 T of the row's maximum, whether masked or merely so far away that q_r is below the
+ *       normal numbers of binary64).
  *     L_r = sum_i p_i (log p_i - log q_{c_i}) + p_r (log p_r - log q_r),  q_r = sum of q_j outside the list;
  *     dL/dz_j = (P q_j - p_j) / T in the list, q_j (P - p_r / q_r) / T outside, P = sum p_i + p_r.
  *   loss_rows [rows] = L_r (nullable); loss [1] = sum_r w_r L_r (nullable); d_logits [rows][vocab] in dtype, row stride ldd:

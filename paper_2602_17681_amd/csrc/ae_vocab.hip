@@ -557,10 +557,24 @@ __global__ __launch_bounds__(NT) void k_logprob_join(LogprobArgs p) {
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------
-struct DistillPart {                     // of a row piece
-  float m, s_out, s_in, pad;             // maximum; sums of e_j outside and inside the teacher's list
-  double p, l;                           // sums over the list's entries in the piece: p_i, and p_i (log p_i - (z_i - m) / T)
+// Statistics of a row piece.  What lies outside the teacher's list has a maximum of its own, so that its sum, by which the
+// teacher's remaining mass is divided, neither vanishes nor loses bits where the list lies far above it.
+struct DistillPart {
+  float m_out, s_out, m_in, s_in;        // outside and inside the list: maximum, and sum of exp((z_j - that maximum) / T)
+  double p, l;                           // sums over the list's entries in the piece: p_i, and p_i (log p_i - (z_i - m) / T), m = the larger maximum
 };
+__device__ __forceinline__ float maximum(const DistillPart& st) { return fmaxf(st.m_out, st.m_in); }
+// a logit joins a sum with its running maximum
+__device__ __forceinline__ void add_logit(float& m, float& s, float z, float c2) {
+  if (z > m) {
+    s *= fast_exp2((m - z) * c2);
+    m = z;
+  }
+  s += fast_exp2((z - reference(m)) * c2);
+}
+// Other tokens with all their logits more than 708 T below the row's maximum (their probabilities are no normal binary64
+// numbers any more; masks like -10^4) are ones that the student does not have.
+constexpr double kFarthest = 708.0;
 struct DistillArgs {
   const void* logits;
   int64_t rows, ld;
@@ -633,61 +647,64 @@ template <int V> __device__ __forceinline__ uint32_t marks_of(const uint32_t* bi
 
 template <typename T>
 __device__ DistillPart piece_stats(const DistillArgs& p, int64_t row, int c0, int n, const uint32_t* bits, double norm, float c2,
-                                   float (*smf)[NW] /* 3 */, double (*smd)[NW] /* 2 */) {
+                                   float (*smf)[NW] /* 4 */, double (*smd)[NW] /* 2 */) {
   constexpr int V = Store<T>::VEC;
   const T* z = (const T*)p.logits + row * p.ld + c0;
-  DistillPart st = {-INFINITY, 0.0f, 0.0f, 0.0f, 0.0, 0.0};
-  for_vectors<T>(z, n, [&](const float (&v)[V], int c, int) {
-    float cm = v[0];
-#pragma unroll
-    for (int i = 1; i < V; ++i) cm = fmaxf(cm, v[i]);
-    if (cm > st.m) {
-      const float f = fast_exp2((st.m - cm) * c2);
-      st.s_out *= f;
-      st.s_in *= f;
-      st.m = cm;
-    }
-    const float ref = reference(st.m);
-    const uint32_t mk = marks_of<V>(bits, c);
-    float e[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = fast_exp2((v[i] - ref) * c2);
-    if (mk) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (mk >> i & 1) st.s_in += e[i];
-        else st.s_out += e[i];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) st.s_out += e[i];
-    }
-  });
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  float m = max_rows(max16(st.m));
-  float f = fast_exp2((st.m - reference(m)) * c2);
-  const float w_out = sum_rows(sum16(f * st.s_out)), w_in = sum_rows(sum16(f * st.s_in));
-  __syncthreads();
-  if (lane == 0) {
-    smf[0][wave] = m;
-    smf[1][wave] = w_out;
-    smf[2][wave] = w_in;
-  }
-  __syncthreads();
-  const int i8 = lane & 15;
-  const float m_i = i8 < NW ? smf[0][i8] : -INFINITY;
-  m = max16(m_i);
-  f = fast_exp2((m_i - reference(m)) * c2);
-  st = {m, sum16(i8 < NW ? f * smf[1][i8] : 0.0f), sum16(i8 < NW ? f * smf[2][i8] : 0.0f), 0.0f, 0.0, 0.0};
-  const double ref = (double)reference(m), inv_t = 1.0 / (double)p.temp;
+  float m_out = -INFINITY, s_out = 0.0f, m_in = -INFINITY, s_in = 0.0f;
+  // the list: its part of the sum, and the loss's terms, relative to the thread's maximum as long as the row's is not known
+  const double inv_t = 1.0 / (double)p.temp;
   double sp = 0.0, sl = 0.0;
   for (int i = threadIdx.x; i < p.top_k; i += NT) {
     const int id = p.top_id[row * p.top_k + i];
     if (id < c0 || id >= c0 + n) continue;
+    const float z_i = Store<T>::ld(z + id - c0);
+    const double before = (double)reference(m_in);
+    add_logit(m_in, s_in, z_i, c2);
+    const double ref_t = (double)reference(m_in);
+    if (sp != 0.0) sl += sp * (ref_t - before) * inv_t;
     const double lp = list_log_p(p, row * p.top_k + i, norm), pi = exp_of(lp);
     sp += pi;
-    if (pi != 0.0) sl += pi * (lp - ((double)Store<T>::ld(z + id - c0) - ref) * inv_t);
+    if (pi != 0.0) sl += pi * (lp - ((double)z_i - ref_t) * inv_t);
   }
+  for_vectors<T>(z, n, [&](const float (&all)[V], int c, int) {
+    float v[V];
+    const uint32_t mk = marks_of<V>(bits, c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = all[i];
+    if (mk) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = mk >> i & 1 ? -INFINITY : v[i];
+    }
+    float cm = v[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) cm = fmaxf(cm, v[i]);
+    if (cm > m_out) {
+      s_out *= fast_exp2((m_out - cm) * c2);
+      m_out = cm;
+    }
+    const float ref = reference(m_out);
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_out += fast_exp2((v[i] - ref) * c2);
+  });
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  float w_out = max_rows(max16(m_out)), w_in = max_rows(max16(m_in));
+  s_out = sum_rows(sum16(fast_exp2((m_out - reference(w_out)) * c2) * s_out));
+  s_in = sum_rows(sum16(fast_exp2((m_in - reference(w_in)) * c2) * s_in));
+  __syncthreads();
+  if (lane == 0) {
+    smf[0][wave] = w_out;
+    smf[1][wave] = s_out;
+    smf[2][wave] = w_in;
+    smf[3][wave] = s_in;
+  }
+  __syncthreads();
+  const int i8 = lane & 15;
+  const bool there = i8 < NW;
+  const float o_i = there ? smf[0][i8] : -INFINITY, i_i = there ? smf[2][i8] : -INFINITY;
+  DistillPart st = {max16(o_i), 0.0f, max16(i_i), 0.0f, 0.0, 0.0};
+  st.s_out = sum16(there ? fast_exp2((o_i - reference(st.m_out)) * c2) * smf[1][i8] : 0.0f);
+  st.s_in = sum16(there ? fast_exp2((i_i - reference(st.m_in)) * c2) * smf[3][i8] : 0.0f);
+  if (sp != 0.0) sl -= sp * ((double)reference(m_in) - (double)reference(maximum(st))) * inv_t;
   if (p.top_k > 64 || wave == 0) {               // whose lanes have entries
     sp = wave_sum(sp);
     sl = wave_sum(sl);
@@ -704,32 +721,38 @@ __device__ DistillPart piece_stats(const DistillArgs& p, int64_t row, int c0, in
 
 // What the statistics of a whole row give.  The loss, with its logarithms in binary64, is for one wavefront to compute.
 struct RowGrad {
-  float ref, f_out, s_all;               // what exponents are relative to; the gradient outside the list is f_out e_j; sum of e_j
+  float ref, ref_out, s_all;             // what exponents are relative to, outside the list; sum of e_j relative to ref
+  float f_out;                           // the gradient outside the list is f_out exp((z_j - ref_out) / T)
   double mass, rest, scale;              // P, p_r, w / T
+  double s_sum, gap;                     // the sum once more; (ref - ref_out) / T
   bool empty;
 };
-__device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillPart& st, float w) {
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillPart& st, float w, float c2) {
   RowGrad r;
-  r.ref = reference(st.m);
-  r.s_all = st.s_out + st.s_in;
+  const float m = maximum(st);
+  r.ref = reference(m);
+  r.ref_out = reference(st.m_out);
+  const float a = fast_exp2((st.m_out - r.ref) * c2), b = fast_exp2((st.m_in - r.ref) * c2);
+  r.s_all = a * st.s_out + b * st.s_in;
+  r.s_sum = (double)a * (double)st.s_out + (double)b * (double)st.s_in;
   r.empty = r.s_all == 0.0f;
   r.rest = p.teacher_lse ? 1.0 - st.p : 0.0;
   if (!(r.rest > 0.0) && r.rest == r.rest) r.rest = 0.0;
-  if (st.s_out == 0.0f) r.rest = 0.0;
+  r.gap = ((double)r.ref - (double)r.ref_out) / (double)p.temp;
+  if (st.s_out == 0.0f || r.gap > kFarthest) r.rest = 0.0;
   r.mass = st.p + r.rest;
   const float scale = w / p.temp;
   r.scale = (double)scale;
-  // P - p_r / q_r, over the sum
-  const float outside = r.rest != 0.0 ? (float)(r.mass - r.rest * (double)(r.s_all / st.s_out)) : (float)r.mass;
+  // P - p_r / q_r, over the sum; of each, a is left where the exponents are relative to the outside's maximum
+  const float outside = r.rest != 0.0 ? (float)(r.mass * (double)a - r.rest * (double)(r.s_all / st.s_out)) : (float)r.mass * a;
   r.f_out = r.empty ? 0.0f : outside * scale / r.s_all;
   return r;
 }
 // off: the sums are 2^off times those of exponents relative to the maximum
-__device__ float row_loss(const DistillArgs& p, const DistillPart& st, const RowGrad& r, float off = 0.0f) {
+__device__ float row_loss(const DistillPart& st, const RowGrad& r, float off = 0.0f) {
   if (r.empty) return 0.0f;
-  const double s_all = (double)st.s_out + (double)st.s_in;
-  double loss = st.l + (st.p != 0.0 ? st.p * (log_of(s_all) - (double)off * 0.69314718055994530942) : 0.0);
-  if (r.rest != 0.0) loss += r.rest * log_of(r.rest * s_all / (double)st.s_out);
+  double loss = st.l + (st.p != 0.0 ? st.p * (log_of(r.s_sum) - (double)off * 0.69314718055994530942) : 0.0);
+  if (r.rest != 0.0) loss += r.rest * (log_of(r.rest * r.s_sum / (double)st.s_out) + r.gap);
   return (float)loss;
 }
 // stores the gradient of a vector's columns: those of the list are left as they are, since g may be z, which they still need
@@ -766,7 +789,7 @@ __device__ void piece_gradient(const DistillArgs& p, int64_t row, int c0, int n,
   for_vectors<T>(z, n, [&](const float (&v)[V], int c, int len) {
     float o[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = r.f_out * fast_exp2((v[i] - r.ref) * c2);
+    for (int i = 0; i < V; ++i) o[i] = r.f_out * fast_exp2((v[i] - r.ref_out) * c2);
     store_outside<T>(g + c, o, marks_of<V>(bits, c), len);
   });
   list_gradient<T, NT>(p, row, c0, n, norm, c2, r);
@@ -775,13 +798,16 @@ __device__ void piece_gradient(const DistillArgs& p, int64_t row, int c0, int n,
 // The statistics of a row from those of its pieces, one to a lane; in every lane.
 __device__ DistillPart joined(const DistillArgs& p, int64_t row, float c2) {
   const int lane = threadIdx.x & 63;
-  DistillPart v = {-INFINITY, 0.0f, 0.0f, 0.0f, 0.0, 0.0};
+  DistillPart v = {-INFINITY, 0.0f, -INFINITY, 0.0f, 0.0, 0.0};
   if (lane < p.splits) v = p.part[row * p.splits + lane];
-  const float m = max_rows(max16(v.m));
-  const float f = fast_exp2((v.m - reference(m)) * c2);
+  DistillPart st = {max_rows(max16(v.m_out)), 0.0f, max_rows(max16(v.m_in)), 0.0f, 0.0, 0.0};
+  st.s_out = sum_rows(sum16(fast_exp2((v.m_out - reference(st.m_out)) * c2) * v.s_out));
+  st.s_in = sum_rows(sum16(fast_exp2((v.m_in - reference(st.m_in)) * c2) * v.s_in));
   // the piece's own maximum in the terms of l becomes the row's
-  if (v.p != 0.0) v.l -= v.p * ((double)reference(v.m) - (double)reference(m)) / (double)p.temp;
-  return {m, sum_rows(sum16(f * v.s_out)), sum_rows(sum16(f * v.s_in)), 0.0f, wave_sum(v.p), wave_sum(v.l)};
+  if (v.p != 0.0) v.l -= v.p * ((double)reference(maximum(v)) - (double)reference(maximum(st))) / (double)p.temp;
+  st.p = wave_sum(v.p);
+  st.l = wave_sum(v.l);
+  return st;
 }
 
 template <typename T>
@@ -804,7 +830,7 @@ __device__ void total_of_pieces(const DistillArgs& p, float c2, double* sm /* NW
     const float w = p.weight ? p.weight[row] : 1.0f;
     if (w == 0.0f) continue;
     const DistillPart st = joined(p, row, c2);
-    if ((threadIdx.x & 63) == 0) acc += (double)w * (double)row_loss(p, st, row_grad(p, st, w));
+    if ((threadIdx.x & 63) == 0) acc += (double)w * (double)row_loss(st, row_grad(p, st, w, c2));
   }
   acc = block_sum<NT>(acc, sm);
   if (threadIdx.x == 0) *p.loss = (float)acc;
@@ -816,7 +842,7 @@ __device__ void total_of_pieces(const DistillArgs& p, float c2, double* sm /* NW
 template <typename T, int MODE>
 __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   extern __shared__ uint32_t bits[];
-  __shared__ float smf[3][NW];
+  __shared__ float smf[4][NW];
   __shared__ double smp[2][NW], smd[NW + 1];
   const int64_t row = blockIdx.x / p.splits;
   const int split = (int)(blockIdx.x - row * p.splits);
@@ -844,8 +870,8 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   } else {
     st = joined(p, row, c2);
   }
-  const RowGrad r = row_grad(p, st, w);
-  if (threadIdx.x == 0 && split == 0) p.loss_rows[row] = row_loss(p, st, r);
+  const RowGrad r = row_grad(p, st, w, c2);
+  if (threadIdx.x == 0 && split == 0) p.loss_rows[row] = row_loss(st, r);
   if (MODE == 2 && p.loss && blockIdx.x == gridDim.x - 1) total_of_pieces(p, c2, smd);
   if (p.d_logits) piece_gradient<T>(p, row, c0, n, bits, norm, c2, r);
 }
@@ -891,6 +917,10 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
   };
   auto element = [&](int u, int i) {
     return sizeof(T) == 4 ? __uint_as_float(raw[u][i % 4]) : __uint_as_float(i & 1 ? raw[u][i / 2] & 0xFFFF0000u : raw[u][i / 2] << 16);
+  };
+  auto exclude = [&](int u, int i) {
+    if constexpr (sizeof(T) == 4) raw[u][i % 4] = 0xFF800000u;
+    else raw[u][i / 2] = i & 1 ? (raw[u][i / 2] & 0xFFFFu) | 0xFF800000u : (raw[u][i / 2] & 0xFFFF0000u) | 0xFF80u;
   };
   int id_next = -1;
   float top_next = 0.0f, tail_next = 0.0f, lse_next = 0.0f;
@@ -975,30 +1005,29 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
           else raw[u][i] = pack_bf16(element(u, 2 * i) - shift, element(u, 2 * i + 1) - shift);
         }
     }
-    const float off = fmaf(reference(m) - shift, c2, k2);
+    const float off = fmaf(reference(m) - shift, c2, k2);     // 0 after that
     // e_j of a vector's columns
     auto exponentials = [&](int u, float (&e)[V]) {
 #pragma unroll
       for (int i = 0; i < V; ++i) e[i] = fast_exp2(fmaf(element(u, i), c2, k2));
     };
-    float s_out = 0.0f, s_in = 0.0f;
-    const float e_tail = fast_exp2(fmaf(z_tail - shift, c2, k2));
+    // the list's logits are its threads'; in the row, -infinity stands for them
     const bool in_tail = c_tail < n && (bits[c_tail >> 5] >> (c_tail & 31) & 1);
-    (in_tail ? s_in : s_out) = e_tail;
+    const float x_tail = in_tail ? -INFINITY : z_tail - shift;
+    const float e0 = valid(id0) ? fast_exp2(fmaf(z0 - shift, c2, k2)) : 0.0f;
+    float e_tail = fast_exp2(fmaf(x_tail, c2, k2)), s_out = e_tail, s_in = e0;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int c = u * STEP + tv;
       if (u * STEP < whole) {
         const uint32_t mk = c < whole ? marks_of<V>(bits, c) : 0u;
-        float e[V];
-        exponentials(u, e);
         if (mk) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            s_in += mk >> i & 1 ? e[i] : 0.0f;
-            e[i] = mk >> i & 1 ? 0.0f : e[i];
-          }
+          for (int i = 0; i < V; ++i)
+            if (mk >> i & 1) exclude(u, i);
         }
+        float e[V];
+        exponentials(u, e);
         float sum = e[0];
 #pragma unroll
         for (int i = 1; i < V; ++i) sum += e[i];
@@ -1024,8 +1053,52 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
       smd[2][wave] = sl;
     }
     __syncthreads();
-    const DistillPart st = {m, sum_of<NWV>(smf[2]), sum_of<NWV>(smf[3]), 0.0f, sum_of<NWV>(smd[1]), sum_of<NWV>(smd[2])};
-    const RowGrad r = row_grad(p, st, w);
+    const float ref = reference(m) - shift;                    // in the row's present numbers
+    DistillPart st = {ref, sum_of<NWV>(smf[2]), ref, sum_of<NWV>(smf[3]), sum_of<NWV>(smd[1]), sum_of<NWV>(smd[2])};
+    float back = 1.0f;
+    // One maximum will do for both sums while the outside's keeps its bits.  Where the teacher has a rest and that sum is small
+    // (the same for all threads), it is taken again, relative to a maximum of its own; so is the gradient outside.
+    if (p.teacher_lse && st.p < 1.0 && st.s_out < 0x1p-40f) {
+      float mo = x_tail;
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) mo = fmaxf(mo, element(u, i));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mo = max_rows(max16(mo));
+      forget();
+      if ((t & 63) == 0) smf[0][wave] = mo;
+      __syncthreads();
+      st.m_out = mo = max_of<NWV>(smf[0]);
+      if (((double)ref - (double)mo) * inv_t <= kFarthest) {     // so mo is hardly larger than the maximum, and k2 as small as before
+        k2 = -mo * c2;
+        float so = e_tail = fast_exp2(fmaf(x_tail, c2, k2));
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+          float e[V];
+          exponentials(u, e);
+#pragma unroll
+          for (int i = 0; i < V; ++i) so += e[i];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        so = sum_rows(sum16(so));
+        forget();
+        if ((t & 63) == 0) smf[1][wave] = so;
+        __syncthreads();
+        // in the measure of the other sum, 2^off
+        back = fast_exp2(off - fmaf(mo, c2, k2));
+        st.s_out = sum_of<NWV>(smf[1]) * back;
+      }
+    }
+    RowGrad r = row_grad(p, st, w, c2);
+    r.f_out *= back;
+    // the list's gradient and the loss first: what they are made of need not be held beside the row
+    if (valid(id0)) {
+      const double q = (double)(e0 / r.s_all);
+      Store<T>::st(g + id0, r.empty ? 0.0f : (float)((r.mass * q - pi0) * r.scale));
+    }
+    if (t == NTH - 64) p.loss_rows[row] = row_loss(st, r, off);      // the last wavefront: the list is the first ones'
     if (w_next != 0.0f) ask_for_rest(row + gridDim.x);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
@@ -1041,11 +1114,6 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
       __builtin_amdgcn_sched_barrier(0);
     }
     if (c_tail < n && !in_tail) Store<T>::st(g + c_tail, r.f_out * e_tail);
-    if (valid(id0)) {
-      const double q = (double)(fast_exp2(fmaf(z0 - shift, c2, k2)) / r.s_all);
-      Store<T>::st(g + id0, r.empty ? 0.0f : (float)((r.mass * q - pi0) * r.scale));
-    }
-    if (t == NTH - 64) p.loss_rows[row] = row_loss(p, st, r, off);      // the last wavefront: the list is the first ones'
     w = w_next;
     __syncthreads();                             // the marks and sums have been read
   }
