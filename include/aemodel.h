@@ -460,7 +460,8 @@ int model_fp8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, con
  *   loss_rows [rows] = L_r (nullable); loss [1] = sum_r w_r L_r (nullable); d_logits [rows][vocab] in dtype, row stride ldd:
  *   the gradient of that sum (nullable; it may be logits itself, with the same stride).  weight [rows] (nullable: 1): a
  *   row whose weight is 0 is not read, its loss and gradient are 0.  A list of one token is the cross entropy with a
- *   label.  Terms with p = 0 are 0.
+ *   label.  Terms with p = 0 are 0.  A teacher's row without any outcome (teacher_lse -infinity, as model_token_logprobs returns it
+ *   for an empty row; without teacher_lse, a list of nothing but -infinity) has no loss and no gradient.
  * workspace: the matching _workspace bytes, 16-byte aligned; its contents need not be kept. */
 int model_token_logprobs_workspace(int64_t rows, int64_t vocab, int top_k, int dtype, int64_t* bytes);
 int model_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, float temperature,

@@ -630,7 +630,11 @@ __device__ double list_norm(const DistillArgs& p, int64_t row, double* sm /* NTH
   s = block_sum<NTH>(s, sm);
   return dm / (double)p.temp + log_of(s);
 }
-__device__ __forceinline__ double list_log_p(const DistillArgs& p, int64_t at, double norm) { return (double)p.top_logit[at] / (double)p.temp - norm; }
+// a norm of -infinity: a teacher without any outcome (-infinity less -infinity would be NaN)
+__device__ __forceinline__ double list_log_p(const DistillArgs& p, int64_t at, double norm) {
+  return norm == -INFINITY ? -INFINITY : (double)p.top_logit[at] / (double)p.temp - norm;
+}
+__device__ __forceinline__ bool has_rest(const DistillArgs& p, double norm) { return p.teacher_lse && norm != -INFINITY; }
 
 // marks the list's tokens that lie in columns [c0, c0 + n): a bit for each column
 template <int NTH>
@@ -727,7 +731,7 @@ struct RowGrad {
   double s_sum, gap;                     // the sum once more; (ref - ref_out) / T
   bool empty;
 };
-__device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillPart& st, float w, float c2) {
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillPart& st, float w, float c2, bool tail) {
   RowGrad r;
   const float m = maximum(st);
   r.ref = reference(m);
@@ -736,7 +740,7 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillP
   r.s_all = a * st.s_out + b * st.s_in;
   r.s_sum = (double)a * (double)st.s_out + (double)b * (double)st.s_in;
   r.empty = r.s_all == 0.0f;
-  r.rest = p.teacher_lse ? 1.0 - st.p : 0.0;
+  r.rest = tail ? 1.0 - st.p : 0.0;
   if (!(r.rest > 0.0) && r.rest == r.rest) r.rest = 0.0;
   r.gap = ((double)r.ref - (double)r.ref_out) / (double)p.temp;
   if (st.s_out == 0.0f || r.gap > kFarthest) r.rest = 0.0;
@@ -830,7 +834,7 @@ __device__ void total_of_pieces(const DistillArgs& p, float c2, double* sm /* NW
     const float w = p.weight ? p.weight[row] : 1.0f;
     if (w == 0.0f) continue;
     const DistillPart st = joined(p, row, c2);
-    if ((threadIdx.x & 63) == 0) acc += (double)w * (double)row_loss(st, row_grad(p, st, w, c2));
+    if ((threadIdx.x & 63) == 0) acc += (double)w * (double)row_loss(st, row_grad(p, st, w, c2, has_rest(p, p.teacher_lse ? (double)p.teacher_lse[row] : 0.0)));
   }
   acc = block_sum<NT>(acc, sm);
   if (threadIdx.x == 0) *p.loss = (float)acc;
@@ -870,7 +874,7 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   } else {
     st = joined(p, row, c2);
   }
-  const RowGrad r = row_grad(p, st, w, c2);
+  const RowGrad r = row_grad(p, st, w, c2, has_rest(p, norm));
   if (threadIdx.x == 0 && split == 0) p.loss_rows[row] = row_loss(st, r);
   if (MODE == 2 && p.loss && blockIdx.x == gridDim.x - 1) total_of_pieces(p, c2, smd);
   if (p.d_logits) piece_gradient<T>(p, row, c0, n, bits, norm, c2, r);
@@ -986,6 +990,7 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     forget();
     if ((t & 63) == 0) smf[1][wave] = m;
     __syncthreads();
+    const bool tail = has_rest(p, norm);
     if (!p.teacher_lse && wave * 64 < k) norm += log_of(sum_of<NWV>(smd[0]));      // for wavefronts with entries of the list
     m = max_of<NWV>(smf[1]);
     // e_j = 2^(z_j c2 + k2) in one operation, k2 = -m c2.  What k2 is rounded by, |k2| 2^-25 at most, is a factor of all e_j, of
@@ -1038,7 +1043,7 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     forget();
     double pi0 = 0.0, sp, sl = 0.0;
     if (valid(id0)) {
-      const double lp = (double)top0 * inv_t - norm;
+      const double lp = norm == -INFINITY ? -INFINITY : (double)top0 * inv_t - norm;
       pi0 = exp_of(lp);
       if (pi0 != 0.0) sl = pi0 * (lp - ((double)z0 - (double)reference(m)) * inv_t);
     }
@@ -1058,7 +1063,7 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
     float back = 1.0f;
     // One maximum will do for both sums while the outside's keeps its bits.  Where the teacher has a rest and that sum is small
     // (the same for all threads), it is taken again, relative to a maximum of its own; so is the gradient outside.
-    if (p.teacher_lse && st.p < 1.0 && st.s_out < 0x1p-40f) {
+    if (tail && st.p < 1.0 && st.s_out < 0x1p-40f) {
       float mo = x_tail;
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
@@ -1091,7 +1096,7 @@ __global__ __launch_bounds__(NTH, 4) void k_distill_row(DistillArgs p) {
         st.s_out = sum_of<NWV>(smf[1]) * back;
       }
     }
-    RowGrad r = row_grad(p, st, w, c2);
+    RowGrad r = row_grad(p, st, w, c2, tail);
     r.f_out *= back;
     // the list's gradient and the loss first: what they are made of need not be held beside the row
     if (valid(id0)) {
