@@ -755,6 +755,7 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& p, const DistillP
 // off: the sums are 2^off times those of exponents relative to the maximum
 __device__ float row_loss(const DistillPart& st, const RowGrad& r, float off = 0.0f) {
   if (r.empty) return 0.0f;
+  if (r.s_all != r.s_all) return r.s_all;        // a NaN or +infinity in the row, also where the teacher gives no probability to anything
   double loss = st.l + (st.p != 0.0 ? st.p * (log_of(r.s_sum) - (double)off * 0.69314718055994530942) : 0.0);
   if (r.rest != 0.0) loss += r.rest * (log_of(r.rest * r.s_sum / (double)st.s_out) + r.gap);
   return (float)loss;
