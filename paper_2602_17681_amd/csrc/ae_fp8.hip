@@ -74,6 +74,7 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
 constexpr int QT_STRIDE = BLK / 4 + 1;    // words of a transposed row in LDS: eight rows on, as far as neighbouring lanes write, are 8 banks on
 struct QuantizeArgs {
   int rows, cols, tiles_c;
+  int first;                              // the launch's first workgroup (row blocks alone)
   uint8_t* q;
   int64_t ldq;
   float* scale;
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const T* __restrict__ x, i
 // also few rows make many workgroups.
 template <typename T, int R>
 __global__ __launch_bounds__(256) void k_fp8_quantize_rows(const T* __restrict__ x, int64_t ldx, QuantizeArgs p) {
-  const int rt = blockIdx.x / p.tiles_c, tc = blockIdx.x - rt * p.tiles_c;
+  const int at = p.first + (int)blockIdx.x, rt = at / p.tiles_c, tc = at - rt * p.tiles_c;
   const int row = rt * 16 * R + (threadIdx.x >> 4), cg = threadIdx.x & 15, col = tc * BLK + cg * 8;
   float v[R][8], m[R];
 #pragma unroll
@@ -402,11 +403,11 @@ template <typename T, bool X, bool BROWS, int MT, int NT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_fp8_few(const void* __restrict__ a, int64_t lda, const float* __restrict__ sa,
                                                         const uint8_t* __restrict__ b, int64_t ldb, const float* __restrict__ sb,
                                                         const float* __restrict__ bias, int m, int n, int k, T* __restrict__ y,
-                                                        int64_t ldy, int tiles_n) {
+                                                        int64_t ldy, int tiles_n, int first) {
   constexpr bool EXACT = sizeof(T) == 4;
   constexpr int UNROLL = MT * NT >= 4 ? 2 : 4;
   __shared__ __align__(16) float red[WAVES][MT * NT][64][4];
-  const int tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
+  const int tile = first + (int)blockIdx.x, tm = tile / tiles_n, tn = tile - tm * tiles_n;
   const int m0 = tm * 16 * MT, n0 = tn * 16 * NT;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -564,7 +565,7 @@ template <typename T, bool BROWS, int WGM, int WGN, int MI, int NJ, int KG>
 __global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t* __restrict__ a, int64_t lda, const float* __restrict__ sa,
                                                              const uint8_t* __restrict__ b, int64_t ldb, const float* __restrict__ sb,
                                                              const float* __restrict__ bias, int m, int n, int k, T* __restrict__ y,
-                                                             int64_t ldy, int tiles_m, int tiles_n) {
+                                                             int64_t ldy, int tiles_m, int tiles_n, int first_tile) {
   constexpr bool EXACT = sizeof(T) == 4;
   constexpr int NTH = WGM * WGN * 64, NWV = WGM * WGN;         // threads and wavefronts of a group
   constexpr int BM = WGM * MI * 16, BN = WGN * NJ * 16;
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t*
   const int t = threadIdx.x - kg * NTH, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WGN, wn = wave - wm * WGN;
   int tm, tn;
-  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  tile_of(first_tile + (int)blockIdx.x, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const int kb = (k + BLK - 1) / BLK;
   const int per = (kb + KG - 1) / KG, first = kg * per;        // blocks of K of a group; behind the last one they are zeros
@@ -882,8 +883,12 @@ int launch_tile(const Product& p, hipStream_t s) {
   constexpr int BM = WGM * MI * 16, BN = WGN * NJ * 16;
   const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
   if (tm * tn > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
-  hipLaunchKernelGGL((k_fp8_tile<T, BROWS, WGM, WGN, MI, NJ, KG>), dim3((unsigned)(tm * tn)), dim3(WGM * WGN * KG * 64), 0, s, (const uint8_t*)p.a, p.lda, p.sa, p.b, p.ldb,
-                     p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tm, (int)tn);
+  const int64_t most = launch_blocks(WGM * WGN * KG * 64);
+  for (int64_t first = 0; first < tm * tn; first += most) {
+    const int64_t left = tm * tn - first;
+    hipLaunchKernelGGL((k_fp8_tile<T, BROWS, WGM, WGN, MI, NJ, KG>), dim3((unsigned)(left < most ? left : most)), dim3(WGM * WGN * KG * 64), 0, s, (const uint8_t*)p.a, p.lda,
+                       p.sa, p.b, p.ldb, p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tm, (int)tn, (int)first);
+  }
   return launch_status("fp8_matmul");
 }
 // The largest tiles that still leave no compute unit idle, by the number of tiles (256 compute units; times with the quantiser):
@@ -912,8 +917,12 @@ template <typename T, bool X, bool BROWS, int MT, int NT, int WAVES>
 int launch_few(const Product& p, hipStream_t s) {
   const int64_t tm = (p.m + 16 * MT - 1) / (16 * MT), tn = (p.n + 16 * NT - 1) / (16 * NT);
   if (tm * tn > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_matmul: result too large");
-  hipLaunchKernelGGL((k_fp8_few<T, X, BROWS, MT, NT, WAVES>), dim3((unsigned)(tm * tn)), dim3(WAVES * 64), 0, s, (const void*)p.a, p.lda, p.sa, p.b, p.ldb,
-                     p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tn);
+  const int64_t most = launch_blocks(WAVES * 64);
+  for (int64_t first = 0; first < tm * tn; first += most) {
+    const int64_t left = tm * tn - first;
+    hipLaunchKernelGGL((k_fp8_few<T, X, BROWS, MT, NT, WAVES>), dim3((unsigned)(left < most ? left : most)), dim3(WAVES * 64), 0, s, (const void*)p.a, p.lda, p.sa, p.b,
+                       p.ldb, p.sb, p.bias, (int)p.m, (int)p.n, (int)p.k, (T*)p.y, p.ldy, (int)tn, (int)first);
+  }
   return launch_status("fp8_matmul");
 }
 // x quantised on the way: every workgroup reads and quantises all of x, so it takes as many columns as leave 256 workgroups
@@ -943,8 +952,10 @@ int launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
                     int64_t ldqt, float* scale_t, hipStream_t s) {
   const int64_t tr = (rows + BLK - 1) / BLK, tc = (cols + BLK - 1) / BLK;
   constexpr int QROWS = 2;                       // 16 384 x 4 096 in bfloat16: 37 us, 5.4 TB/s (one 38, four 45; 128 x 128 tiles 46)
-  if (tr * tc * 8 > 0x7FFFFFFF) return fail(AE_EINVAL, "model_fp8_quantize: matrix too large");
-  const QuantizeArgs p = {(int)rows, (int)cols, (int)tc, (uint8_t*)q, ldq, scale, (uint8_t*)qt, ldqt, scale_t};
+  const int64_t row_blocks = (rows + 16 * QROWS - 1) / (16 * QROWS) * tc, most = launch_blocks(256);
+  const bool rows_alone = blocks == AE_FP8_ROWS && !qt;
+  if (rows_alone ? row_blocks > 0x7FFFFFFF : tr * tc > most) return fail(AE_EINVAL, "model_fp8_quantize: matrix too large");      // over 288 GB in any case
+  QuantizeArgs p = {(int)rows, (int)cols, (int)tc, 0, (uint8_t*)q, ldq, scale, (uint8_t*)qt, ldqt, scale_t};
 #define QUANT(TI, A, B)                                                                                                         \
   hipLaunchKernelGGL((k_fp8_quantize<T, TI, A, B>), dim3((unsigned)(tr * tc)), dim3(256), 0, s, (const T*)x, ldx, p)
   if (blocks == AE_FP8_TILES) {
@@ -953,8 +964,13 @@ int launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
     else QUANT(true, false, true);
   } else {
     if (q && qt) QUANT(false, true, true);
-    else if (q) hipLaunchKernelGGL((k_fp8_quantize_rows<T, QROWS>), dim3((unsigned)((rows + 16 * QROWS - 1) / (16 * QROWS) * tc)), dim3(256), 0, s, (const T*)x, ldx, p);
-    else QUANT(false, false, true);
+    else if (qt) QUANT(false, false, true);
+    else
+      for (int64_t first = 0; first < row_blocks; first += most) {
+        const int64_t left = row_blocks - first;
+        p.first = (int)first;
+        hipLaunchKernelGGL((k_fp8_quantize_rows<T, QROWS>), dim3((unsigned)(left < most ? left : most)), dim3(256), 0, s, (const T*)x, ldx, p);
+      }
   }
 #undef QUANT
   return launch_status("fp8_quantize");

@@ -33,6 +33,10 @@ inline int launch_status(const char* what) {
   return AE_OK;
 }
 
+// Workgroups that one launch takes: the runtime counts its threads in 32 bits, and launches what is left of a larger number
+// without an error.
+inline int64_t launch_blocks(int threads) { return 0xFFFFFFFFll / threads; }
+
 inline size_t dtype_size(int dtype) { return dtype == AE_BF16 ? 2 : 4; }
 // channel count rounded up to whole 16-byte chunks
 inline int chan_pad(int c, int dtype) {

@@ -356,7 +356,7 @@ struct ListKeys {
 
 struct LogprobArgs {
   const void* logits;
-  int64_t rows, ld;
+  int64_t row0, rows, ld;                // the launch's first row
   int vocab, splits, chunk;              // columns of a piece
   float temp;
   const int* tokens;
@@ -406,8 +406,9 @@ __global__ __launch_bounds__(NT, 6) void k_logprob(LogprobArgs p) {
   constexpr int V = Store<T>::VEC, STEP = NT * V;
   __shared__ Stats sm[NW];
   __shared__ TopShared sh;
-  const int64_t row = blockIdx.x / p.splits;
-  const int split = (int)(blockIdx.x - row * p.splits), t = threadIdx.x;
+  const unsigned at_row = blockIdx.x / p.splits;
+  const int64_t row = p.row0 + at_row;
+  const int split = (int)(blockIdx.x - at_row * p.splits), t = threadIdx.x;
   const int c0 = split * p.chunk;
   const int n = p.vocab - c0 < p.chunk ? p.vocab - c0 : p.chunk;
   const T* z = (const T*)p.logits + row * p.ld + c0;
@@ -577,7 +578,7 @@ __device__ __forceinline__ void add_logit(float& m, float& s, float z, float c2)
 constexpr double kFarthest = 708.0;
 struct DistillArgs {
   const void* logits;
-  int64_t rows, ld;
+  int64_t row0, rows, ld;                // the launch's first row
   int vocab, splits, chunk;
   float temp;
   const int* top_id;
@@ -849,8 +850,9 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
   extern __shared__ uint32_t bits[];
   __shared__ float smf[4][NW];
   __shared__ double smp[2][NW], smd[NW + 1];
-  const int64_t row = blockIdx.x / p.splits;
-  const int split = (int)(blockIdx.x - row * p.splits);
+  const unsigned at_row = blockIdx.x / p.splits;
+  const int64_t row = p.row0 + at_row;
+  const int split = (int)(blockIdx.x - at_row * p.splits);
   const int c0 = split * p.chunk;
   const int n = p.vocab - c0 < p.chunk ? p.vocab - c0 : p.chunk;
   const float w = p.weight ? p.weight[row] : 1.0f;
@@ -1152,7 +1154,7 @@ int launch_distill_row(const DistillArgs& p, size_t lds, hipStream_t s) {
   // 16 vectors: workgroups that stay, as many as the registers of 256 compute units hold (128 to a thread).  Fewer: a row
   // each, since more of them run at a time (4 096 x 32 000 in bfloat16 124 us, with staying ones 145; 8 192 x 131 072 1 007, a
   // row each 1 071; 4 096 x 50 021 230 and 243)
-  const int64_t stay = NV == 16 ? 256 * (1024 / NTH) : p.rows;
+  const int64_t stay = NV == 16 ? 256 * (1024 / NTH) : launch_blocks(NTH);
   hipLaunchKernelGGL((k_distill_row<T, NTH, NV>), dim3((unsigned)(p.rows < stay ? p.rows : stay)), dim3(NTH), lds, s, p);
   return launch_status("loss_distill");
 }
@@ -1166,7 +1168,11 @@ int launch_distill_rows(const DistillArgs& p, size_t lds, hipStream_t s) {
     if (vecs <= 512 * 16) return launch_distill_row<T, 512, 16>(p, lds, s);
     if (vecs <= 1024 * 16) return launch_distill_row<T, 1024, 16>(p, lds, s);
   }
-  hipLaunchKernelGGL((k_distill<T, 0>), dim3((unsigned)p.rows), dim3(NT), lds, s, p);
+  DistillArgs q = p;
+  for (; q.row0 < p.rows; q.row0 += launch_blocks(NT)) {
+    const int64_t left = p.rows - q.row0, most = launch_blocks(NT);
+    hipLaunchKernelGGL((k_distill<T, 0>), dim3((unsigned)(left < most ? left : most)), dim3(NT), lds, s, q);
+  }
   return launch_status("loss_distill");
 }
 template <typename T>
@@ -1248,15 +1254,17 @@ extern "C" int model_token_logprobs(const void* logits, int64_t rows, int64_t vo
   p.part_top = (uint64_t*)((char*)workspace + align16(rows * p.splits * (int64_t)sizeof(Stats)));
   const bool top = top_k > 0 && (top_id || top_logit || top_logprob);
   hipStream_t s = (hipStream_t)stream;
-  const dim3 grid((unsigned)(rows * p.splits)), grid_j((unsigned)rows);
+  // rows in pieces are few: one launch takes them all
+  const int64_t most = p.splits > 1 ? rows : launch_blocks(NT);
 #define LOGPROB(T, TOP)                                                        \
-  do {                                                                         \
+  for (; p.row0 < rows; p.row0 += most) {                                      \
+    const dim3 grid((unsigned)((rows - p.row0 < most ? rows - p.row0 : most) * p.splits));    \
     if (entropy) hipLaunchKernelGGL((k_logprob<T, TOP, true>), grid, dim3(NT), 0, s, p);      \
     else hipLaunchKernelGGL((k_logprob<T, TOP, false>), grid, dim3(NT), 0, s, p);             \
-    if (p.splits > 1) hipLaunchKernelGGL((k_logprob_join<T, TOP>), grid_j, dim3(NT), 0, s, p); \
-  } while (0)
-  if (dtype == AE_BF16) { if (top) LOGPROB(bf16_t, true); else LOGPROB(bf16_t, false); }
-  else { if (top) LOGPROB(float, true); else LOGPROB(float, false); }
+    if (p.splits > 1) hipLaunchKernelGGL((k_logprob_join<T, TOP>), dim3((unsigned)rows), dim3(NT), 0, s, p); \
+  }
+  if (dtype == AE_BF16) { if (top) LOGPROB(bf16_t, true) else LOGPROB(bf16_t, false) }
+  else { if (top) LOGPROB(float, true) else LOGPROB(float, false) }
 #undef LOGPROB
   return launch_status("token_logprobs");
 }
