@@ -404,14 +404,18 @@ int model_fold_embedding(const void* e, int64_t vocab, int64_t d, const void* a,
  *
  * model_fp8_quantize  quantises x [rows][cols] (dtype, row stride ldx elements, any alignment of the elements' own):
  *     scale = max(amax / 448, 2^-126), amax the largest finite magnitude of the block,
- *     code  = E4M3(x * (1 / scale)), rounded to nearest even, magnitudes over 448 (infinities too) to 448, NaN to NaN;
+ *     code  = E4M3(x * (1 / scale)), rounded to nearest even, magnitudes over 448 (infinities too) to 448, NaN to NaN (the
+ *   specification's saturating conversion: an infinity, such as an overflowed gradient, is a finite number from here on; who wants
+ *   to know of it looks at x);
  *   quotient, reciprocal and product are correctly rounded binary32 operations, so codes and scales are reproducible.
  *   q [rows][cols], scale: the codes of x (both nullable together).  qt [cols][rows], scale_t: the codes of the
  *   transposed matrix (both nullable together): for AE_FP8_ROWS its own blocks of 128 along the rows of x, for
  *   AE_FP8_TILES the same codes and scales transposed.  Both orientations take one pass over x.
  * model_fp8_matmul    y[i][j] = bias[j] + sum over blocks c of a_scale[c][i] * b_scale[c; j] * sum over k in c of a[i][k] * b[j][k]:
  *   a [m][k] in AE_FP8_ROWS, b [n][k] in either form (b_blocks), so that y = a b^T; bias binary32 [n], nullable; y [m][n]
- *   in dtype, row stride ldy elements.  a_scale * b_scale is one binary32 product; the blocks are added up in binary32 and
+ *   in dtype, row stride ldy elements.  a_scale * b_scale is one binary32 product, with that type's range: beyond 2^128 it is
+ *   infinite (and NaN with a block sum of 0), and digits or all of it are lost below 2^-126; the quantiser's scales are magnitudes
+ *   / 448, so that is for factors whose product binary32 hardly holds.  The blocks are added up in binary32 and
  *   rounded to dtype once.  The sum over a block: for binary32 y the codes are multiplied as bfloat16, which holds them
  *   exactly, and added in binary32 (an error of about 2^-23 of the block's largest sums); for bfloat16 y the 8-bit matrix
  *   instruction multiplies them at twice the rate and keeps, of each eight neighbouring products, 14 bits below the largest
