@@ -521,9 +521,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_fp8_few(const void* __restrict__
 //   pieces g and g + 4 (any order of K will do, as long as it is b's too): 5.8 cycles a read, as for consecutive addresses;
 //   pieces 2 g and 2 g + 1 take 8.0
 // Bound by the matrix cores and by what of a tile's first load and last store nothing runs beside (one workgroup of
-// 256 x 256 fills a compute unit): 16 384 x 4 096 x 4 096 in bfloat16 250 us, 2 200 TFLOP/s; 4 096 x 4 096 x 4 096 62.
+// 256 x 256 fills a compute unit): 16 384 x 4 096 x 4 096 in bfloat16 247 - 268 us by box and operands, 2.05 - 2.2 PFLOP/s (under
+// the profiler 251 at least, 281 in the mean); 4 096 x 4 096 x 4 096 63.  b in row blocks, 256 x 128 tiles: 355 and 84.
 // Binary32 results: by turning codes into bfloat16 (an instruction of half rate for two codes, 16 times a fragment) beside
-// the bfloat16 products: 4 096 x 4 096 x 4 096 140 us, 980 TFLOP/s, b in row blocks 156.
+// the bfloat16 products: 4 096 x 4 096 x 4 096 145 us, 950 TFLOP/s, b in row blocks 153 (alone; after the other launches of a
+// backward pass, under the profiler, 164 - 178).
 template <int NJ> __device__ __forceinline__ int b_row(int i, int j) { return (i >> 2) * (4 * NJ) + j * 4 + (i & 3); }   // row of b in fragment j, place i
 __device__ __forceinline__ int a_key(int r) { return (r >> 1) & 7; }
 template <int NJ> __device__ __forceinline__ int b_key(int r) { return ((r / (4 * NJ)) & 3) << 1 | ((r >> 1) & 1); }
@@ -691,7 +693,7 @@ __global__ __launch_bounds__(WGM * WGN * KG * 64) void k_fp8_tile(const uint8_t*
   // Binary32 results: the next fragment of a is turned into bfloat16 a quarter at a time beside the products of the present
   // one (fn), a fragment of b before the first product that takes it (LATE_B).  All where a step begins they took 551 us at
   // 16 384 x 4 096 x 4 096, so 522, and held registers for longer (1 000 x 1 000 x 1 024, b in row blocks, 13.2 and 10.1).  Only
-  // 256 x 128 tiles with b in row blocks gain nothing (4 096 x 4 096 x 4 096 167 and, late, 169).
+  // 256 x 128 tiles with b in row blocks gain nothing (in a backward pass of 4 096 x 4 096 x 4 096 167 and, late, 169).
   constexpr bool LATE_B = EXACT && !(BROWS && NWV == 8);
   Frag<EXACT> fb[NJ], fn;
   v4f cs[NJ];
@@ -897,7 +899,11 @@ int launch_tile(const Product& p, hipStream_t s) {
 //   up to 256 of 128 x 128   two groups of K     777 x 4 096 x 4 096 36 us (one 44; 64 x 64 39; 256 x 256 57)
 //   more                     one group, two workgroups to a compute unit    1 500 x 4 096 x 4 096 49 us (256 x 256 59; 64 x 64 63)
 //   from 192 of 256 x 256    1 500 x 8 192 x 2 048 41 us (128 x 128 48).  Binary32 results and b in row blocks need more registers:
-//                            256 x 128, and only where it is a whole round or many (1 500 x 4 096 x 4 096 78 us, 128 x 128 83; 1 500 x 8 192 x 2 048 88, 78)
+//                            256 x 128, and only where it is a whole round or many (1 500 x 4 096 x 4 096 78 us, 128 x 128 83; 1 500 x 8 192 x 2 048 88, 78).
+// Products alone at K = 2 048, in us.  bfloat16, b in tiles, by the number of 256 x 256 tiles: 128 29 (128 x 128: 25), 176 31 (38), 208 32 (45),
+// 272 59 (58), 512 69 (89).  By the number of 256 x 128 tiles, binary32 with b in tiles / in rows, bfloat16 with b in rows:
+//   160 39 / 44 / 23 (128 x 128: 42 / 46 / 23)   320 76 / 82 / 44 (66 / 70 / 37)    416 82 / 87 / 45 (82 / 85 / 45)   480 86 / 92 / 47 (86 / 89 / 47)
+//   576 116 / 124 / 66 (104 / 107 / 58)          768 128 / 136 / 70 (128 / 133 / 71)   896 160 / 172 / 88 (148 / 153 / 81)   1 024 165 / 178 / 93 (168 / 172 / 93)
 template <typename T, bool BROWS>
 int launch_tiles(const Product& p, hipStream_t s) {
   auto tiles = [&](int64_t bm, int64_t bn) { return ((p.m + bm - 1) / bm) * ((p.n + bn - 1) / bn); };

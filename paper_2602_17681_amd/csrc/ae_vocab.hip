@@ -886,7 +886,7 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs p) {
 // Whole rows that fit the registers: a workgroup of NTH threads holds a row, NV vectors to a thread, so that it is read
 // once: 16 vectors in 1 024 threads are 256 KiB, half of a compute unit's registers.  As no more than one or a few
 // workgroups then fit a compute unit, they stay, and ask for a vector of their next row as soon as the gradient of the
-// present one's is stored.  Bound by memory: 8 192 x 131 072 in bfloat16 1 007 us, 4.3 TB/s read and written (a copy: 4.9),
+// present one's is stored.  Bound by memory: 8 192 x 131 072 in bfloat16 1 010 us, 4.25 TB/s read and written (a copy: 4.9),
 // the difference being barriers that nothing is loaded beside.  A thread also holds its entry of the list, which is no
 // longer than there are threads.
 template <typename T, int NTH, int NV>
@@ -1152,7 +1152,7 @@ __global__ __launch_bounds__(NT) void k_distill_total(const float* __restrict__ 
 template <typename T, int NTH, int NV>
 int launch_distill_row(const DistillArgs& p, size_t lds, hipStream_t s) {
   // 16 vectors: workgroups that stay, as many as the registers of 256 compute units hold (128 to a thread).  Fewer: a row
-  // each, since more of them run at a time (4 096 x 32 000 in bfloat16 124 us, with staying ones 145; 8 192 x 131 072 1 007, a
+  // each, since more of them run at a time (4 096 x 32 000 in bfloat16 124 us, with staying ones 145; 8 192 x 131 072 1 010, a
   // row each 1 071; 4 096 x 50 021 230 and 243)
   const int64_t stay = NV == 16 ? 256 * (1024 / NTH) : launch_blocks(NTH);
   hipLaunchKernelGGL((k_distill_row<T, NTH, NV>), dim3((unsigned)(p.rows < stay ? p.rows : stay)), dim3(NTH), lds, s, p);
@@ -1196,7 +1196,8 @@ void cut_rows(int64_t rows, int64_t vocab, bool cut, int* splits, int* chunk) {
 // log probabilities with a list of 20, 4 rows: 131 072 bfloat16 columns 16 us in pieces, 20 whole; 65 536 17 and 13; 50 021 binary32
 // 15 and 13; 100 rows of 131 072 24 and 20
 void cut_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 65536, splits, chunk); }
-// room for the pieces of rows is asked for from 32 769 columns on, so that the rule above is not the callers' concern
+// The room that is asked for: from 32 769 columns on, as when rows were cut from there on.  Up to 65 536 no launch uses it; the
+// query's answer, and that the call refuses less, stay as they were (4 rows of 65 536 with a list of 20: 11 KB).
 void room_logprob(int64_t rows, int64_t vocab, int* splits, int* chunk) { cut_rows(rows, vocab, rows < 64 && vocab > 32768, splits, chunk); }
 // distillation: 64 rows of 131 072 17 us in pieces, 28 whole; 100 of 50 021 16 and 19, 130 23 and 20; 4 rows
 // of 32 768 in binary32 with the sum 11 and 14, of 17 000 11 and 9; 8 000 columns 10 and 8.  Rows that fill a compute
