@@ -443,7 +443,7 @@ int model_fp8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, con
  * of -infinity are outcomes that cannot occur.  A row in which all are is empty: its lse and log probabilities are
  * -infinity, its entropy, loss and gradient zero.  A row that holds a NaN or +infinity gives NaN for its own results only.
  * All sums are binary32 or wider; a row's results do not depend on what the other rows hold (their number decides how rows
- * are divided among workgroups, and so last bits).  The same call gives the same bits.  1 <= vocab <= 2^20.
+ * are divided among workgroups, and so last bits).  The same call gives the same bits.  At most 2^24 rows, 1 <= vocab <= 2^20.
  *
  * model_token_logprobs  for every row
  *   logprob [rows][n_tokens]: log q of the given tokens [rows][n_tokens] (int32); an index outside 0 .. vocab - 1 marks a
