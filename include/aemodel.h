@@ -476,6 +476,67 @@ int model_loss_distill(const void* logits, int64_t rows, int64_t vocab, int64_t 
                        const int* top_id, const float* top_logit, int top_k, const float* teacher_lse, const float* weight,
                        float* loss_rows, float* loss, void* d_logits, int64_t ldd, void* workspace, void* stream);
 
+/* ---- from tokens to an 8-bit output layer, and from its gradient to the optimiser ----------------------------------
+ * Matrices have rows of contiguous elements in dtype with a row stride in elements (no alignment beyond the element's own)
+ * and do not overlap each other, except where an output may take an input's place.
+ *
+ * model_rms_norm  for every row of x [rows][d] and residual [rows][d] (nullable: none)
+ *     h = x + residual,   y_j = h_j * weight_j / sqrt(mean_k h_k^2 + eps)
+ *   in binary32 from the sum on (y is that of the sum, not of its rounding); weight binary32 [d], nullable (ones); eps a
+ *   positive normal number.  Outputs, each nullable, one at least: h and y in dtype, rounded once; q with scale: y in E4M3
+ *   codes, AE_FP8_ROWS (what model_fp8_matmul takes as a; codes and scales of model_fp8_quantize applied to the binary32
+ *   y).  h, or y where h is null, may be x or residual itself, with the same stride.  A row that holds an infinity gives NaN there and 0
+ *   elsewhere, one that holds a NaN gives NaN; other rows are not affected.  1 <= d <= 2^20, rows up to 2^31 - 513.
+ * model_rms_norm_backward  from dy [rows][d] and the sum h [rows][d] that model_rms_norm wrote (or x, without residual), with
+ *   r = 1 / sqrt(mean h^2 + eps), u = h r, g = dy weight:
+ *     dx = d_h + r (g - u mean(g u)),   d_weight_j = sum over the rows of dy_j u_j
+ *   d_h [rows][d] (nullable): the gradient that reaches h on the residual path; dx is the gradient of x and of residual
+ *   alike, it may be dy, h or d_h itself with the same stride.  dx or d_weight may be null.  Sums are binary32 in an order that depends on the sizes alone.
+ *
+ * model_embedding  out[i] = scale * table[ids[i]] (n rows of d, rounded once); ids int32, an id outside 0 .. vocab - 1 gives zeros.
+ * model_embedding_backward  d_table[v] = scale * (sum of d_out[i] over all i with ids[i] = v, added in binary32 in an order
+ *   that depends on ids alone), binary32 [vocab][d] with row stride ldt.  accumulate = 0: every row is written, zeros where no
+ *   id is v; otherwise the sum is added to what is there, and rows without an id are left alone (a table that is the
+ *   output layer's weight, too, has that layer's weight gradient there).  ids outside 0 .. vocab - 1 have no part.
+ *   vocab and d up to 2^20, n up to 2^30.
+ *
+ * model_grad_clip  grads: `count` device tensors of sizes[k] elements in dtypes[k]; the four arrays are HOST memory and
+ *   read during the call (a captured call keeps the addresses in it).
+ *     *norm = sqrt(sum of all squares)  (binary32, device, nullable; squares are added up in binary64)
+ *     out[k] = grads[k] * min(1, max_norm / norm), rounded once
+ *   out null: the norm alone.  out[k] = grads[k] clips in place, and writes nothing if norm <= max_norm.  Where the norm is
+ *   infinite or NaN nothing is scaled: out has the gradients as they are.  max_norm > 0 (infinity: never clip).  No output may overlap another, or
+ *   another's gradient.  Tensors of size 0 may be null.
+ *
+ * model_logits_adjust  for every row of logits z [rows][vocab], in this order and in binary32, rounded once:
+ *     1. tokens of history [rows][n_history] (int32; outside 0 .. vocab - 1: no token):  z = z > 0 ? z / repetition : z * repetition
+ *     2. of those, the ones that occur c > 0 times behind the row's first n_prompt[row] places:  z = z - frequency * c - presence
+ *     3. tokens of bias_id [rows][n_bias] (int32, as above; of a token listed twice the last entry counts):  z = z + bias
+ *     4. tokens whose bit j % 32 in word j / 32 of the row's ceil(vocab / 32) words of allowed is 0:  z = -infinity
+ *   n_prompt int32 [rows] (nullable: 0); repetition, presence, frequency binary32 [rows] (nullable: 1, 0, 0); bias
+ *   [rows][n_bias]; allowed nullable (all).  n_history up to 2^20 - 1, n_bias up to 2 047, rows up to 2^24, vocab up to 2^20.
+ *   out [rows][vocab] in dtype may be logits itself with the same stride.  The rows are what model_token_logprobs takes.
+ * workspace: the matching _workspace bytes (a call without such a query has none), 16-byte aligned; its contents need not be kept. */
+int model_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, int64_t rows, int64_t d,
+                   float eps, int dtype, void* h, int64_t ldh, void* y, int64_t ldy, void* q, int64_t ldq, float* scale,
+                   void* stream);
+int model_rms_norm_backward_workspace(int64_t rows, int64_t d, int dtype, int64_t* bytes);
+int model_rms_norm_backward(const void* dy, int64_t ldy, const void* h, int64_t ldh, const float* weight, const void* d_h,
+                            int64_t ldg, int64_t rows, int64_t d, float eps, int dtype, void* dx, int64_t lddx,
+                            float* d_weight, void* workspace, void* stream);
+int model_embedding(const void* table, int64_t ldt, int64_t vocab, int64_t d, const int* ids, int64_t n, float scale, int dtype,
+                    void* out, int64_t ldo, void* stream);
+int model_embedding_backward_workspace(int64_t n, int64_t vocab, int64_t d, int dtype, int64_t* bytes);
+int model_embedding_backward(const void* d_out, int64_t ldo, const int* ids, int64_t n, int64_t vocab, int64_t d, float scale,
+                             int dtype, float* d_table, int64_t ldt, int accumulate, void* workspace, void* stream);
+int model_grad_clip_workspace(const int64_t* sizes, int count, int64_t* bytes);
+int model_grad_clip(void* const* grads, const int64_t* sizes, const int* dtypes, int count, float max_norm, float* norm,
+                    void* const* out, void* workspace, void* stream);
+int model_logits_adjust(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int* history,
+                        int64_t n_history, const int* n_prompt, const float* repetition, const float* presence,
+                        const float* frequency, const int* bias_id, const float* bias, int n_bias, const uint32_t* allowed,
+                        void* out, int64_t ldo, void* stream);
+
 /* Measurement aid: TFLOP/s of a loop of nothing but independent 32x32x16 bf16 matrix-core
  * instructions on every compute unit (two workgroups of four wavefronts each, two wavefronts per
  * SIMD), the practical ceiling beside the nominal peak; with lds_reads = 6 each wavefront also reads

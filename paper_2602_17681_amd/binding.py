@@ -24,7 +24,7 @@ SYMBOLS = [
     "model_set_sample_offset", "model_forward", "model_backward", "model_loss_mse", "model_noise",
     "model_pnorm_awgn", "model_gen_bits", "model_count_errors", "model_monte_carlo", "model_num_steps", "model_step_info",
     "model_get_activation", "model_get_conv_output", "model_timing_enable", "model_set_overlap", "model_set_params_static", "model_set_inference", "model_set_recompute", "model_set_fused_backward", "model_calibrate_mfma", "model_mx_quantize", "model_mx_quantize_elem", "model_transform_mse_workspace",
-    "model_transform_mse", "model_transform_mse_elem", "model_transform_mse_static", "model_inverse_shift", "model_lu_workspace", "model_lu_compose", "model_lu_backward", "model_vol_penalty", "model_lu_inverse_workspace", "model_lu_inverse", "model_lu_compose_batch", "model_lu_backward_batch", "model_lu_inverse_batch", "model_lu_timing", "model_qr_workspace", "model_qr_squarings", "model_qr_compose", "model_qr_backward", "model_qr_inverse", "model_fold_workspace", "model_fold_linear", "model_fold_embedding", "model_fp8_quantize", "model_fp8_matmul_workspace", "model_fp8_matmul", "model_fp8_linear_workspace", "model_fp8_linear", "model_token_logprobs_workspace", "model_token_logprobs", "model_loss_distill_workspace", "model_loss_distill", "model_timing_slots",
+    "model_transform_mse", "model_transform_mse_elem", "model_transform_mse_static", "model_inverse_shift", "model_lu_workspace", "model_lu_compose", "model_lu_backward", "model_vol_penalty", "model_lu_inverse_workspace", "model_lu_inverse", "model_lu_compose_batch", "model_lu_backward_batch", "model_lu_inverse_batch", "model_lu_timing", "model_qr_workspace", "model_qr_squarings", "model_qr_compose", "model_qr_backward", "model_qr_inverse", "model_fold_workspace", "model_fold_linear", "model_fold_embedding", "model_fp8_quantize", "model_fp8_matmul_workspace", "model_fp8_matmul", "model_fp8_linear_workspace", "model_fp8_linear", "model_token_logprobs_workspace", "model_token_logprobs", "model_loss_distill_workspace", "model_loss_distill", "model_rms_norm", "model_rms_norm_backward_workspace", "model_rms_norm_backward", "model_embedding", "model_embedding_backward_workspace", "model_embedding_backward", "model_grad_clip_workspace", "model_grad_clip", "model_logits_adjust", "model_timing_slots",
     "model_timing_read", "model_timing_reset", "model_last_error",
 ]
 
@@ -102,6 +102,16 @@ def _load():
     L.model_token_logprobs.argtypes = [vp, i64, i64, i64, C.c_int, C.c_float, vp, C.c_int, C.c_int, vp, vp, vp, vp, vp, vp, vp, vp]
     L.model_loss_distill_workspace.argtypes = [i64, i64, C.c_int, i64p]
     L.model_loss_distill.argtypes = [vp, i64, i64, i64, C.c_int, C.c_float, vp, vp, C.c_int, vp, vp, vp, vp, vp, i64, vp, vp]
+    f32 = C.c_float
+    L.model_rms_norm.argtypes = [vp, i64, vp, i64, vp, i64, i64, f32, C.c_int, vp, i64, vp, i64, vp, i64, vp, vp]
+    L.model_rms_norm_backward_workspace.argtypes = [i64, i64, C.c_int, i64p]
+    L.model_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, C.c_int, vp, i64, vp, vp, vp]
+    L.model_embedding.argtypes = [vp, i64, i64, i64, vp, i64, f32, C.c_int, vp, i64, vp]
+    L.model_embedding_backward_workspace.argtypes = [i64, i64, i64, C.c_int, i64p]
+    L.model_embedding_backward.argtypes = [vp, i64, vp, i64, i64, i64, f32, C.c_int, vp, i64, C.c_int, vp, vp]
+    L.model_grad_clip_workspace.argtypes = [vp, C.c_int, i64p]
+    L.model_grad_clip.argtypes = [vp, vp, vp, C.c_int, f32, vp, vp, vp, vp]
+    L.model_logits_adjust.argtypes = [vp, i64, i64, i64, C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, C.c_int, vp, vp, i64, vp]
     L.model_timing_slots.argtypes = [vp, C.POINTER(C.c_int)]
     L.model_timing_read.argtypes = [vp, C.c_int, C.c_char_p, C.c_int, C.POINTER(C.c_double), i64p,
                                     C.POINTER(C.c_double), C.POINTER(C.c_double)]
@@ -612,6 +622,104 @@ def model_loss_distill(logits, rows, vocab, top_id, top_logit, loss_rows, loss, 
     _check(lib.model_loss_distill(zp, rows, vocab, ld, dtype, temperature, _vec(top_id, rows * top_k, torch.int32), _vec(top_logit, rows * top_k),
                                   top_k, _vec(teacher_lse, rows), _vec(weight, rows), _vec(loss_rows, rows), _vec(loss, 1), gp, ldd,
                                   _room(workspace, model_loss_distill_workspace(rows, vocab, dtype)), _raw_stream()))
+
+
+def model_rms_norm(x, rows, d, weight, eps, h=None, y=None, q=None, scale=None, residual=None):
+    """h = x + residual; y = h / sqrt(mean h^2 + eps) * weight in x's type and / or as codes q with row blocks' scales (each output may be None)."""
+    xp, ldx = _mat(x, rows, d)
+    rp, ldr = _mat(residual, rows, d, x.dtype)
+    hp, ldh = _mat(h, rows, d, x.dtype)
+    yp, ldy = _mat(y, rows, d, x.dtype)
+    qp, ldq = _codes(q, rows, d)
+    _check(lib.model_rms_norm(xp, ldx, rp, ldr, _vec(weight, d), rows, d, eps, _dtype_of(x), hp, ldh, yp, ldy, qp, ldq,
+                              _fp8_scales(scale, rows, d, "rows"), _raw_stream()))
+
+
+@functools.lru_cache(maxsize=1024)                # by sizes alone
+def model_rms_norm_backward_workspace(rows, d, dtype):
+    b = C.c_int64()
+    _check(lib.model_rms_norm_backward_workspace(rows, d, dtype, C.byref(b)))
+    return b.value
+
+
+def model_rms_norm_backward(dy, h, rows, d, weight, eps, dx, d_weight, workspace, d_h=None):
+    """Gradients of h (d_h, what arrives there from elsewhere, added) and of the weight; dx or d_weight may be None."""
+    gp, ldy = _mat(dy, rows, d)
+    hp, ldh = _mat(h, rows, d, dy.dtype)
+    ap, lda = _mat(d_h, rows, d, dy.dtype)
+    dp, ldd = _mat(dx, rows, d, dy.dtype)
+    dtype = _dtype_of(dy)
+    _check(lib.model_rms_norm_backward(gp, ldy, hp, ldh, _vec(weight, d), ap, lda, rows, d, eps, dtype, dp, ldd, _vec(d_weight, d),
+                                       _room(workspace, model_rms_norm_backward_workspace(rows, d, dtype)), _raw_stream()))
+
+
+def model_embedding(table, vocab, d, ids, n, out, scale=1.0):
+    """out[i] = scale * table[ids[i]]; zeros for an id outside 0 .. vocab - 1."""
+    tp, ldt = _mat(table, vocab, d)
+    op, ldo = _mat(out, n, d, table.dtype)
+    _check(lib.model_embedding(tp, ldt, vocab, d, _vec(ids, n, torch.int32), n, scale, _dtype_of(table), op, ldo, _raw_stream()))
+
+
+@functools.lru_cache(maxsize=1024)                # by sizes alone
+def model_embedding_backward_workspace(n, vocab, d, dtype):
+    b = C.c_int64()
+    _check(lib.model_embedding_backward_workspace(n, vocab, d, dtype, C.byref(b)))
+    return b.value
+
+
+def model_embedding_backward(d_out, ids, n, vocab, d, d_table, workspace, scale=1.0, accumulate=False):
+    """d_table[v] = scale * sum of d_out[i] with ids[i] = v, or added to what is there."""
+    gp, ldo = _mat(d_out, n, d)
+    tp, ldt = _mat(d_table, vocab, d, torch.float32)
+    dtype = _dtype_of(d_out)
+    _check(lib.model_embedding_backward(gp, ldo, _vec(ids, n, torch.int32), n, vocab, d, scale, dtype, tp, ldt, 1 if accumulate else 0,
+                                        _room(workspace, model_embedding_backward_workspace(n, vocab, d, dtype)), _raw_stream()))
+
+
+class GradList:
+    """Gradients that are clipped together, and where the clipped ones go: `out` None leaves the gradients alone (the norm only),
+    the same list puts them in their place.  Holds the tensors; made once for buffers that a program keeps."""
+
+    def __init__(self, grads, out=None):
+        grads = list(grads)
+        out = None if out is None else list(out)
+        for g in grads + (out or []):
+            assert g.is_cuda and g.is_contiguous() and g.dtype in (torch.float32, torch.bfloat16), "contiguous device tensors in float32 or bfloat16 required"
+        assert out is None or (len(out) == len(grads) and all(o.numel() == g.numel() and o.dtype == g.dtype for o, g in zip(out, grads))), \
+            "as many outputs as gradients, of their sizes and types"
+        self.grads, self.out, n = grads, out, len(grads)
+        self._grads = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
+        self._out = None if out is None else (C.c_void_p * n)(*[o.data_ptr() for o in out])
+        self._sizes = (C.c_int64 * n)(*[g.numel() for g in grads])
+        self._dtypes = (C.c_int * n)(*[_dtype_of(g) for g in grads])
+        b = C.c_int64()
+        _check(lib.model_grad_clip_workspace(self._sizes, n, C.byref(b)))
+        self.workspace_bytes = b.value
+
+
+def model_grad_clip_workspace(grads):
+    return grads.workspace_bytes
+
+
+def model_grad_clip(grads, max_norm, norm, workspace):
+    """norm[0] = the norm of a GradList's gradients together; each times min(1, max_norm / norm) into its output (norm may be None)."""
+    _check(lib.model_grad_clip(grads._grads, grads._sizes, grads._dtypes, len(grads.grads), max_norm, _vec(norm, 1), grads._out,
+                               _room(workspace, grads.workspace_bytes), _raw_stream()))
+
+
+def model_logits_adjust(logits, rows, vocab, out, history=None, n_prompt=None, repetition=None, presence=None, frequency=None, bias_id=None, bias=None,
+                        allowed=None):
+    """Penalties for the tokens of each row's history, biases of given tokens, -infinity where `allowed` has no bit; out may be logits."""
+    zp, ld = _mat(logits, rows, vocab)
+    op, ldo = _mat(out, rows, vocab, logits.dtype)
+    assert (history is None or history.dim() == 2) and (bias_id is None or bias_id.dim() == 2), "[rows][n] lists required"
+    assert (bias_id is None) == (bias is None), "biases and their tokens go together"
+    n_history = 0 if history is None else history.shape[1]
+    n_bias = 0 if bias_id is None else bias_id.shape[1]
+    _check(lib.model_logits_adjust(zp, rows, vocab, ld, _dtype_of(logits), _vec(history, rows * n_history, torch.int32), n_history,
+                                   _vec(n_prompt, rows, torch.int32), _vec(repetition, rows), _vec(presence, rows), _vec(frequency, rows),
+                                   _vec(bias_id, rows * n_bias, torch.int32), _vec(bias, rows * n_bias), n_bias,
+                                   _vec(allowed, rows * -(-vocab // 32), torch.int32), op, ldo, _raw_stream()))
 
 
 def model_calibrate_mfma(lds_reads, random_data=0, iters=4000):

@@ -1,0 +1,241 @@
+// ae_clip.hip — the norm of many gradients taken together, and the gradients scaled down to a largest norm.
+//   norm = sqrt(sum over all elements of g^2);   out = g min(1, max_norm / norm)
+// Two passes bound by memory.  The tensors' addresses are arguments of the kernels, so that nothing is copied to the device
+// and a captured call keeps them; a list longer than the arguments' room takes several launches.  Squares are added up
+// in binary64, whose range the squares of binary32 numbers do not leave.
+#include <hip/hip_runtime.h>
+#include <float.h>
+
+#include <algorithm>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "ae_device.h"
+#include "ae_internal.h"
+#include "ae_rows.h"
+
+namespace ae {
+namespace {
+
+constexpr int NT = 256, U = 4;                   // threads, pieces of eight elements of a thread
+constexpr int64_t CHUNK = (int64_t)NT * 8 * U;   // elements that a workgroup takes at a time
+constexpr int LIST = 112;                        // tensors of a launch: 3.3 KB of arguments
+struct GradArgs {
+  const void* in[LIST];
+  void* out[LIST];
+  int64_t size[LIST];
+  int end[LIST];                                 // chunks of the tensors up to this one
+  uint8_t bf16[LIST];
+  int count, chunks;
+};
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T* p, int64_t left) {
+  Eight<T> e[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = ((int64_t)u * NT + threadIdx.x) * 8, l = left - at;
+    fetch8(p + at, l < 8 ? (int)(l < 0 ? 0 : l) : 8, e[u]);
+  }
+  double acc = 0.0;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const double v = (double)value(e[u], j);
+      acc = fma(v, v, acc);
+    }
+  return acc;
+}
+// Workgroup g takes the g-th of gridDim.x equal shares of the chunks, in order.
+__device__ __forceinline__ int share(const GradArgs& p, int g) { return (int)((int64_t)p.chunks * g / (int)gridDim.x); }
+__global__ __launch_bounds__(NT) void k_grad_squares(GradArgs p, double* __restrict__ part) {
+  __shared__ double sm[NT / 64 + 1];
+  const int from = share(p, blockIdx.x), to = share(p, blockIdx.x + 1);
+  double acc = 0.0;
+  int k = 0;
+  for (int c = from; c < to; ++c) {
+    while (c >= p.end[k]) ++k;
+    const int64_t at = (int64_t)(c - (k ? p.end[k - 1] : 0)) * CHUNK, left = p.size[k] - at;
+    acc += p.bf16[k] ? chunk_squares((const bf16_t*)p.in[k] + at, left) : chunk_squares((const float*)p.in[k] + at, left);
+  }
+  acc = block_sum<NT>(acc, sm);
+  if (threadIdx.x == 0) part[blockIdx.x] = acc;
+}
+
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const T* p, T* out, int64_t left, float factor) {
+  Eight<T> e[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = ((int64_t)u * NT + threadIdx.x) * 8, l = left - at;
+    fetch8(p + at, l < 8 ? (int)(l < 0 ? 0 : l) : 8, e[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = ((int64_t)u * NT + threadIdx.x) * 8, l = left - at;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = value(e[u], j) * factor;
+    if (l > 0) put8(out + at, l < 8 ? (int)l : 8, v);
+  }
+}
+// Every workgroup adds up the shares' sums itself, in the same order (8 KB, from L2), so that no launch stands in between.
+__global__ __launch_bounds__(NT) void k_grad_scale(GradArgs p, const double* __restrict__ part, int parts, float max_norm, float* __restrict__ norm) {
+  __shared__ double sm[NT / 64 + 1];
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += NT) sum += part[i];
+  const double all = sqrt(block_sum<NT>(sum, sm));
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
+  // a norm that is no number, or infinite, scales nothing
+  const float factor = all > (double)max_norm && all <= DBL_MAX ? (float)((double)max_norm / all) : 1.0f;
+  const int from = share(p, blockIdx.x), to = share(p, blockIdx.x + 1);
+  int k = p.count - 1;
+  for (int c = to - 1; c >= from; --c) {           // backwards: what the first pass read last is still in the cache
+    while (k > 0 && c < p.end[k - 1]) --k;
+    if (factor == 1.0f && p.in[k] == p.out[k]) continue;
+    const int64_t at = (int64_t)(c - (k ? p.end[k - 1] : 0)) * CHUNK, left = p.size[k] - at;
+    if (p.bf16[k]) chunk_scale((const bf16_t*)p.in[k] + at, (bf16_t*)p.out[k] + at, left, factor);
+    else chunk_scale((const float*)p.in[k] + at, (float*)p.out[k] + at, left, factor);
+  }
+}
+
+constexpr int kShares = 1024;                    // workgroups of a launch at most
+int64_t chunks_of(int64_t size) { return (size + CHUNK - 1) / CHUNK; }
+// the tensors [from, *next) of one launch: *next is behind the last, chunks are counted
+int64_t launch_range(const int64_t* sizes, int count, int from, int* next) {
+  int64_t chunks = 0;
+  int n = 0, k = from;
+  for (; k < count && n < LIST; ++k) {
+    const int64_t c = chunks_of(sizes[k]);
+    if (c == 0) continue;
+    if (chunks + c > 0x7FFFFFFF) break;
+    chunks += c;
+    ++n;
+  }
+  *next = k;
+  return chunks;
+}
+int shares_of(int64_t chunks) { return (int)(chunks < kShares ? chunks : kShares); }
+constexpr int64_t kSizeMax = (int64_t)1 << 40;   // elements of a tensor: 2^27 chunks
+int check_sizes(const char* who, const int64_t* sizes, int count) {
+  if (count < 0 || count > (1 << 20) || (count && !sizes)) return fail(AE_EINVAL, "%s: count must be 0 .. 2^20, with a size for each", who);
+  for (int k = 0; k < count; ++k)
+    if (sizes[k] < 0 || sizes[k] > kSizeMax) return fail(AE_EINVAL, "%s: sizes must be 0 .. 2^40", who);
+  return AE_OK;
+}
+int64_t parts_of(const int64_t* sizes, int count) {
+  int64_t parts = 0;
+  for (int k = 0; k < count;) parts += shares_of(launch_range(sizes, count, k, &k));
+  return parts;
+}
+
+// Whether no output overlaps another, or a gradient other than the one that it is the place of.
+typedef std::pair<uintptr_t, uintptr_t> Range;
+bool apart(void* const* grads, void* const* out, const int64_t* sizes, const int* dtypes, int count) {
+  std::vector<Range> w, r;
+  w.reserve(count);
+  r.reserve(count);
+  for (int k = 0; k < count; ++k) {
+    const uintptr_t bytes = (uintptr_t)sizes[k] * dtype_size(dtypes[k]);
+    if (!bytes) continue;
+    w.emplace_back((uintptr_t)out[k], (uintptr_t)out[k] + bytes);
+    if (out[k] != grads[k]) r.emplace_back((uintptr_t)grads[k], (uintptr_t)grads[k] + bytes);
+  }
+  if (!std::is_sorted(w.begin(), w.end())) std::sort(w.begin(), w.end());
+  if (!std::is_sorted(r.begin(), r.end())) std::sort(r.begin(), r.end());
+  for (size_t i = 1; i < w.size(); ++i)
+    if (w[i].first < w[i - 1].second) return false;
+  size_t j = 0;
+  for (const Range& a : r) {
+    while (j < w.size() && w[j].second <= a.first) ++j;
+    if (j < w.size() && w[j].first < a.second) return false;
+  }
+  return true;
+}
+
+}  // namespace
+}  // namespace ae
+
+extern "C" int model_grad_clip_workspace(const int64_t* sizes, int count, int64_t* bytes) {
+  using namespace ae;
+  if (!bytes) return fail(AE_EINVAL, "model_grad_clip_workspace: null argument");
+  AE_TRY(check_sizes("model_grad_clip_workspace", sizes, count));
+  *bytes = parts_of(sizes, count) * 8;
+  return AE_OK;
+}
+
+extern "C" int model_grad_clip(void* const* grads, const int64_t* sizes, const int* dtypes, int count, float max_norm, float* norm,
+                               void* const* out, void* workspace, void* stream) {
+  using namespace ae;
+  AE_TRY(check_sizes("model_grad_clip", sizes, count));
+  if (!norm && !out) return fail(AE_EINVAL, "model_grad_clip: no output");
+  if ((uintptr_t)norm & 3) return fail(AE_EINVAL, "model_grad_clip: misaligned norm");
+  if (!(max_norm > 0.0f)) return fail(AE_EINVAL, "model_grad_clip: max_norm must be positive");
+  if (count && (!grads || !dtypes)) return fail(AE_EINVAL, "model_grad_clip: null argument");
+  for (int k = 0; k < count; ++k) {
+    if (dtypes[k] != AE_F32 && dtypes[k] != AE_BF16) return fail(AE_EINVAL, "model_grad_clip: bad dtype of tensor %d", k);
+    if (!sizes[k]) continue;
+    if (!grads[k] || (out && !out[k])) return fail(AE_EINVAL, "model_grad_clip: tensor %d is null", k);
+    if (((uintptr_t)grads[k] | (uintptr_t)(out ? out[k] : nullptr)) % dtype_size(dtypes[k])) return fail(AE_EINVAL, "model_grad_clip: tensor %d is misaligned", k);
+  }
+  if (out) {
+    bool ok = false;
+    try {
+      ok = apart(grads, out, sizes, dtypes, count);
+    } catch (const std::bad_alloc&) {
+      return fail(AE_ENOMEM, "model_grad_clip: out of host memory");
+    }
+    if (!ok) return fail(AE_EINVAL, "model_grad_clip: an output overlaps another, or the gradient of another tensor");
+  }
+  const int64_t parts = parts_of(sizes, count);
+  if (parts > 0x7FFFFFFF) return fail(AE_EINVAL, "model_grad_clip: too many tensors");
+  if (parts && (!workspace || ((uintptr_t)workspace & 15))) return fail(AE_EINVAL, "model_grad_clip: workspace is null or not on a 16-byte border");
+  hipStream_t s = (hipStream_t)stream;
+  double* part = (double*)workspace;
+  GradArgs p;
+  auto fill = [&](int from, int next) {
+    p.count = 0;
+    p.chunks = 0;
+    for (int k = from; k < next; ++k) {
+      if (!sizes[k]) continue;
+      const int n = p.count++;
+      p.in[n] = grads[k];
+      p.out[n] = out ? out[k] : nullptr;
+      p.size[n] = sizes[k];
+      p.bf16[n] = dtypes[k] == AE_BF16;
+      p.end[n] = p.chunks += (int)chunks_of(sizes[k]);
+    }
+  };
+  int64_t done = 0;
+  int launches = 0;
+  for (int k = 0; k < count;) {
+    int next;
+    const int shares = shares_of(launch_range(sizes, count, k, &next));
+    if (shares) {
+      fill(k, next);
+      hipLaunchKernelGGL(k_grad_squares, dim3((unsigned)shares), dim3(NT), 0, s, p, part + done);
+      done += shares;
+      ++launches;
+    }
+    k = next;
+  }
+  AE_TRY(launch_status("grad_clip"));
+  if (!out || !launches) {
+    p.count = p.chunks = 0;
+    hipLaunchKernelGGL(k_grad_scale, dim3(1), dim3(NT), 0, s, p, part, (int)parts, max_norm, norm);
+    return launch_status("grad_clip");
+  }
+  for (int k = 0; k < count;) {
+    int next;
+    const int shares = shares_of(launch_range(sizes, count, k, &next));
+    if (shares) {
+      if (launches > 1) fill(k, next);
+      hipLaunchKernelGGL(k_grad_scale, dim3((unsigned)shares), dim3(NT), 0, s, p, part, (int)parts, max_norm, norm);
+      norm = nullptr;
+    }
+    k = next;
+  }
+  return launch_status("grad_clip");
+}

@@ -9,62 +9,16 @@
 #include <type_traits>
 
 #include "ae_device.h"
+#include "ae_fp8.h"
 #include "ae_internal.h"
 
 namespace ae {
 namespace {
 
-constexpr int BLK = 128;                 // elements that share a scale
-constexpr float kCodeMax = 448.0f;       // largest magnitude of an E4M3 code
-constexpr float kScaleMin = 1.17549435e-38f;
-
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-
-// Infinities are rare and cost the common case nothing: the maximum over all magnitudes (which passes NaN by) tells whether
-// a block holds any.  If not, x * (1 / scale) is at most 448 (1 + 2^-23), which the conversion rounds to 448, and a NaN
-// becomes the NaN code by itself; if so, the maximum is taken again over what is finite, and the products are cut off at 448.
-__device__ __forceinline__ float finite_abs(float v) {
-  const float a = fabsf(v);
-  return a <= FLT_MAX ? a : 0.0f;
-}
-__device__ __forceinline__ float block_scale(float amax) { return fmaxf(amax / kCodeMax, kScaleMin); }
-template <bool INF>
-__device__ __forceinline__ float code_value(float v, float inv) {
-  const float y = v * inv;
-  if constexpr (!INF) return y;
-  return y != y ? y : fminf(fmaxf(y, -kCodeMax), kCodeMax);
-}
-template <bool INF>
-__device__ __forceinline__ float magnitude(float v) { return INF ? finite_abs(v) : fabsf(v); }
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
-}
-
-// eight elements of a row from column c on, zeros behind the row's end; whole pieces with one load (bf16) or two
-// (binary32) at any alignment of the element's own
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
-  if (left >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      uint32_t w[4];
-      __builtin_memcpy(w, p, 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    } else {
-      __builtin_memcpy(v, p, 32);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? Store<T>::ld(p + i) : 0.0f;
-  }
-}
 
 // ---- quantiser -----------------------------------------------------------------------------------------------------
 // One workgroup of 256 threads per 128 x 128 tile of x: thread t holds rows 8 (t / 16) .. + 7 of columns 8 (t % 16) .. + 7

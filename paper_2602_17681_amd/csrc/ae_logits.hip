@@ -1,0 +1,149 @@
+// ae_logits.hip — what comes between an output layer's logits and the choice of a token: penalties for tokens that occurred,
+// biases of given tokens, and a mask of what a grammar allows.
+// A workgroup takes a slice of a row.  Every column of the slice has a word in LDS: how often the token was answered, whether
+// it occurred at all, and which bias it has.  The row's history and list of biases are read by each slice (they are short
+// beside it, and in the cache), then the slice passes through registers once.
+#include <hip/hip_runtime.h>
+
+#include "ae_device.h"
+#include "ae_internal.h"
+#include "ae_rows.h"
+
+namespace ae {
+namespace {
+
+constexpr int NT = 256;
+// a column's word: bits 0 .. 19 how often among the answers, bit 20 in the prompt, bits 21 .. 31 place in the list of biases + 1
+constexpr uint32_t kCount = (1u << 20) - 1, kPrompt = 1u << 20, kSeen = kCount | kPrompt;
+constexpr int kBiasAt = 21, kMaxHistory = kCount, kMaxBias = 2047;
+
+struct AdjustArgs {
+  const void* logits;
+  int64_t ld, rows;
+  int vocab;
+  const int* history;
+  int n_history;
+  const int* n_prompt;
+  const float *repetition, *presence, *frequency;
+  const int* bias_id;
+  const float* bias;
+  int n_bias;
+  const uint32_t* allowed;
+  void* out;
+  int64_t ldo;
+  int slices;
+  int64_t first;
+};
+
+template <typename T, int NP, bool LISTS>
+__global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
+  constexpr int S = NT * 8 * NP;                 // columns of a slice
+  __shared__ uint4 word4[LISTS ? S / 4 : 1];
+  uint32_t* const word = (uint32_t*)word4;
+  const int64_t at = p.first + blockIdx.x, row = at / p.slices;
+  const int s0 = (int)(at - row * p.slices) * S, mine = p.vocab - s0 < S ? p.vocab - s0 : S;
+  const T* z = (const T*)p.logits + row * p.ld + s0;
+  Eight<T> e[NP];
+  uint32_t ok[NP];
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    const int c = (k * NT + (int)threadIdx.x) * 8;
+    fetch8(z + c, mine - c, e[k]);
+    ok[k] = 0xFF;
+    if (p.allowed && c < mine) ok[k] = p.allowed[row * ((p.vocab + 31) / 32) + (s0 + c) / 32] >> (c & 31) & 0xFF;
+  }
+  float repetition = 1.0f, presence = 0.0f, frequency = 0.0f;
+  if constexpr (LISTS) {
+    for (int i = threadIdx.x; i < S / 4; i += NT) word4[i] = make_uint4(0, 0, 0, 0);
+    if (p.repetition) repetition = p.repetition[row];
+    if (p.presence) presence = p.presence[row];
+    if (p.frequency) frequency = p.frequency[row];
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.n_bias; i += NT) {
+      const unsigned c = (unsigned)p.bias_id[row * p.n_bias + i] - (unsigned)s0;
+      if (c < (unsigned)mine) atomicMax(&word[c], (uint32_t)(i + 1) << kBiasAt);       // the last entry of a token counts
+    }
+    if (p.n_bias) __syncthreads();
+    const int prompt = p.n_prompt ? p.n_prompt[row] : 0;
+    for (int i = threadIdx.x; i < p.n_history; i += NT) {
+      const unsigned c = (unsigned)p.history[row * p.n_history + i] - (unsigned)s0;
+      if (c >= (unsigned)mine) continue;
+      if (i < prompt) atomicOr(&word[c], kPrompt);
+      else atomicAdd(&word[c], 1u);
+    }
+    __syncthreads();
+  }
+  const bool in_place = p.logits == p.out;
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    const int c = (k * NT + (int)threadIdx.x) * 8;
+    if (c >= mine) continue;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = value(e[k], j);
+    if constexpr (LISTS) {
+      const uint4 a = word4[c / 4], b = word4[c / 4 + 1];
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      const bool touched = (a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w) != 0;
+      if (in_place && !touched && ok[k] == 0xFF) continue;      // stays as it is
+      if (touched) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (w[j] & kSeen) v[j] = v[j] > 0.0f ? v[j] / repetition : v[j] * repetition;
+          if (w[j] & kCount) v[j] = v[j] - frequency * (float)(w[j] & kCount) - presence;
+          if (w[j] >> kBiasAt) v[j] += p.bias[row * p.n_bias + (w[j] >> kBiasAt) - 1];
+        }
+      }
+    } else {
+      if (in_place && ok[k] == 0xFF) continue;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (!(ok[k] >> j & 1)) v[j] = -INFINITY;
+    put8((T*)p.out + row * p.ldo + s0 + c, mine - c, v);
+  }
+}
+
+template <typename T, int NP, bool LISTS>
+int launch_adjust(AdjustArgs p, hipStream_t s) {
+  constexpr int S = NT * 8 * NP;
+  p.slices = (p.vocab + S - 1) / S;
+  const int64_t all = p.rows * p.slices, most = launch_blocks(NT);
+  for (; p.first < all; p.first += most) {
+    const int64_t left = all - p.first;
+    hipLaunchKernelGGL((k_logits_adjust<T, NP, LISTS>), dim3((unsigned)(left < most ? left : most)), dim3(NT), 0, s, p);
+  }
+  return launch_status("logits_adjust");
+}
+template <typename T>
+int launch_adjust_rows(const AdjustArgs& p, hipStream_t s) {
+  if (!p.n_history && !p.n_bias) return launch_adjust<T, 2, false>(p, s);
+  if (p.rows * ((p.vocab + 4095) / 4096) < 1024) return launch_adjust<T, 1, true>(p, s);
+  return launch_adjust<T, 4, true>(p, s);
+}
+
+}  // namespace
+}  // namespace ae
+
+extern "C" int model_logits_adjust(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int* history, int64_t n_history,
+                                   const int* n_prompt, const float* repetition, const float* presence, const float* frequency,
+                                   const int* bias_id, const float* bias, int n_bias, const uint32_t* allowed, void* out, int64_t ldo,
+                                   void* stream) {
+  using namespace ae;
+  if (dtype != AE_F32 && dtype != AE_BF16) return fail(AE_EINVAL, "model_logits_adjust: bad dtype");
+  if (rows < 0 || rows > ((int64_t)1 << 24)) return fail(AE_EINVAL, "model_logits_adjust: rows must be 0 .. 2^24");
+  if (vocab < 1 || vocab > ((int64_t)1 << 20)) return fail(AE_EINVAL, "model_logits_adjust: vocab must be 1 .. 2^20");
+  if (ld < vocab || ldo < vocab || ld >= ((int64_t)1 << 40) || ldo >= ((int64_t)1 << 40)) return fail(AE_EINVAL, "model_logits_adjust: rows must not overlap");
+  if (n_history < 0 || n_history > kMaxHistory) return fail(AE_EINVAL, "model_logits_adjust: n_history must be 0 .. 2^20 - 1");
+  if (n_bias < 0 || n_bias > kMaxBias) return fail(AE_EINVAL, "model_logits_adjust: n_bias must be 0 .. 2047");
+  if (rows == 0) return AE_OK;
+  if (!logits || !out || (n_history && !history) || (n_bias && (!bias_id || !bias))) return fail(AE_EINVAL, "model_logits_adjust: null argument");
+  if (((uintptr_t)logits | (uintptr_t)out) % dtype_size(dtype)) return fail(AE_EINVAL, "model_logits_adjust: misaligned logits");
+  if (((uintptr_t)history | (uintptr_t)n_prompt | (uintptr_t)repetition | (uintptr_t)presence | (uintptr_t)frequency | (uintptr_t)bias_id | (uintptr_t)bias |
+       (uintptr_t)allowed) & 3)
+    return fail(AE_EINVAL, "model_logits_adjust: misaligned list");
+  if (logits == out && ld != ldo) return fail(AE_EINVAL, "model_logits_adjust: a result in the logits' place has their stride");
+  const AdjustArgs p = {logits, ld, rows, (int)vocab, history, (int)n_history, n_prompt, repetition, presence, frequency,
+                        bias_id, bias, n_bias, allowed, out, ldo, 0, 0};
+  return dtype == AE_BF16 ? launch_adjust_rows<bf16_t>(p, (hipStream_t)stream) : launch_adjust_rows<float>(p, (hipStream_t)stream);
+}

@@ -1,0 +1,523 @@
+// ae_norm.hip — root-mean-square norm of rows with the residual's addition, and its adjoint.
+//   h = x + residual,   y = h r w,   r = 1 / sqrt(mean h^2 + eps);   y in dtype and / or as E4M3 codes in blocks of 128
+//   g = dy w,   u = h r:   dh = d_h + r (g - u mean(g u)),   dw = sum over rows of dy u
+// Both are bound by memory: a row is read once, stays in registers between its sum and its results, and the row after it is
+// asked for before the sum is waited for.  Sums are binary32.  A row whose sum of squares leaves binary32's range
+// (|h| from 2^60 on) is multiplied by 2^-100 first, in its registers: exact, and u does not change.
+#include <hip/hip_runtime.h>
+#include <float.h>
+
+#include "ae_device.h"
+#include "ae_fp8.h"
+#include "ae_internal.h"
+
+namespace ae {
+namespace {
+
+constexpr float kDown = 7.8886090522101181e-31f;   // 2^-100
+
+// sum over the W wavefronts that share a row; sm is not written again before the workgroup's next barrier but one
+template <int W>
+__device__ __forceinline__ float team_sum(float v, float* sm) {
+  v = sum_rows(sum16(v));
+  if constexpr (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return sum_of<W>(sm);
+}
+
+struct NormArgs {
+  const void* x;
+  int64_t ldx;
+  const void* residual;
+  int64_t ldr;
+  const float* weight;
+  int64_t rows;
+  int d;
+  float eps;
+  void* h;
+  int64_t ldh;
+  void* y;
+  int64_t ldy;
+  uint8_t* q;
+  int64_t ldq;
+  float* scale;
+};
+
+// eight results of a row from column col on; the 16 lanes of a block of 128 come here together
+template <typename T>
+__device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, const float (&y)[8]) {
+  const int left = p.d - col;
+  if (p.y && left > 0) put8((T*)p.y + row * p.ldy + col, left, y);
+  if (!p.q) return;
+  float m = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
+  m = max16(m);
+  const bool inf = __any(m > FLT_MAX);
+  if (inf) {
+    m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(y[j]));
+    m = max16(m);
+  }
+  const float s = block_scale(m), inv = 1.0f / s;
+  float u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) u[j] = inf ? code_value<true>(y[j], inv) : code_value<false>(y[j], inv);
+  if (left <= 0) return;
+  if ((threadIdx.x & 15) == 0) p.scale[(int64_t)(col / BLK) * p.rows + row] = s;
+  uint8_t* at = p.q + row * p.ldq + col;
+  const uint32_t lo = codes4(u[0], u[1], u[2], u[3]), hi = codes4(u[4], u[5], u[6], u[7]);
+  if (left >= 8) {
+    *reinterpret_cast<uint2*>(at) = make_uint2(lo, hi);
+  } else {
+    for (int j = 0; j < left; ++j) at[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+  }
+}
+
+// 1 / sqrt(mean + eps) of a row; down: of the row times 2^-100, whose mean is so large that eps plays no part
+__device__ __forceinline__ float rms_inverse(float sum, int d, float eps, bool down) { return 1.0f / sqrtf(sum / (float)d + (down ? 0.0f : eps)); }
+
+// W wavefronts hold a row in NV pieces of eight elements per lane; with W = 1 a workgroup has four rows at a time.
+template <typename T, int W, int NV>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_rms_norm(NormArgs p) {
+  constexpr int TEAM = 64 * W, TEAMS = W == 1 ? 4 : 1;
+  __shared__ float sm[3][W];
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, step = (int)gridDim.x * TEAMS;
+  const T* x = (const T*)p.x;
+  const T* res = (const T*)p.residual;
+  float w[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int col = (v * TEAM + t) * 8, left = p.d - col;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[v][j] = 1.0f;
+    if (p.weight) load8<float>(p.weight + col, left, w[v]);
+  }
+  Eight<T> xe[NV], re[NV];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TEAM + t) * 8, left = p.d - col;
+      fetch8(x + row * p.ldx + col, left, xe[v]);
+      if (res) fetch8(res + row * p.ldr + col, left, re[v]);
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * TEAMS + team;
+  if (row < p.rows) fetch(row);
+  for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+    float h[NV][8], sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[v][j] = value(xe[v], j);
+        if (res) h[v][j] += value(re[v], j);
+        sum = fmaf(h[v][j], h[v][j], sum);
+      }
+    if (row + step < p.rows) fetch(row + step);
+    if (p.h) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * TEAM + t) * 8;
+        if (col < p.d) put8((T*)p.h + row * p.ldh + col, p.d - col, h[v]);
+      }
+    }
+    sum = team_sum<W>(sum, sm[turn]);
+    const bool down = !(sum <= FLT_MAX);           // the same in all threads of the row
+    if (down) {
+      sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          h[v][j] *= kDown;
+          sum = fmaf(h[v][j], h[v][j], sum);
+        }
+      if constexpr (W > 1) __syncthreads();
+      sum = team_sum<W>(sum, sm[2]);
+      if constexpr (W > 1) __syncthreads();
+    }
+    const float r = rms_inverse(sum, p.d, p.eps, down);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = h[v][j] * r * w[v][j];
+      emit<T>(p, row, (v * TEAM + t) * 8, y);
+    }
+  }
+}
+
+// Rows that registers do not hold are read twice; each element's results are written by the thread that reads it, behind
+// its second read, so that h may take the place of x or of the residual here too.
+constexpr int WIDE = 1024;
+template <typename T>
+__global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
+  __shared__ float sm[2][WIDE / 64];
+  const T* x = (const T*)p.x;
+  const T* res = (const T*)p.residual;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    auto load = [&](int col, float by, float (&h)[8]) {
+      float r8[8];
+      load8<T>(x + row * p.ldx + col, p.d - col, h);
+      if (res) load8<T>(res + row * p.ldr + col, p.d - col, r8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = (res ? h[j] + r8[j] : h[j]) * by;
+    };
+    auto squares = [&](float by) {
+      float sum = 0.0f, h[8];
+      for (int col = threadIdx.x * 8; col < p.d; col += WIDE * 8) {
+        load(col, by, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fmaf(h[j], h[j], sum);
+      }
+      return sum;
+    };
+    float sum = team_sum<WIDE / 64>(squares(1.0f), sm[0]);
+    const bool down = !(sum <= FLT_MAX);
+    if (down) sum = team_sum<WIDE / 64>(squares(kDown), sm[1]);
+    const float r = rms_inverse(sum, p.d, p.eps, down);
+    for (int c0 = 0; c0 < p.d; c0 += WIDE * 8) {           // all threads: a block's lanes meet in emit
+      const int col = c0 + threadIdx.x * 8;
+      float h[8], w[8], y[8];
+      load(col, 1.0f, h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = 1.0f;
+      if (p.weight) load8<float>(p.weight + col, p.d - col, w);
+      if (p.h && col < p.d) put8((T*)p.h + row * p.ldh + col, p.d - col, h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = (down ? h[j] * kDown : h[j]) * r * w[j];
+      emit<T>(p, row, col, y);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, int W, int NV>
+int launch_norm_row(const NormArgs& p, hipStream_t s) {
+  constexpr int TEAMS = W == 1 ? 4 : 1;
+  const int64_t want = (p.rows + TEAMS - 1) / TEAMS, most = 256 * (W <= 4 ? 8 : 32 / W);
+  hipLaunchKernelGGL((k_rms_norm<T, W, NV>), dim3((unsigned)(want < most ? want : most)), dim3(W == 1 ? 256 : 64 * W), 0, s, p);
+  return launch_status("rms_norm");
+}
+template <typename T>
+int launch_norm(const NormArgs& p, hipStream_t s) {
+  if (p.d <= 512) return launch_norm_row<T, 1, 1>(p, s);
+  if (p.d <= 1024) return launch_norm_row<T, 1, 2>(p, s);
+  if (p.d <= 2048) return launch_norm_row<T, 4, 1>(p, s);
+  if (p.d <= 4096) return launch_norm_row<T, 4, 2>(p, s);
+  if (p.d <= 8192) return launch_norm_row<T, 8, 2>(p, s);
+  if (p.d <= 16384) return launch_norm_row<T, 16, 2>(p, s);
+  if (p.d <= 32768) return launch_norm_row<T, 16, 4>(p, s);
+  const int64_t most = 512;
+  hipLaunchKernelGGL((k_rms_norm_wide<T>), dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(WIDE), 0, s, p);
+  return launch_status("rms_norm");
+}
+
+// ---- adjoint -------------------------------------------------------------------------------------------------------
+struct NormGradArgs {
+  const void* dy;
+  int64_t ldy;
+  const void* h;
+  int64_t ldh;
+  const float* weight;
+  const void* d_h;
+  int64_t ldg;
+  int64_t rows;
+  int d;
+  float eps;
+  void* dx;
+  int64_t lddx;
+  float* part;                            // [teams][d]: each team's sum of dy u over its rows; null: not wanted
+  float* stat;                            // [rows][4], rows that registers do not hold
+};
+
+// u = h times down (1 or 2^-100) times r; the gradient's common factor is r times down
+struct RowStat {
+  float r, down, mean;                    // mean(g u)
+};
+template <int W>
+__device__ __forceinline__ RowStat row_stat(float hh, float gh, int d, float eps, bool down) {
+  const float r = rms_inverse(hh, d, eps, down);
+  return {r, down ? kDown : 1.0f, r * gh / (float)d};
+}
+
+template <typename T, int W, int NV>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_rms_norm_grad(NormGradArgs p) {
+  constexpr int TEAM = 64 * W, TEAMS = W == 1 ? 4 : 1;
+  __shared__ float sm[3][2][W];
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, step = (int)gridDim.x * TEAMS;
+  float w[NV][8], acc[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int col = (v * TEAM + t) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { w[v][j] = 1.0f; acc[v][j] = 0.0f; }
+    if (p.weight) load8<float>(p.weight + col, p.d - col, w[v]);
+  }
+  Eight<T> he[NV], ge[NV], re[NV];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TEAM + t) * 8, left = p.d - col;
+      fetch8((const T*)p.h + row * p.ldh + col, left, he[v]);
+      fetch8((const T*)p.dy + row * p.ldy + col, left, ge[v]);
+      if (p.d_h) fetch8((const T*)p.d_h + row * p.ldg + col, left, re[v]);
+    }
+  };
+  const int64_t first = (int64_t)blockIdx.x * TEAMS + team;
+  if (first < p.rows) fetch(first);
+  int turn = 0;
+  for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
+    float h[NV][8], dy[NV][8], add[NV][8], hh = 0.0f, gh = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[v][j] = value(he[v], j);
+        dy[v][j] = value(ge[v], j);
+        add[v][j] = p.d_h ? value(re[v], j) : 0.0f;
+        hh = fmaf(h[v][j], h[v][j], hh);
+        gh = fmaf(dy[v][j] * w[v][j], h[v][j], gh);
+      }
+    if (row + step < p.rows) fetch(row + step);
+    // both sums at one barrier
+    auto sums = [&](float (&s2)[2][W]) {
+      hh = sum_rows(sum16(hh));
+      gh = sum_rows(sum16(gh));
+      if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) { s2[0][threadIdx.x >> 6] = hh; s2[1][threadIdx.x >> 6] = gh; }
+        __syncthreads();
+        hh = sum_of<W>(s2[0]);
+        gh = sum_of<W>(s2[1]);
+      }
+    };
+    sums(sm[turn]);
+    const bool down = !(hh <= FLT_MAX) || !(fabsf(gh) <= FLT_MAX);
+    if (down) {
+      hh = gh = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          h[v][j] *= kDown;
+          hh = fmaf(h[v][j], h[v][j], hh);
+          gh = fmaf(dy[v][j] * w[v][j], h[v][j], gh);
+        }
+      if constexpr (W > 1) __syncthreads();
+      sums(sm[2]);
+      if constexpr (W > 1) __syncthreads();
+    }
+    const RowStat st = row_stat<W>(hh, gh, p.d, p.eps, down);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TEAM + t) * 8;
+      float o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float u = h[v][j] * st.r;
+        acc[v][j] = fmaf(dy[v][j], u, acc[v][j]);
+        o[j] = (dy[v][j] * w[v][j] - u * st.mean) * st.r * st.down + add[v][j];
+      }
+      if (p.dx && col < p.d) put8((T*)p.dx + row * p.lddx + col, p.d - col, o);
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int col = (v * TEAM + t) * 8;
+    if (col < p.d) put8(p.part + first * p.d + col, p.d - col, acc[v]);
+  }
+}
+
+// Rows that registers do not hold: r, 2^0 or 2^-100 and mean(g u) of every row first, then the gradients by columns.
+template <typename T>
+__global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
+  __shared__ float sm[4][WIDE / 64];
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    float hh, gh;
+    auto sums = [&](float by) {
+      hh = gh = 0.0f;
+      for (int col = threadIdx.x * 8; col < p.d; col += WIDE * 8) {
+        float h[8], g[8], w[8];
+        load8<T>((const T*)p.h + row * p.ldh + col, p.d - col, h);
+        load8<T>((const T*)p.dy + row * p.ldy + col, p.d - col, g);
+        if (p.weight) load8<float>(p.weight + col, p.d - col, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          h[j] *= by;
+          hh = fmaf(h[j], h[j], hh);
+          gh = fmaf(p.weight ? g[j] * w[j] : g[j], h[j], gh);
+        }
+      }
+    };
+    sums(1.0f);
+    hh = team_sum<WIDE / 64>(hh, sm[0]);
+    gh = team_sum<WIDE / 64>(gh, sm[1]);
+    const bool down = !(hh <= FLT_MAX) || !(fabsf(gh) <= FLT_MAX);
+    if (down) {
+      sums(kDown);
+      hh = team_sum<WIDE / 64>(hh, sm[2]);
+      gh = team_sum<WIDE / 64>(gh, sm[3]);
+    }
+    const RowStat st = row_stat<1>(hh, gh, p.d, p.eps, down);
+    if (threadIdx.x == 0) {
+      float* at = p.stat + row * 4;
+      at[0] = st.r; at[1] = st.down; at[2] = st.mean;
+    }
+    __syncthreads();
+  }
+}
+// blockIdx.x: 2 048 columns, blockIdx.y: every gridDim.y-th row
+template <typename T>
+__global__ __launch_bounds__(256) void k_rms_norm_grad_columns(NormGradArgs p) {
+  const int col = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8, left = p.d - col;
+  if (left <= 0) return;
+  float w[8], acc[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) { w[j] = 1.0f; acc[j] = 0.0f; }
+  if (p.weight) load8<float>(p.weight + col, left, w);
+  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+    const RowStat st = {p.stat[row * 4], p.stat[row * 4 + 1], p.stat[row * 4 + 2]};
+    float h[8], dy[8], add[8], o[8];
+    load8<T>((const T*)p.h + row * p.ldh + col, left, h);
+    load8<T>((const T*)p.dy + row * p.ldy + col, left, dy);
+    if (p.d_h) load8<T>((const T*)p.d_h + row * p.ldg + col, left, add);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float u = h[j] * st.down * st.r;
+      acc[j] = fmaf(dy[j], u, acc[j]);
+      o[j] = (dy[j] * w[j] - u * st.mean) * st.r * st.down + (p.d_h ? add[j] : 0.0f);
+    }
+    if (p.dx) put8((T*)p.dx + row * p.lddx + col, left, o);
+  }
+  if (p.part) put8(p.part + (int64_t)blockIdx.y * p.d + col, left, acc);
+}
+
+// dw[j] = sum of n parts in a fixed order: 16 wavefronts take every 16th part of 64 columns each
+__global__ __launch_bounds__(1024) void k_sum_parts(const float* __restrict__ part, int64_t n, int d, float* __restrict__ out) {
+  __shared__ float sm[16][64];
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, col = (int)blockIdx.x * 64 + lane;
+  float acc = 0.0f;
+  if (col < d) {
+    constexpr int U = 8;
+    for (int64_t i0 = g; i0 < n; i0 += 16 * U) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = i0 + 16 * u < n ? part[(i0 + 16 * u) * d + col] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc += v[u];
+    }
+  }
+  sm[g][lane] = acc;
+  __syncthreads();
+  if (g == 0 && col < d) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) acc += sm[i][lane];
+    out[col] = acc;
+  }
+}
+
+constexpr int kInRegisters = 32768;                // columns
+// teams of a launch, each with a part of the weight's gradient
+int64_t grad_teams(int64_t rows, int64_t d) {
+  if (d > kInRegisters) return rows < 64 ? rows : 64;
+  const int64_t most = d <= 1024 ? 256 * 4 * 4 : d <= 4096 ? 256 * 4 : 512;
+  const int64_t teams = d <= 1024 ? (rows + 3) / 4 * 4 : rows;
+  return teams < most ? teams : most;
+}
+int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
+
+template <typename T, int W, int NV>
+int launch_grad_row(const NormGradArgs& p, int64_t teams, hipStream_t s) {
+  hipLaunchKernelGGL((k_rms_norm_grad<T, W, NV>), dim3((unsigned)(W == 1 ? teams / 4 : teams)), dim3(W == 1 ? 256 : 64 * W), 0, s, p);
+  return launch_status("rms_norm_backward");
+}
+template <typename T>
+int launch_grad(const NormGradArgs& p, int64_t teams, hipStream_t s) {
+  if (p.d <= 512) return launch_grad_row<T, 1, 1>(p, teams, s);
+  if (p.d <= 1024) return launch_grad_row<T, 1, 2>(p, teams, s);
+  if (p.d <= 2048) return launch_grad_row<T, 4, 1>(p, teams, s);
+  if (p.d <= 4096) return launch_grad_row<T, 4, 2>(p, teams, s);
+  if (p.d <= 8192) return launch_grad_row<T, 8, 2>(p, teams, s);
+  if (p.d <= 16384) return launch_grad_row<T, 16, 2>(p, teams, s);
+  if (p.d <= kInRegisters) return launch_grad_row<T, 16, 4>(p, teams, s);
+  hipLaunchKernelGGL((k_rms_norm_stat<T>), dim3((unsigned)(p.rows < 512 ? p.rows : 512)), dim3(WIDE), 0, s, p);
+  hipLaunchKernelGGL((k_rms_norm_grad_columns<T>), dim3((unsigned)((p.d + 2047) / 2048), (unsigned)teams), dim3(256), 0, s, p);
+  return launch_status("rms_norm_backward");
+}
+
+constexpr int64_t kRowsMax = 0x7FFFFFFF - 512;
+constexpr int64_t kWidthMax = 1 << 20;
+int check_norm(const char* who, int64_t rows, int64_t d, float eps, int dtype) {
+  if (dtype != AE_F32 && dtype != AE_BF16) return fail(AE_EINVAL, "%s: bad dtype", who);
+  if (rows < 0 || rows > kRowsMax) return fail(AE_EINVAL, "%s: rows must be 0 .. 2^31 - 513", who);
+  if (d < 1 || d > kWidthMax) return fail(AE_EINVAL, "%s: d must be 1 .. 2^20", who);
+  if (!(eps >= FLT_MIN && eps <= FLT_MAX)) return fail(AE_EINVAL, "%s: eps must be a positive normal number", who);
+  return AE_OK;
+}
+// a matrix of rows that do not overlap, on its elements' borders; null is no matrix
+bool rows_ok(const void* p, int64_t ld, int64_t d, int dtype) {
+  return !p || (ld >= d && ld < ((int64_t)1 << 40) && (uintptr_t)p % dtype_size(dtype) == 0);
+}
+
+}  // namespace
+}  // namespace ae
+
+extern "C" int model_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, int64_t rows, int64_t d,
+                              float eps, int dtype, void* h, int64_t ldh, void* y, int64_t ldy, void* q, int64_t ldq, float* scale,
+                              void* stream) {
+  using namespace ae;
+  AE_TRY(check_norm("model_rms_norm", rows, d, eps, dtype));
+  if (rows == 0) return AE_OK;                       // a matrix without rows may have no address
+  if ((!q) != (!scale)) return fail(AE_EINVAL, "model_rms_norm: codes and their scales go together");
+  if (!h && !y && !q) return fail(AE_EINVAL, "model_rms_norm: no output");
+  if (!x) return fail(AE_EINVAL, "model_rms_norm: null argument");
+  if (!rows_ok(x, ldx, d, dtype) || !rows_ok(residual, ldr, d, dtype) || !rows_ok(h, ldh, d, dtype) || !rows_ok(y, ldy, d, dtype))
+    return fail(AE_EINVAL, "model_rms_norm: rows must not overlap and must lie on their elements' borders");
+  if (((uintptr_t)weight | (uintptr_t)scale) & 3) return fail(AE_EINVAL, "model_rms_norm: misaligned weight or scales");
+  if (q && (((uintptr_t)q & 15) || ldq < d || ldq % 16 || ldq >= ((int64_t)1 << 40)))
+    return fail(AE_EINVAL, "model_rms_norm: rows of codes must begin on 16-byte borders and not overlap");
+  if ((h && ((h == x && ldh != ldx) || (h == residual && ldh != ldr))) || (y && ((y == x && ldy != ldx) || (y == residual && ldy != ldr))) || (h && h == y))
+    return fail(AE_EINVAL, "model_rms_norm: an output in an input's place has its stride, and h and y have places of their own");
+  const NormArgs p = {x, ldx, residual, ldr, weight, rows, (int)d, eps, h, ldh, y, ldy, (uint8_t*)q, ldq, scale};
+  return dtype == AE_BF16 ? launch_norm<bf16_t>(p, (hipStream_t)stream) : launch_norm<float>(p, (hipStream_t)stream);
+}
+
+extern "C" int model_rms_norm_backward_workspace(int64_t rows, int64_t d, int dtype, int64_t* bytes) {
+  using namespace ae;
+  if (!bytes) return fail(AE_EINVAL, "model_rms_norm_backward_workspace: null argument");
+  AE_TRY(check_norm("model_rms_norm_backward_workspace", rows, d, 1.0f, dtype));
+  *bytes = align16(grad_teams(rows, d) * d * 4) + (d > kInRegisters ? rows * 16 : 0);
+  return AE_OK;
+}
+
+extern "C" int model_rms_norm_backward(const void* dy, int64_t ldy, const void* h, int64_t ldh, const float* weight, const void* d_h,
+                                       int64_t ldg, int64_t rows, int64_t d, float eps, int dtype, void* dx, int64_t lddx,
+                                       float* d_weight, void* workspace, void* stream) {
+  using namespace ae;
+  AE_TRY(check_norm("model_rms_norm_backward", rows, d, eps, dtype));
+  if (rows == 0 && !d_weight) return AE_OK;          // a matrix without rows may have no address
+  if (!dx && !d_weight) return fail(AE_EINVAL, "model_rms_norm_backward: no output");
+  if (((uintptr_t)weight | (uintptr_t)d_weight) & 3) return fail(AE_EINVAL, "model_rms_norm_backward: misaligned weight");
+  int64_t need = 0;
+  AE_TRY(model_rms_norm_backward_workspace(rows, d, dtype, &need));
+  if (need && (!workspace || ((uintptr_t)workspace & 15))) return fail(AE_EINVAL, "model_rms_norm_backward: workspace is null or not on a 16-byte border");
+  hipStream_t s = (hipStream_t)stream;
+  const int64_t teams = grad_teams(rows, d);
+  if (rows > 0) {
+    if (!dy || !h) return fail(AE_EINVAL, "model_rms_norm_backward: null argument");
+    if (!rows_ok(dy, ldy, d, dtype) || !rows_ok(h, ldh, d, dtype) || !rows_ok(d_h, ldg, d, dtype) || !rows_ok(dx, lddx, d, dtype))
+      return fail(AE_EINVAL, "model_rms_norm_backward: rows must not overlap and must lie on their elements' borders");
+    if (dx && ((dx == dy && lddx != ldy) || (dx == h && lddx != ldh) || (dx == d_h && lddx != ldg)))
+      return fail(AE_EINVAL, "model_rms_norm_backward: a gradient in an input's place has its stride");
+    NormGradArgs p = {dy, ldy, h, ldh, weight, d_h, ldg, rows, (int)d, eps, dx, lddx, nullptr, nullptr};
+    if (d_weight) p.part = (float*)workspace;
+    p.stat = (float*)((char*)workspace + align16(teams * d * 4));
+    AE_TRY(dtype == AE_BF16 ? launch_grad<bf16_t>(p, teams, s) : launch_grad<float>(p, teams, s));
+  }
+  if (d_weight) hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0, s, (const float*)workspace, teams, (int)d, d_weight);
+  return launch_status("rms_norm_backward");
+}
