@@ -18,6 +18,7 @@ _LIB_PATH = os.path.join(_HERE, "libaemodel.so")
 AE_F32, AE_BF16 = 0, 1
 DTYPES = {"f32": AE_F32, "bf16": AE_BF16}
 TORCH_DTYPE = {AE_F32: torch.float32, AE_BF16: torch.bfloat16}
+_DTYPE_CODE = {t: c for c, t in TORCH_DTYPE.items()}
 
 SYMBOLS = [
     "model_describe", "model_create", "model_destroy", "model_param_count", "model_io_shape",
@@ -146,7 +147,7 @@ def _ptr(t, dtype=None):
 
 def _raw_stream():
     """The current stream of the current device as a number: what _stream() wraps, without the Stream object in between."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _mat(t, rows, cols, dtype=None):
@@ -192,8 +193,9 @@ def _room(t, nbytes):
 
 
 def _dtype_of(t):
-    assert t.dtype == torch.bfloat16 or t.dtype == torch.float32, t.dtype
-    return AE_BF16 if t.dtype == torch.bfloat16 else AE_F32
+    code = _DTYPE_CODE.get(t.dtype)
+    assert code is not None, t.dtype
+    return code
 
 
 def model_last_error():

@@ -18,31 +18,50 @@
 namespace ae {
 namespace {
 
-constexpr int NT = 256, U = 4;                   // threads, pieces of eight elements of a thread
-constexpr int64_t CHUNK = (int64_t)NT * 8 * U;   // elements that a workgroup takes at a time
-constexpr int LIST = 112;                        // tensors of a launch: 3.3 KB of arguments
+constexpr int NT = 256;
+constexpr int64_t CHUNK = 8192;                  // elements that a workgroup takes at a time
+constexpr int LIST = 128;                        // tensors of a launch: 3.8 of the 4 KB that arguments may have
+template <typename T> constexpr int VEC = 16 / (int)sizeof(T);
+template <typename T> constexpr int PIECES = (int)(CHUNK / NT / VEC<T>);          // 16-byte pieces of a thread, all in flight
 struct GradArgs {
   const void* in[LIST];
   void* out[LIST];
   int64_t size[LIST];
-  int end[LIST];                                 // chunks of the tensors up to this one
+  int end[LIST];                                 // chunks of the tensors up to this one; behind the last: the largest int
   uint8_t bf16[LIST];
   int count, chunks;
+  float keep;                                    // part of a share, at its end, that is read to stay in the cache
 };
-
-template <typename T>
-__device__ __forceinline__ double chunk_squares(const T* p, int64_t left) {
-  Eight<T> e[U];
+// the tensor that a chunk belongs to: the first whose end lies behind it, all compared at once
+__device__ __forceinline__ int tensor_of(const GradArgs& p, int chunk) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t at = ((int64_t)u * NT + threadIdx.x) * 8, l = left - at;
-    fetch8(p + at, l < 8 ? (int)(l < 0 ? 0 : l) : 8, e[u]);
+  for (int i = 0; i < LIST; i += 64) n += __popcll(__ballot(p.end[i + lane] <= chunk));
+  return n;
+}
+template <typename T, bool STREAM>
+__device__ __forceinline__ void chunk_load(const T* p, int64_t left, Piece<T, VEC<T>> (&e)[PIECES<T>]) {
+  if (left >= CHUNK) {                            // whole chunks: nothing between the loads
+#pragma unroll
+    for (int u = 0; u < PIECES<T>; ++u) fetch_whole<STREAM>(p + (u * NT + (int)threadIdx.x) * VEC<T>, e[u]);
+  } else {
+#pragma unroll
+    for (int u = 0; u < PIECES<T>; ++u) {
+      const int at = (u * NT + (int)threadIdx.x) * VEC<T>, l = (int)left - at;
+      fetch(p + at, l < 0 ? 0 : l, e[u]);
+    }
   }
+}
+template <typename T, bool STREAM>
+__device__ __forceinline__ double chunk_squares(const T* p, int64_t left) {
+  Piece<T, VEC<T>> e[PIECES<T>];
+  chunk_load<T, STREAM>(p, left, e);
   double acc = 0.0;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int u = 0; u < PIECES<T>; ++u)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < VEC<T>; ++j) {
       const double v = (double)value(e[u], j);
       acc = fma(v, v, acc);
     }
@@ -53,12 +72,14 @@ __device__ __forceinline__ int share(const GradArgs& p, int g) { return (int)((i
 __global__ __launch_bounds__(NT) void k_grad_squares(GradArgs p, double* __restrict__ part) {
   __shared__ double sm[NT / 64 + 1];
   const int from = share(p, blockIdx.x), to = share(p, blockIdx.x + 1);
+  const int stay = to - (int)ceilf((float)(to - from) * p.keep);
   double acc = 0.0;
-  int k = 0;
+  int k = tensor_of(p, from);
   for (int c = from; c < to; ++c) {
     while (c >= p.end[k]) ++k;
     const int64_t at = (int64_t)(c - (k ? p.end[k - 1] : 0)) * CHUNK, left = p.size[k] - at;
-    acc += p.bf16[k] ? chunk_squares((const bf16_t*)p.in[k] + at, left) : chunk_squares((const float*)p.in[k] + at, left);
+    if (c >= stay) acc += p.bf16[k] ? chunk_squares<bf16_t, false>((const bf16_t*)p.in[k] + at, left) : chunk_squares<float, false>((const float*)p.in[k] + at, left);
+    else acc += p.bf16[k] ? chunk_squares<bf16_t, true>((const bf16_t*)p.in[k] + at, left) : chunk_squares<float, true>((const float*)p.in[k] + at, left);
   }
   acc = block_sum<NT>(acc, sm);
   if (threadIdx.x == 0) part[blockIdx.x] = acc;
@@ -66,19 +87,16 @@ __global__ __launch_bounds__(NT) void k_grad_squares(GradArgs p, double* __restr
 
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T* p, T* out, int64_t left, float factor) {
-  Eight<T> e[U];
+  Piece<T, VEC<T>> e[PIECES<T>];
+  chunk_load<T, true>(p, left, e);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t at = ((int64_t)u * NT + threadIdx.x) * 8, l = left - at;
-    fetch8(p + at, l < 8 ? (int)(l < 0 ? 0 : l) : 8, e[u]);
-  }
+  for (int u = 0; u < PIECES<T>; ++u) {
+    const int at = (u * NT + (int)threadIdx.x) * VEC<T>;
+    float v[VEC<T>];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t at = ((int64_t)u * NT + threadIdx.x) * 8, l = left - at;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = value(e[u], j) * factor;
-    if (l > 0) put8(out + at, l < 8 ? (int)l : 8, v);
+    for (int j = 0; j < VEC<T>; ++j) v[j] = value(e[u], j) * factor;
+    if (left >= CHUNK) put_whole<true>(out + at, v);
+    else if (left > at) put(out + at, (int)left - at, v);
   }
 }
 // Every workgroup adds up the shares' sums itself, in the same order (8 KB, from L2), so that no launch stands in between.
@@ -91,7 +109,7 @@ __global__ __launch_bounds__(NT) void k_grad_scale(GradArgs p, const double* __r
   // a norm that is no number, or infinite, scales nothing
   const float factor = all > (double)max_norm && all <= DBL_MAX ? (float)((double)max_norm / all) : 1.0f;
   const int from = share(p, blockIdx.x), to = share(p, blockIdx.x + 1);
-  int k = p.count - 1;
+  int k = from < to ? tensor_of(p, to - 1) : 0;
   for (int c = to - 1; c >= from; --c) {           // backwards: what the first pass read last is still in the cache
     while (k > 0 && c < p.end[k - 1]) --k;
     if (factor == 1.0f && p.in[k] == p.out[k]) continue;
@@ -101,7 +119,10 @@ __global__ __launch_bounds__(NT) void k_grad_scale(GradArgs p, const double* __r
   }
 }
 
-constexpr int kShares = 1024;                    // workgroups of a launch at most
+constexpr int kShares = 1024;                    // workgroups of a launch at most (512 MB, norm alone / clipped: 83 / 253 us; 2 048 83 / 258, 4 096 86 / 266)
+// What the second pass finds in the cache, beginning with what the first read last; the first reads the rest of a list, and all
+// where there is no second, as a stream.  512 MB clipped: 253 us with 256 MB kept, 261 with 192, 278 with 64, 257 with all; 1 024 MB 529, 537, 555, 547.
+constexpr int64_t kKeep = (int64_t)256 << 20;
 int64_t chunks_of(int64_t size) { return (size + CHUNK - 1) / CHUNK; }
 // the tensors [from, *next) of one launch: *next is behind the last, chunks are counted
 int64_t launch_range(const int64_t* sizes, int count, int from, int* next) {
@@ -207,7 +228,11 @@ extern "C" int model_grad_clip(void* const* grads, const int64_t* sizes, const i
       p.bf16[n] = dtypes[k] == AE_BF16;
       p.end[n] = p.chunks += (int)chunks_of(sizes[k]);
     }
+    for (int n = p.count; n < LIST; ++n) p.end[n] = 0x7FFFFFFF;
   };
+  int64_t bytes = 0;
+  for (int k = 0; k < count; ++k) bytes += sizes[k] * (int64_t)dtype_size(dtypes[k]);
+  p.keep = !out ? 0.0f : bytes <= kKeep ? 1.0f : (float)kKeep / (float)bytes;
   int64_t done = 0;
   int launches = 0;
   for (int k = 0; k < count;) {

@@ -18,6 +18,7 @@ template <typename T, int LANES, int U>
 __global__ __launch_bounds__(256) void k_embedding(const T* __restrict__ table, int64_t ldt, int64_t vocab, int d, const int* __restrict__ ids,
                                                    int64_t n, float scale, T* __restrict__ out, int64_t ldo, int64_t first) {
   constexpr int ROWS = 256 / LANES;
+  constexpr bool SHORT = LANES == 16;
   const int t = threadIdx.x % LANES;
   const int64_t i0 = (first + blockIdx.x) * (ROWS * U) + threadIdx.x / LANES;
   int64_t at[U];
@@ -31,14 +32,15 @@ __global__ __launch_bounds__(256) void k_embedding(const T* __restrict__ table, 
     const int left = d - col;
     Eight<T> e[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) fetch8(table + (at[u] < 0 ? 0 : at[u]) + col, at[u] < 0 ? 0 : left, e[u]);
+    for (int u = 0; u < U; ++u) fetch_row<false, SHORT>(table + (at[u] < 0 ? 0 : at[u]), col, d, e[u]);       // no token: the first row, not used
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u * ROWS >= n) continue;
+      settle<SHORT>(col, d, e[u]);
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = at[u] < 0 ? 0.0f : value(e[u], j) * scale;
-      put8(out + (i0 + u * ROWS) * ldo + col, left, v);
+      put(out + (i0 + u * ROWS) * ldo + col, left, v);
     }
   }
 }
@@ -47,7 +49,8 @@ __global__ __launch_bounds__(256) void k_embedding(const T* __restrict__ table, 
 // Places in the order of their tokens, without a pass over global counters: each workgroup owns a range of tokens, reads
 // all ids twice (they are few bytes beside the rows) and keeps its tokens' counters in LDS.  The first pass counts its
 // tokens and what lies below its range; the second puts its places down in their order.
-constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_RANGE = 4096, SORT_IDS = 4;    // tokens of a range at most; ids of a thread at a time
+constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_RANGE = 4096;    // tokens of a range at most
+constexpr int SORT_LOADS = 4096 / SORT_NT, SORT_IDS = SORT_NT * 4 * SORT_LOADS;             // ids that a workgroup has in registers: four neighbours to a load
 struct EmbedSort {
   int* place;                             // [n]: places in the order of their tokens
   int* token;                             // [n]: the token at each position of that order
@@ -55,31 +58,47 @@ struct EmbedSort {
 };
 __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ ids, int64_t n, int vocab, int range, EmbedSort out) {
   __shared__ int at[SORT_RANGE];
-  __shared__ int queue_v[SORT_NT * SORT_IDS], queue_i[SORT_NT * SORT_IDS];
-  __shared__ int wave_sum_of[SORT_WAVES + 1];
+  __shared__ uint32_t queue[SORT_IDS];           // token within the range << 14 | place within the ids at hand
+  __shared__ int sums[SORT_LOADS * SORT_WAVES];
+  static_assert(SORT_IDS == 1 << 14 && SORT_RANGE <= 1 << 18, "a queue entry holds both");
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int v0 = (int)blockIdx.x * range, mine = vocab - v0 < range ? vocab - v0 : range;
+  int id[SORT_LOADS][4];
+  auto load = [&](int64_t base) {
+#pragma unroll
+    for (int l = 0; l < SORT_LOADS; ++l) {
+      const int64_t i = base + (l * SORT_NT + t) * 4;
+      if (i + 4 <= n) {
+        __builtin_memcpy(id[l], ids + i, 16);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) id[l][k] = i + k < n ? ids[i + k] : -1;
+      }
+    }
+  };
+  load(0);
   for (int v = t; v < mine; v += SORT_NT) at[v] = 0;
   __syncthreads();
   int below = 0;
-  for (int64_t i = t; i < n; i += SORT_NT) {
-    const int id = ids[i];
-    below += id >= 0 && id < v0;
-    if ((unsigned)(id - v0) < (unsigned)mine && id >= 0) atomicAdd(&at[id - v0], 1);
+  for (int64_t base = 0; base < n; base += SORT_IDS) {
+    if (base) load(base);
+#pragma unroll
+    for (int l = 0; l < SORT_LOADS; ++l)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {              // a negative id is a large unsigned number
+        below += (unsigned)id[l][k] < (unsigned)v0;
+        const unsigned v = (unsigned)id[l][k] - (unsigned)v0;
+        if (v < (unsigned)mine) atomicAdd(&at[v], 1);
+      }
   }
   // exclusive sums: of `below` over the threads, then of the counters
-  auto wave_total = [&](int v) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-  };
-  below = wave_total(below);
-  if (lane == 0) wave_sum_of[wave] = below;
+  for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
+  if (lane == 0) sums[wave] = below;
   __syncthreads();
-  int base = 0;
-  for (int w = 0; w < SORT_WAVES; ++w) base += wave_sum_of[w];
   const int each = (range + SORT_NT - 1) / SORT_NT, c0 = t * each;
-  int count = 0;
+  int run = 0, count = 0;
+  for (int w = 0; w < SORT_WAVES; ++w) run += sums[w];
   for (int v = c0; v < c0 + each && v < mine; ++v) count += at[v];
   int incl = count;
 #pragma unroll
@@ -87,11 +106,10 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
     const int up = __shfl_up(incl, o, 64);
     if (lane >= o) incl += up;
   }
+  if (lane == 63) sums[SORT_WAVES + wave] = incl;
   __syncthreads();
-  if (lane == 63) wave_sum_of[wave] = incl;
-  __syncthreads();
-  int run = base + incl - count;
-  for (int w = 0; w < wave; ++w) run += wave_sum_of[w];
+  run += incl - count;
+  for (int w = 0; w < wave; ++w) run += sums[SORT_WAVES + w];
   for (int v = c0; v < c0 + each && v < mine; ++v) {
     const int c = at[v];
     at[v] = run;
@@ -99,45 +117,55 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
     run += c;
   }
   if (v0 + mine == vocab && c0 < mine && c0 + each >= mine) out.start[vocab] = run;
-  __syncthreads();
-  for (int64_t i0 = 0; i0 < n; i0 += SORT_NT * SORT_IDS) {
-    // this range's tokens among the next ids, in order
-    int v[SORT_IDS], total = 0, before = 0;
-    bool hit[SORT_IDS];
-#pragma unroll
-    for (int k = 0; k < SORT_IDS; ++k) {
-      const int64_t i = i0 + t * SORT_IDS + k;
-      const int id = i < n ? ids[i] : -1;
-      v[k] = id - v0;
-      hit[k] = id >= 0 && (unsigned)v[k] < (unsigned)mine;
-      const uint64_t m = __ballot(hit[k]);
-      before += __popcll(m & (((uint64_t)1 << lane) - 1));
-      total += __popcll(m);
-    }
-    if (lane == 0) wave_sum_of[wave] = total;
+  for (int64_t base = 0; base < n; base += SORT_IDS) {
     __syncthreads();
-    int all = 0;
-    for (int w = 0; w < SORT_WAVES; ++w) {
-      if (w < wave) before += wave_sum_of[w];
-      all += wave_sum_of[w];
-    }
+    if (n > SORT_IDS) load(base);
+    // this range's tokens among these ids, in order
+    int before[SORT_LOADS];
 #pragma unroll
-    for (int k = 0; k < SORT_IDS; ++k)
-      if (hit[k]) {
-        queue_v[before] = v[k];
-        queue_i[before++] = (int)(i0 + t * SORT_IDS + k);
+    for (int l = 0; l < SORT_LOADS; ++l) {
+      int total = 0;
+      before[l] = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t m = __ballot((unsigned)id[l][k] - (unsigned)v0 < (unsigned)mine);
+        before[l] += __popcll(m & (((uint64_t)1 << lane) - 1));
+        total += __popcll(m);
       }
+      if (lane == 0) sums[l * SORT_WAVES + wave] = total;
+    }
+    __syncthreads();
+    // 64 sums, one to a lane: all wavefronts scan them alike
+    static_assert(SORT_LOADS * SORT_WAVES == 64, "a sum to a lane");
+    int scan = sums[lane];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(scan, o, 64);
+      if (lane >= o) scan += up;
+    }
+    const int all = __builtin_amdgcn_readlane(scan, 63);
+#pragma unroll
+    for (int l = 0; l < SORT_LOADS; ++l) {
+      const int slot = l * SORT_WAVES + wave;
+      int q = before[l] + (slot ? __shfl(scan, slot - 1, 64) : 0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned v = (unsigned)id[l][k] - (unsigned)v0;
+        if (v < (unsigned)mine) queue[q++] = v << 14 | ((l * SORT_NT + t) * 4 + k);
+      }
+    }
     __syncthreads();
     for (int q0 = 0; q0 < all; q0 += SORT_NT) {
       const bool live = q0 + t < all;
-      const int mv = live ? queue_v[q0 + t] : -1;
+      const uint32_t e = live ? queue[q0 + t] : 0;
+      const int mv = live ? (int)(e >> 14) : -1;
       // among the wavefront's 64: how many equal ones come before, and who of them stands for all
       int rank = 0, leader = 0, equal = 0;
       uint64_t todo = __ballot(live);
       while (todo) {
-        const int first = __ffsll((unsigned long long)todo) - 1, fv = __shfl(mv, first, 64);
-        const uint64_t m = __ballot(live && mv == fv);
-        if (live && mv == fv) {
+        const int first = __ffsll((unsigned long long)todo) - 1, fv = __builtin_amdgcn_readlane(mv, first);
+        const uint64_t m = __ballot(mv == fv);
+        if (mv == fv) {
           rank = __popcll(m & (((uint64_t)1 << lane) - 1));
           leader = first;
           equal = __popcll(m);
@@ -155,11 +183,10 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
       }
       from = __shfl(from, leader, 64);
       if (live) {
-        out.place[from + rank] = queue_i[q0 + t];
+        out.place[from + rank] = (int)(base + (e & (SORT_IDS - 1)));
         out.token[from + rank] = v0 + mv;
       }
     }
-    __syncthreads();
   }
 }
 
@@ -167,107 +194,187 @@ struct EmbedGrad {
   const void* d_out;
   int64_t ldo;
   EmbedSort sort;
-  int vocab, d, run;                      // run: positions of the sorted list that a workgroup takes
-  int64_t runs;
+  int vocab, d, run;                      // run: positions of the sorted list that are added up by one team
+  int64_t n, runs;
+  int cols, sums;                         // pieces of a row, and workgroups that add up; the others write zeros
   float scale;
   float* d_table;
   int64_t ldt;
   int accumulate;
+  int* owner;                             // [runs]: the token that begins in a run and goes on behind it, or -1
   float* part;                            // [runs][2][d]: a run's share of a token that begins before it, of one that goes on behind it
 };
-__device__ __forceinline__ void add_row(const EmbedGrad& p, int v, int col, const float (&acc)[8]) {
+__device__ __forceinline__ void add_row(const EmbedGrad& p, int v, int col, const float (&acc)[4]) {
   float* at = p.d_table + (int64_t)v * p.ldt + col;
   const int left = p.d - col;
-  float o[8];
-  if (p.accumulate) load8<float>(at, left, o);
+  Piece<float, 4> old;
+  if (p.accumulate) fetch(at, left, old);
+  float o[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = p.accumulate ? o[j] + acc[j] * p.scale : acc[j] * p.scale;
-  put8(at, left, o);
+  for (int j = 0; j < 4; ++j) o[j] = p.accumulate ? value(old, j) + acc[j] * p.scale : acc[j] * p.scale;
+  put(at, left, o);
 }
-// Workgroups below `runs` add up a run of the sorted places each, the others write the zeros of tokens that do not occur.
-// blockIdx.y: 2 048 columns.
-template <typename T>
+// W wavefronts add up the rows of a run of sorted places, NV times four neighbouring columns to a lane (16 bytes of the result, so
+// that a wavefront's stores are whole lines).  The workgroups behind `sums` write the zeros of tokens that do not occur.
+constexpr int ZERO_ROWS = 4;
+template <typename T, int W, int NV>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
-  const int col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 8, left = p.d - col;
-  if ((int64_t)blockIdx.x >= p.runs) {
-    if (left <= 0) return;
-    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int stride = (int)(gridDim.x - p.runs);
-    for (int v = (int)(blockIdx.x - p.runs); v < p.vocab; v += stride)
-      if (!p.sort.start || p.sort.start[v] == p.sort.start[v + 1]) put8(p.d_table + (int64_t)v * p.ldt + col, left, zero);
+  constexpr int TEAM = 64 * W, TEAMS = 4 / W;
+  constexpr bool SHORT = W == 1 && NV == 1;
+  if ((int)blockIdx.x >= p.sums) {
+    const int lane = threadIdx.x & 63, v0 = ((int)blockIdx.x - p.sums) * ZERO_ROWS, v = v0 + lane;
+    uint64_t todo = __ballot(lane < ZERO_ROWS && v < p.vocab && (!p.sort.start || p.sort.start[v] == p.sort.start[v + 1]));
+    const float zero[4] = {0, 0, 0, 0};
+    while (todo) {
+      float* at = p.d_table + (int64_t)(v0 + __ffsll((unsigned long long)todo) - 1) * p.ldt;
+      for (int col = threadIdx.x * 4; col < p.d; col += 1024) put(at + col, p.d - col, zero);
+      todo &= todo - 1;
+    }
     return;
   }
-  const int all = p.sort.start[p.vocab];
-  const int64_t from = (int64_t)blockIdx.x * p.run, to = from + p.run < all ? from + p.run : all;
-  if (from >= to || left <= 0) return;
-  constexpr int U = sizeof(T) == 2 ? 8 : 4;        // rows in flight
-  float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  float* const mine = p.part + (int64_t)blockIdx.x * 2 * p.d + col;
-  int v = p.sort.token[from];
-  const bool begun = p.sort.start[v] < from;       // the run's first token began before it
-  bool first = true;
-  for (int64_t s0 = from; s0 < to; s0 += U) {
-    Eight<T> e[U];
-    int tok[U];
+  const int t = threadIdx.x % TEAM, lane = threadIdx.x & 63;
+  const int group = (int)blockIdx.x / p.cols, c0 = ((int)blockIdx.x - group * p.cols) * (TEAM * 4 * NV) + t * 4;
+  const int64_t run = (int64_t)group * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+  if (run >= p.runs) return;
+  // what the run depends on is asked for at once: behind `all` the lists hold nothing, but there is room up to n
+  const int64_t from = run * p.run;
+  const int all = p.sort.start[p.vocab], earlier = from ? p.sort.token[from - 1] : -1;
+  int place = from + lane < p.n ? p.sort.place[from + lane] : 0, token = from + lane < p.n ? p.sort.token[from + lane] : -1;
+  const int64_t to = from + p.run < all ? from + p.run : all;
+  if (from >= to) {
+    if (c0 == 0) p.owner[run] = -1;
+    return;
+  }
+  const int behind = to < all ? p.sort.token[to] : -1;
+  constexpr int U = NV * sizeof(T) > 4 ? 8 : 16;               // rows in flight
+  float acc[NV][4];
+  auto clear = [&] {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = s0 + u < to;
-      tok[u] = in ? p.sort.token[s0 + u] : -1;
-      const int64_t i = in ? p.sort.place[s0 + u] : 0;
-      fetch8((const T*)p.d_out + i * p.ldo + col, in ? left : 0, e[u]);
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[k][j] = 0.0f;
+  };
+  auto give = [&](int v) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (c0 + k * TEAM * 4 < p.d) add_row(p, v, c0 + k * TEAM * 4, acc[k]);
+  };
+  auto keep = [&](int slot) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int col = c0 + k * TEAM * 4;
+      if (col < p.d) put(p.part + (run * 2 + slot) * p.d + col, p.d - col, acc[k]);
     }
+  };
+  clear();
+  int v = __builtin_amdgcn_readfirstlane(token);
+  bool begun = earlier == v;                     // the sum at hand is of a token that began before the run
+  for (int64_t s0 = from; s0 < to; s0 += 64) {
+    const int here = to - s0 < 64 ? (int)(to - s0) : 64;
+    if (s0 > from) {
+      place = lane < here ? p.sort.place[s0 + lane] : 0;
+      token = lane < here ? p.sort.token[s0 + lane] : -1;
+    }
+    for (int u0 = 0; u0 < here; u0 += U) {
+      Piece<T, 4> e[U][NV];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (tok[u] < 0) continue;
-      if (tok[u] != v) {
-        if (first && begun) put8(mine, left, acc);
-        else add_row(p, v, col, acc);
-        first = false;
-        v = tok[u];
+      for (int u = 0; u < U; ++u) {                // behind the run's end: its last row again
+        const T* row = (const T*)p.d_out + (int64_t)__builtin_amdgcn_readlane(place, u0 + u < here ? u0 + u : here - 1) * p.ldo;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+        for (int k = 0; k < NV; ++k) fetch_row<true, SHORT>(row, c0 + k * TEAM * 4, p.d, e[u][k]);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += value(e[u], j);
+      for (int u = 0; u < U; ++u) {
+        if (u0 + u >= here) break;
+        const int tok = __builtin_amdgcn_readlane(token, u0 + u);
+        if (tok != v) {
+          if (begun) keep(0);
+          else give(v);
+          begun = false;
+          v = tok;
+          clear();
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          settle<SHORT>(c0 + k * TEAM * 4, p.d, e[u][k]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[k][j] += value(e[u][k], j);
+        }
+      }
     }
   }
-  const bool on = p.sort.start[v + 1] > to;        // the last one goes on behind the run
-  if (first && begun) put8(mine, left, acc);
-  else if (on) put8(mine + p.d, left, acc);
-  else add_row(p, v, col, acc);
+  const bool on = !begun && behind == v;
+  if (begun) keep(0);
+  else if (on) keep(1);
+  else give(v);
+  if (c0 == 0) p.owner[run] = on ? v : -1;
 }
-// A token that began in this run and goes on: the shares of the runs that follow, in their order.
+// A token that begins in a run and goes on: the shares of the runs that follow, a quarter of them to a wavefront, joined in their
+// order.  A workgroup has 256 columns of one run's token.
 __global__ __launch_bounds__(256) void k_embed_join(EmbedGrad p) {
-  const int all = p.sort.start[p.vocab], col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 8, left = p.d - col;
-  const int64_t from = (int64_t)blockIdx.x * p.run, to = from + p.run;
-  if (to >= all || left <= 0) return;
-  const int v = p.sort.token[to - 1];
-  if (p.sort.start[v] < from || p.sort.start[v + 1] <= to) return;
-  const int64_t last = (p.sort.start[v + 1] - 1) / p.run;
-  float acc[8];
-  load8<float>(p.part + ((int64_t)blockIdx.x * 2 + 1) * p.d + col, left, acc);
-  constexpr int U = 4;
-  for (int64_t r0 = blockIdx.x + 1; r0 <= last; r0 += U) {
-    float e[U][8];
+  __shared__ float sm[3][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (int)blockIdx.y * 256 + lane * 4, left = p.d - col;
+  const int64_t r = blockIdx.x;
+  const int v = p.owner[r];
+  if (v < 0) return;
+  const int64_t n = (p.sort.start[v + 1] - 1) / p.run - r;
+  const int64_t begin = r + 1 + n * wave / 4, end = r + 1 + n * (wave + 1) / 4;
+  float acc[4];
+  Piece<float, 4> own;
+  fetch(p.part + (r * 2 + 1) * p.d + col, wave == 0 ? left : 0, own);
 #pragma unroll
-    for (int u = 0; u < U; ++u) load8<float>(p.part + (r0 + u) * 2 * p.d + col, r0 + u <= last ? left : 0, e[u]);
+  for (int j = 0; j < 4; ++j) acc[j] = value(own, j);
+  constexpr int U = 8;
+  for (int64_t i = begin; i < end; i += U) {
+    Piece<float, 4> e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(p.part + (i + u) * 2 * p.d + col, i + u < end ? left : 0, e[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += e[u][j];
+      for (int j = 0; j < 4; ++j) acc[j] += value(e[u], j);
   }
-  add_row(p, v, col, acc);
+  if (wave) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sm[wave - 1][lane * 4 + j] = acc[j];
+  }
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += sm[w][lane * 4 + j];
+  if (left > 0) add_row(p, v, col, acc);
+}
+
+// Wavefronts and four-column pieces of a lane that share a run, and from them its positions: at least 16, and as many as leave
+// 1 024 workgroups.
+int team_of(int64_t d) { return d <= 512 ? 1 : 4; }
+int pieces_of(int64_t d) { return d > 256 && d <= 512 ? 2 : 1; }
+int64_t run_of(int64_t n, int64_t d) {
+  const int64_t cols = 256 * team_of(d) * pieces_of(d), groups = 1024 * (4 / team_of(d)) / ((d + cols - 1) / cols);
+  const int64_t r = (n + groups - 1) / (groups < 1 ? 1 : groups);
+  return r < 16 ? 16 : r;
+}
+int64_t runs_of(int64_t n, int64_t d) { return (n + run_of(n, d) - 1) / run_of(n, d); }
+
+template <typename T, int W, int NV>
+int launch_embed_sum(EmbedGrad p, hipStream_t s) {
+  constexpr int TEAMS = 4 / W, COLS = 64 * W * 4 * NV;
+  p.cols = (p.d + COLS - 1) / COLS;
+  p.sums = (int)((p.runs + TEAMS - 1) / TEAMS) * p.cols;
+  const int zeros = p.accumulate ? 0 : (p.vocab + ZERO_ROWS - 1) / ZERO_ROWS;
+  hipLaunchKernelGGL((k_embed_sum<T, W, NV>), dim3((unsigned)(p.sums + zeros)), dim3(256), 0, s, p);
+  return launch_status("embedding_backward");
+}
+template <typename T>
+int launch_embed_sums(const EmbedGrad& p, hipStream_t s) {
+  if (team_of(p.d) == 1) return pieces_of(p.d) == 1 ? launch_embed_sum<T, 1, 1>(p, s) : launch_embed_sum<T, 1, 2>(p, s);
+  return launch_embed_sum<T, 4, 1>(p, s);
 }
 
 constexpr int64_t kTokensMax = 1 << 30, kVocabMax = 1 << 20, kWidthMax = 1 << 20;
 int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
-// positions of a run, and runs: at least 16 rows, at most 2 048 runs
-int run_of(int64_t n) {
-  const int64_t r = (n + 2047) / 2048;
-  return (int)(r < 16 ? 16 : r);
-}
-int64_t runs_of(int64_t n) { return (n + run_of(n) - 1) / run_of(n); }
-
 int check_embedding(const char* who, int64_t n, int64_t vocab, int64_t d, int dtype) {
   if (dtype != AE_F32 && dtype != AE_BF16) return fail(AE_EINVAL, "%s: bad dtype", who);
   if (n < 0 || n > kTokensMax) return fail(AE_EINVAL, "%s: tokens must be 0 .. 2^30", who);
@@ -318,7 +425,7 @@ extern "C" int model_embedding_backward_workspace(int64_t n, int64_t vocab, int6
   using namespace ae;
   if (!bytes) return fail(AE_EINVAL, "model_embedding_backward_workspace: null argument");
   AE_TRY(check_embedding("model_embedding_backward_workspace", n, vocab, d, dtype));
-  *bytes = n == 0 ? 0 : 2 * align16(n * 4) + align16((vocab + 1) * 4) + runs_of(n) * 2 * d * 4;
+  *bytes = n == 0 ? 0 : 2 * align16(n * 4) + align16((vocab + 1) * 4) + align16(runs_of(n, d) * 4) + runs_of(n, d) * 2 * d * 4;
   return AE_OK;
 }
 
@@ -339,23 +446,18 @@ extern "C" int model_embedding_backward(const void* d_out, int64_t ldo, const in
     return AE_OK;
   }
   char* ws = (char*)workspace;
-  EmbedGrad p = {d_out, ldo, {}, (int)vocab, (int)d, run_of(n), runs_of(n), scale, d_table, ldt, accumulate ? 1 : 0, nullptr};
-  const unsigned cols = (unsigned)((d + 2047) / 2048);
-  const int64_t zeros = accumulate ? 0 : (vocab < 4096 ? vocab : 4096);
-  if (n == 0) {
-    p.runs = 0;
-    hipLaunchKernelGGL((k_embed_sum<float>), dim3((unsigned)zeros, cols), dim3(256), 0, s, p);
-    return launch_status("embedding_backward");
-  }
+  EmbedGrad p = {d_out, ldo, {}, (int)vocab, (int)d, (int)run_of(n, d), n, runs_of(n, d), 0, 0, scale, d_table, ldt, accumulate ? 1 : 0, nullptr, nullptr};
+  if (n == 0) return launch_embed_sums<float>(p, s);       // zeros alone
   p.sort.place = (int*)ws;
   p.sort.token = (int*)(ws + align16(n * 4));
   p.sort.start = (int*)(ws + 2 * align16(n * 4));
-  p.part = (float*)(ws + 2 * align16(n * 4) + align16((vocab + 1) * 4));
+  p.owner = (int*)(ws + 2 * align16(n * 4) + align16((vocab + 1) * 4));
+  p.part = (float*)((char*)p.owner + align16(p.runs * 4));
   const int range = (int)((vocab + 255) / 256);
   static_assert(kVocabMax / 256 <= SORT_RANGE, "a range's counters fit into LDS");
   hipLaunchKernelGGL(k_embed_sort, dim3((unsigned)((vocab + range - 1) / range)), dim3(SORT_NT), 0, s, ids, n, (int)vocab, range, p.sort);
-  if (dtype == AE_BF16) hipLaunchKernelGGL((k_embed_sum<bf16_t>), dim3((unsigned)(p.runs + zeros), cols), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((k_embed_sum<float>), dim3((unsigned)(p.runs + zeros), cols), dim3(256), 0, s, p);
-  if (p.runs > 1) hipLaunchKernelGGL(k_embed_join, dim3((unsigned)(p.runs - 1), cols), dim3(256), 0, s, p);
+  AE_TRY(dtype == AE_BF16 ? launch_embed_sums<bf16_t>(p, s) : launch_embed_sums<float>(p, s));
+  if (p.runs > 1)
+    hipLaunchKernelGGL(k_embed_join, dim3((unsigned)(p.runs - 1), (unsigned)((d + 255) / 256)), dim3(256), 0, s, p);
   return launch_status("embedding_backward");
 }

@@ -12,7 +12,7 @@
 namespace ae {
 namespace {
 
-constexpr int NT = 256;
+constexpr int NT = 512;
 // a column's word: bits 0 .. 19 how often among the answers, bit 20 in the prompt, bits 21 .. 31 place in the list of biases + 1
 constexpr uint32_t kCount = (1u << 20) - 1, kPrompt = 1u << 20, kSeen = kCount | kPrompt;
 constexpr int kBiasAt = 21, kMaxHistory = kCount, kMaxBias = 2047;
@@ -37,20 +37,22 @@ struct AdjustArgs {
 
 template <typename T, int NP, bool LISTS>
 __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
-  constexpr int S = NT * 8 * NP;                 // columns of a slice
+  constexpr int VEC = 16 / sizeof(T), S = NT * VEC * NP;       // elements of a piece, columns of a slice
+  constexpr uint32_t ALL = (1u << VEC) - 1;
   __shared__ uint4 word4[LISTS ? S / 4 : 1];
   uint32_t* const word = (uint32_t*)word4;
   const int64_t at = p.first + blockIdx.x, row = at / p.slices;
   const int s0 = (int)(at - row * p.slices) * S, mine = p.vocab - s0 < S ? p.vocab - s0 : S;
   const T* z = (const T*)p.logits + row * p.ld + s0;
-  Eight<T> e[NP];
+  Piece<T, VEC> e[NP];
   uint32_t ok[NP];
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
-    const int c = (k * NT + (int)threadIdx.x) * 8;
-    fetch8(z + c, mine - c, e[k]);
-    ok[k] = 0xFF;
-    if (p.allowed && c < mine) ok[k] = p.allowed[row * ((p.vocab + 31) / 32) + (s0 + c) / 32] >> (c & 31) & 0xFF;
+    const int c = (k * NT + (int)threadIdx.x) * VEC;
+    if (mine == S) fetch_whole<true>(z + c, e[k]);
+    else fetch_row<true, true>(z - s0, s0 + c, p.vocab, e[k]);
+    ok[k] = ALL;
+    if (p.allowed && c < mine) ok[k] = p.allowed[row * ((p.vocab + 31) / 32) + (s0 + c) / 32] >> (c & 31) & ALL;
   }
   float repetition = 1.0f, presence = 0.0f, frequency = 0.0f;
   if constexpr (LISTS) {
@@ -76,37 +78,44 @@ __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
   const bool in_place = p.logits == p.out;
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
-    const int c = (k * NT + (int)threadIdx.x) * 8;
+    const int c = (k * NT + (int)threadIdx.x) * VEC;
     if (c >= mine) continue;
-    float v[8];
+    if (mine < S) settle<true>(s0 + c, p.vocab, e[k]);
+    float v[VEC];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = value(e[k], j);
+    for (int j = 0; j < VEC; ++j) v[j] = value(e[k], j);
     if constexpr (LISTS) {
-      const uint4 a = word4[c / 4], b = word4[c / 4 + 1];
-      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-      const bool touched = (a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w) != 0;
-      if (in_place && !touched && ok[k] == 0xFF) continue;      // stays as it is
+      uint32_t w[VEC], any = 0;
+#pragma unroll
+      for (int j = 0; j < VEC; j += 4) {
+        const uint4 a = word4[(c + j) / 4];
+        w[j] = a.x; w[j + 1] = a.y; w[j + 2] = a.z; w[j + 3] = a.w;
+        any |= a.x | a.y | a.z | a.w;
+      }
+      const bool touched = any != 0;
+      if (in_place && !touched && ok[k] == ALL) continue;      // stays as it is
       if (touched) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < VEC; ++j) {
           if (w[j] & kSeen) v[j] = v[j] > 0.0f ? v[j] / repetition : v[j] * repetition;
           if (w[j] & kCount) v[j] = v[j] - frequency * (float)(w[j] & kCount) - presence;
           if (w[j] >> kBiasAt) v[j] += p.bias[row * p.n_bias + (w[j] >> kBiasAt) - 1];
         }
       }
     } else {
-      if (in_place && ok[k] == 0xFF) continue;
+      if (in_place && ok[k] == ALL) continue;
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < VEC; ++j)
       if (!(ok[k] >> j & 1)) v[j] = -INFINITY;
-    put8((T*)p.out + row * p.ldo + s0 + c, mine - c, v);
+    if (mine == S) put_whole<false>((T*)p.out + row * p.ldo + s0 + c, v);
+    else put((T*)p.out + row * p.ldo + s0 + c, mine - c, v);
   }
 }
 
 template <typename T, int NP, bool LISTS>
 int launch_adjust(AdjustArgs p, hipStream_t s) {
-  constexpr int S = NT * 8 * NP;
+  constexpr int S = NT * 16 / (int)sizeof(T) * NP;
   p.slices = (p.vocab + S - 1) / S;
   const int64_t all = p.rows * p.slices, most = launch_blocks(NT);
   for (; p.first < all; p.first += most) {
@@ -117,9 +126,10 @@ int launch_adjust(AdjustArgs p, hipStream_t s) {
 }
 template <typename T>
 int launch_adjust_rows(const AdjustArgs& p, hipStream_t s) {
-  if (!p.n_history && !p.n_bias) return launch_adjust<T, 2, false>(p, s);
-  if (p.rows * ((p.vocab + 4095) / 4096) < 1024) return launch_adjust<T, 1, true>(p, s);
-  return launch_adjust<T, 4, true>(p, s);
+  constexpr int E = sizeof(T) / 2;               // pieces for 4 096 columns
+  if (!p.n_history && !p.n_bias) return launch_adjust<T, 2 * E, false>(p, s);
+  if (p.rows * ((p.vocab + 4095) / 4096) < 1024) return launch_adjust<T, E, true>(p, s);
+  return launch_adjust<T, 2 * E, true>(p, s);
 }
 
 }  // namespace

@@ -9,6 +9,7 @@
 
 #include "ae_device.h"
 #include "ae_fp8.h"
+#include "ae_rows.h"
 #include "ae_internal.h"
 
 namespace ae {
@@ -16,14 +17,28 @@ namespace {
 
 constexpr float kDown = 7.8886090522101181e-31f;   // 2^-100
 
-// sum over the W wavefronts that share a row; sm is not written again before the workgroup's next barrier but one
-template <int W>
+// eight elements as numbers, zeros behind the row's end
+template <typename T>
+__device__ __forceinline__ void numbers(const T* p, int left, float (&v)[8]) {
+  Eight<T> e;
+  fetch(p, left, e);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = value(e, i);
+}
+
+// sum over the lanes that share a row: 16, 32 or 64 of a wavefront, or several wavefronts; sm is not written again before the
+// workgroup's next barrier but one
+template <int LANES>
 __device__ __forceinline__ float team_sum(float v, float* sm) {
-  v = sum_rows(sum16(v));
-  if constexpr (W == 1) return v;
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return sum_of<W>(sm);
+  v = sum16(v);
+  if constexpr (LANES == 32) return v + __shfl_xor(v, 16, 64);
+  if constexpr (LANES >= 64) v = sum_rows(v);
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sum_of<LANES / 64>(sm);
+  }
+  return v;
 }
 
 struct NormArgs {
@@ -42,13 +57,14 @@ struct NormArgs {
   uint8_t* q;
   int64_t ldq;
   float* scale;
+  bool stream;
 };
 
-// eight results of a row from column col on; the 16 lanes of a block of 128 come here together
+// eight results of a row from column col on (behind the row's end: none); the 16 lanes of a block of 128 come here together
 template <typename T>
 __device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, const float (&y)[8]) {
   const int left = p.d - col;
-  if (p.y && left > 0) put8((T*)p.y + row * p.ldy + col, left, y);
+  if (p.y && left > 0) put((T*)p.y + row * p.ldy + col, left, y);
   if (!p.q) return;
   float m = 0.0f;
 #pragma unroll
@@ -79,73 +95,81 @@ __device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, co
 // 1 / sqrt(mean + eps) of a row; down: of the row times 2^-100, whose mean is so large that eps plays no part
 __device__ __forceinline__ float rms_inverse(float sum, int d, float eps, bool down) { return 1.0f / sqrtf(sum / (float)d + (down ? 0.0f : eps)); }
 
-// W wavefronts hold a row in NV pieces of eight elements per lane; with W = 1 a workgroup has four rows at a time.
-template <typename T, int W, int NV>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_rms_norm(NormArgs p) {
-  constexpr int TEAM = 64 * W, TEAMS = W == 1 ? 4 : 1;
+// LANES lanes hold a row in NV pieces of eight elements each; a workgroup has 256 / LANES rows at a time, or one.
+template <typename T, int LANES, int NV, bool STREAM>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs p) {
+  constexpr int TEAMS = LANES < 256 ? 256 / LANES : 1, W = LANES / 64 ? LANES / 64 : 1;
+  constexpr bool SHORT = LANES == 16;
   __shared__ float sm[3][W];
-  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, step = (int)gridDim.x * TEAMS;
+  const int t = threadIdx.x % LANES, team = threadIdx.x / LANES, step = (int)gridDim.x * TEAMS;
   const T* x = (const T*)p.x;
   const T* res = (const T*)p.residual;
-  float w[NV][8];
+  Eight<float> w[NV];
+  if (p.weight) {
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int col = (v * TEAM + t) * 8, left = p.d - col;
+    for (int v = 0; v < NV; ++v) fetch_row<false, SHORT>(p.weight, (v * LANES + t) * 8, p.d, w[v]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[v][j] = 1.0f;
-    if (p.weight) load8<float>(p.weight + col, left, w[v]);
+    for (int v = 0; v < NV; ++v) settle<SHORT>((v * LANES + t) * 8, p.d, w[v]);
   }
-  Eight<T> xe[NV], re[NV];
-  auto fetch = [&](int64_t row) {
+  int turn = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < p.rows; row0 += step, turn ^= 1) {
+    const int64_t row = row0 + team;
+    const bool live = row < p.rows;                // the rows of a wavefront go together
+    Eight<T> xe[NV], re[NV];
+    const int64_t at = live ? row : p.rows - 1;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * TEAM + t) * 8, left = p.d - col;
-      fetch8(x + row * p.ldx + col, left, xe[v]);
-      if (res) fetch8(res + row * p.ldr + col, left, re[v]);
+    for (int v = 0; v < NV; ++v) fetch_row<STREAM, SHORT>(x + at * p.ldx, (v * LANES + t) * 8, p.d, xe[v]);
+    if (res) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) fetch_row<STREAM, SHORT>(res + at * p.ldr, (v * LANES + t) * 8, p.d, re[v]);
     }
-  };
-  int64_t row = (int64_t)blockIdx.x * TEAMS + team;
-  if (row < p.rows) fetch(row);
-  for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
     float h[NV][8], sum = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + t) * 8;
+      settle<SHORT>(col, p.d, xe[v]);
+      if (res) settle<SHORT>(col, p.d, re[v]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         h[v][j] = value(xe[v], j);
         if (res) h[v][j] += value(re[v], j);
         sum = fmaf(h[v][j], h[v][j], sum);
       }
-    if (row + step < p.rows) fetch(row + step);
-    if (p.h) {
+    }
+    if (p.h && live) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int col = (v * TEAM + t) * 8;
-        if (col < p.d) put8((T*)p.h + row * p.ldh + col, p.d - col, h[v]);
+        const int col = (v * LANES + t) * 8;
+        if (col < p.d) put<STREAM>((T*)p.h + row * p.ldh + col, p.d - col, h[v]);
       }
     }
-    sum = team_sum<W>(sum, sm[turn]);
+    sum = team_sum<LANES>(sum, sm[turn]);
     const bool down = !(sum <= FLT_MAX);           // the same in all threads of the row
-    if (down) {
+    if (LANES <= 64 ? __any(down) : down) {        // of several rows in a wavefront the others are multiplied by one
+      const float by = down ? kDown : 1.0f;
       sum = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          h[v][j] *= kDown;
+          h[v][j] *= by;
           sum = fmaf(h[v][j], h[v][j], sum);
         }
-      if constexpr (W > 1) __syncthreads();
-      sum = team_sum<W>(sum, sm[2]);
-      if constexpr (W > 1) __syncthreads();
+      if constexpr (LANES > 64) __syncthreads();
+      sum = team_sum<LANES>(sum, sm[2]);
+      if constexpr (LANES > 64) __syncthreads();
     }
     const float r = rms_inverse(sum, p.d, p.eps, down);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = h[v][j] * r * w[v][j];
-      emit<T>(p, row, (v * TEAM + t) * 8, y);
+      for (int j = 0; j < 8; ++j) y[j] = h[v][j] * r;
+      if (p.weight) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] *= value(w[v], j);
+      }
+      emit<T>(p, row, live ? (v * LANES + t) * 8 : p.d, y);
     }
   }
 }
@@ -161,8 +185,8 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     auto load = [&](int col, float by, float (&h)[8]) {
       float r8[8];
-      load8<T>(x + row * p.ldx + col, p.d - col, h);
-      if (res) load8<T>(res + row * p.ldr + col, p.d - col, r8);
+      numbers(x + row * p.ldx + col, p.d - col, h);
+      if (res) numbers(res + row * p.ldr + col, p.d - col, r8);
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[j] = (res ? h[j] + r8[j] : h[j]) * by;
     };
@@ -175,9 +199,9 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
       }
       return sum;
     };
-    float sum = team_sum<WIDE / 64>(squares(1.0f), sm[0]);
+    float sum = team_sum<WIDE>(squares(1.0f), sm[0]);
     const bool down = !(sum <= FLT_MAX);
-    if (down) sum = team_sum<WIDE / 64>(squares(kDown), sm[1]);
+    if (down) sum = team_sum<WIDE>(squares(kDown), sm[1]);
     const float r = rms_inverse(sum, p.d, p.eps, down);
     for (int c0 = 0; c0 < p.d; c0 += WIDE * 8) {           // all threads: a block's lanes meet in emit
       const int col = c0 + threadIdx.x * 8;
@@ -185,8 +209,8 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
       load(col, 1.0f, h);
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = 1.0f;
-      if (p.weight) load8<float>(p.weight + col, p.d - col, w);
-      if (p.h && col < p.d) put8((T*)p.h + row * p.ldh + col, p.d - col, h);
+      if (p.weight) numbers(p.weight + col, p.d - col, w);
+      if (p.h && col < p.d) put((T*)p.h + row * p.ldh + col, p.d - col, h);
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = (down ? h[j] * kDown : h[j]) * r * w[j];
       emit<T>(p, row, col, y);
@@ -195,22 +219,23 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
   }
 }
 
-template <typename T, int W, int NV>
+template <typename T, int LANES, int NV>
 int launch_norm_row(const NormArgs& p, hipStream_t s) {
-  constexpr int TEAMS = W == 1 ? 4 : 1;
-  const int64_t want = (p.rows + TEAMS - 1) / TEAMS, most = 256 * (W <= 4 ? 8 : 32 / W);
-  hipLaunchKernelGGL((k_rms_norm<T, W, NV>), dim3((unsigned)(want < most ? want : most)), dim3(W == 1 ? 256 : 64 * W), 0, s, p);
+  constexpr int TEAMS = LANES < 256 ? 256 / LANES : 1;
+  const int64_t want = (p.rows + TEAMS - 1) / TEAMS, most = 1 << 20;
+  hipLaunchKernelGGL((p.stream ? k_rms_norm<T, LANES, NV, true> : k_rms_norm<T, LANES, NV, false>), dim3((unsigned)(want < most ? want : most)), dim3(LANES < 256 ? 256 : LANES), 0, s, p);
   return launch_status("rms_norm");
 }
 template <typename T>
 int launch_norm(const NormArgs& p, hipStream_t s) {
-  if (p.d <= 512) return launch_norm_row<T, 1, 1>(p, s);
-  if (p.d <= 1024) return launch_norm_row<T, 1, 2>(p, s);
-  if (p.d <= 2048) return launch_norm_row<T, 4, 1>(p, s);
-  if (p.d <= 4096) return launch_norm_row<T, 4, 2>(p, s);
-  if (p.d <= 8192) return launch_norm_row<T, 8, 2>(p, s);
-  if (p.d <= 16384) return launch_norm_row<T, 16, 2>(p, s);
-  if (p.d <= 32768) return launch_norm_row<T, 16, 4>(p, s);
+  if (p.d <= 128) return launch_norm_row<T, 16, 1>(p, s);
+  if (p.d <= 256) return launch_norm_row<T, 32, 1>(p, s);
+  if (p.d <= 512) return launch_norm_row<T, 64, 1>(p, s);
+  if (p.d <= 1024) return launch_norm_row<T, 64, 2>(p, s);
+  if (p.d <= 2048) return launch_norm_row<T, 256, 1>(p, s);
+  if (p.d <= 4096) return launch_norm_row<T, 256, 2>(p, s);
+  if (p.d <= 8192) return launch_norm_row<T, 512, 2>(p, s);
+  if (p.d <= 16384) return launch_norm_row<T, 1024, 2>(p, s);
   const int64_t most = 512;
   hipLaunchKernelGGL((k_rms_norm_wide<T>), dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(WIDE), 0, s, p);
   return launch_status("rms_norm");
@@ -230,64 +255,79 @@ struct NormGradArgs {
   float eps;
   void* dx;
   int64_t lddx;
-  float* part;                            // [teams][d]: each team's sum of dy u over its rows; null: not wanted
+  float* part;                            // [workgroups][d]: each one's sum of dy u over its rows; null: not wanted
   float* stat;                            // [rows][4], rows that registers do not hold
+  bool stream;
 };
 
 // u = h times down (1 or 2^-100) times r; the gradient's common factor is r times down
 struct RowStat {
   float r, down, mean;                    // mean(g u)
 };
-template <int W>
 __device__ __forceinline__ RowStat row_stat(float hh, float gh, int d, float eps, bool down) {
   const float r = rms_inverse(hh, d, eps, down);
   return {r, down ? kDown : 1.0f, r * gh / (float)d};
 }
 
-template <typename T, int W, int NV>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_rms_norm_grad(NormGradArgs p) {
-  constexpr int TEAM = 64 * W, TEAMS = W == 1 ? 4 : 1;
+template <typename T, int LANES, int NV, bool STREAM>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(NormGradArgs p) {
+  constexpr int TEAMS = LANES < 256 ? 256 / LANES : 1, W = LANES / 64 ? LANES / 64 : 1;
+  constexpr bool SHORT = LANES == 16;
   __shared__ float sm[3][2][W];
-  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, step = (int)gridDim.x * TEAMS;
+  __shared__ float join[TEAMS > 1 ? TEAMS - 1 : 1][TEAMS > 1 ? NV * LANES * 8 : 1];
+  const int t = threadIdx.x % LANES, team = threadIdx.x / LANES, step = (int)gridDim.x * TEAMS;
   float w[NV][8], acc[NV][8];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int col = (v * TEAM + t) * 8;
+    const int col = (v * LANES + t) * 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) { w[v][j] = 1.0f; acc[v][j] = 0.0f; }
-    if (p.weight) load8<float>(p.weight + col, p.d - col, w[v]);
+    if (p.weight) numbers(p.weight + col, p.d - col, w[v]);
   }
   Eight<T> he[NV], ge[NV], re[NV];
-  auto fetch = [&](int64_t row) {
+  auto ask = [&](int64_t row) {
+    const int64_t at = row < p.rows ? row : p.rows - 1;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * TEAM + t) * 8, left = p.d - col;
-      fetch8((const T*)p.h + row * p.ldh + col, left, he[v]);
-      fetch8((const T*)p.dy + row * p.ldy + col, left, ge[v]);
-      if (p.d_h) fetch8((const T*)p.d_h + row * p.ldg + col, left, re[v]);
+      fetch_row<STREAM, SHORT>((const T*)p.h + at * p.ldh, (v * LANES + t) * 8, p.d, he[v]);
+      fetch_row<STREAM, SHORT>((const T*)p.dy + at * p.ldy, (v * LANES + t) * 8, p.d, ge[v]);
+    }
+    if (p.d_h) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) fetch_row<STREAM, SHORT>((const T*)p.d_h + at * p.ldg, (v * LANES + t) * 8, p.d, re[v]);
     }
   };
-  const int64_t first = (int64_t)blockIdx.x * TEAMS + team;
-  if (first < p.rows) fetch(first);
+  int64_t row0 = (int64_t)blockIdx.x * TEAMS;
+  if (row0 < p.rows) ask(row0 + team);
   int turn = 0;
-  for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
+  for (; row0 < p.rows; row0 += step, turn ^= 1) {
+    const int64_t row = row0 + team;
+    const bool live = row < p.rows;                // the rows of a wavefront go together
     float h[NV][8], dy[NV][8], add[NV][8], hh = 0.0f, gh = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + t) * 8;
+      settle<SHORT>(col, p.d, he[v]);
+      settle<SHORT>(col, p.d, ge[v]);
+      if (p.d_h) settle<SHORT>(col, p.d, re[v]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         h[v][j] = value(he[v], j);
-        dy[v][j] = value(ge[v], j);
+        dy[v][j] = live ? value(ge[v], j) : 0.0f;
         add[v][j] = p.d_h ? value(re[v], j) : 0.0f;
         hh = fmaf(h[v][j], h[v][j], hh);
         gh = fmaf(dy[v][j] * w[v][j], h[v][j], gh);
       }
-    if (row + step < p.rows) fetch(row + step);
+    }
+    if (row0 + step < p.rows) ask(row + step);
     // both sums at one barrier
     auto sums = [&](float (&s2)[2][W]) {
-      hh = sum_rows(sum16(hh));
-      gh = sum_rows(sum16(gh));
-      if constexpr (W > 1) {
+      if constexpr (LANES <= 64) {
+        hh = team_sum<LANES>(hh, nullptr);
+        gh = team_sum<LANES>(gh, nullptr);
+      } else {
+        hh = sum_rows(sum16(hh));
+        gh = sum_rows(sum16(gh));
         if ((threadIdx.x & 63) == 0) { s2[0][threadIdx.x >> 6] = hh; s2[1][threadIdx.x >> 6] = gh; }
         __syncthreads();
         hh = sum_of<W>(s2[0]);
@@ -296,39 +336,57 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_rms_norm_grad(NormGra
     };
     sums(sm[turn]);
     const bool down = !(hh <= FLT_MAX) || !(fabsf(gh) <= FLT_MAX);
-    if (down) {
+    if (LANES <= 64 ? __any(down) : down) {        // of several rows in a wavefront the others are multiplied by one
+      const float by = down ? kDown : 1.0f;
       hh = gh = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          h[v][j] *= kDown;
+          h[v][j] *= by;
           hh = fmaf(h[v][j], h[v][j], hh);
           gh = fmaf(dy[v][j] * w[v][j], h[v][j], gh);
         }
-      if constexpr (W > 1) __syncthreads();
+      if constexpr (LANES > 64) __syncthreads();
       sums(sm[2]);
-      if constexpr (W > 1) __syncthreads();
+      if constexpr (LANES > 64) __syncthreads();
     }
-    const RowStat st = row_stat<W>(hh, gh, p.d, p.eps, down);
+    const RowStat st = row_stat(hh, gh, p.d, p.eps, down);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * TEAM + t) * 8;
+      const int col = (v * LANES + t) * 8;
       float o[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float u = h[v][j] * st.r;
-        acc[v][j] = fmaf(dy[v][j], u, acc[v][j]);
+        if (live) acc[v][j] = fmaf(dy[v][j], u, acc[v][j]);
         o[j] = (dy[v][j] * w[v][j] - u * st.mean) * st.r * st.down + add[v][j];
       }
-      if (p.dx && col < p.d) put8((T*)p.dx + row * p.lddx + col, p.d - col, o);
+      if (p.dx && live && col < p.d) put((T*)p.dx + row * p.lddx + col, p.d - col, o);
     }
   }
   if (!p.part) return;
+  // the rows that a workgroup has at a time: added in their order
+  if constexpr (TEAMS > 1) {
+    if (team) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) join[team - 1][(v * 8 + j) * LANES + t] = acc[v][j];
+    }
+    __syncthreads();
+    if (team) return;
+#pragma unroll
+    for (int k = 0; k < TEAMS - 1; ++k)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[v][j] += join[k][(v * 8 + j) * LANES + t];
+  }
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int col = (v * TEAM + t) * 8;
-    if (col < p.d) put8(p.part + first * p.d + col, p.d - col, acc[v]);
+    const int col = (v * LANES + t) * 8;
+    if (col < p.d) put(p.part + (int64_t)blockIdx.x * p.d + col, p.d - col, acc[v]);
   }
 }
 
@@ -342,9 +400,9 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
       hh = gh = 0.0f;
       for (int col = threadIdx.x * 8; col < p.d; col += WIDE * 8) {
         float h[8], g[8], w[8];
-        load8<T>((const T*)p.h + row * p.ldh + col, p.d - col, h);
-        load8<T>((const T*)p.dy + row * p.ldy + col, p.d - col, g);
-        if (p.weight) load8<float>(p.weight + col, p.d - col, w);
+        numbers((const T*)p.h + row * p.ldh + col, p.d - col, h);
+        numbers((const T*)p.dy + row * p.ldy + col, p.d - col, g);
+        if (p.weight) numbers(p.weight + col, p.d - col, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           h[j] *= by;
@@ -354,15 +412,15 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
       }
     };
     sums(1.0f);
-    hh = team_sum<WIDE / 64>(hh, sm[0]);
-    gh = team_sum<WIDE / 64>(gh, sm[1]);
+    hh = team_sum<WIDE>(hh, sm[0]);
+    gh = team_sum<WIDE>(gh, sm[1]);
     const bool down = !(hh <= FLT_MAX) || !(fabsf(gh) <= FLT_MAX);
     if (down) {
       sums(kDown);
-      hh = team_sum<WIDE / 64>(hh, sm[2]);
-      gh = team_sum<WIDE / 64>(gh, sm[3]);
+      hh = team_sum<WIDE>(hh, sm[2]);
+      gh = team_sum<WIDE>(gh, sm[3]);
     }
-    const RowStat st = row_stat<1>(hh, gh, p.d, p.eps, down);
+    const RowStat st = row_stat(hh, gh, p.d, p.eps, down);
     if (threadIdx.x == 0) {
       float* at = p.stat + row * 4;
       at[0] = st.r; at[1] = st.down; at[2] = st.mean;
@@ -378,74 +436,73 @@ __global__ __launch_bounds__(256) void k_rms_norm_grad_columns(NormGradArgs p) {
   float w[8], acc[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) { w[j] = 1.0f; acc[j] = 0.0f; }
-  if (p.weight) load8<float>(p.weight + col, left, w);
+  if (p.weight) numbers(p.weight + col, left, w);
   for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
     const RowStat st = {p.stat[row * 4], p.stat[row * 4 + 1], p.stat[row * 4 + 2]};
     float h[8], dy[8], add[8], o[8];
-    load8<T>((const T*)p.h + row * p.ldh + col, left, h);
-    load8<T>((const T*)p.dy + row * p.ldy + col, left, dy);
-    if (p.d_h) load8<T>((const T*)p.d_h + row * p.ldg + col, left, add);
+    numbers((const T*)p.h + row * p.ldh + col, left, h);
+    numbers((const T*)p.dy + row * p.ldy + col, left, dy);
+    if (p.d_h) numbers((const T*)p.d_h + row * p.ldg + col, left, add);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float u = h[j] * st.down * st.r;
       acc[j] = fmaf(dy[j], u, acc[j]);
       o[j] = (dy[j] * w[j] - u * st.mean) * st.r * st.down + (p.d_h ? add[j] : 0.0f);
     }
-    if (p.dx) put8((T*)p.dx + row * p.lddx + col, left, o);
+    if (p.dx) put((T*)p.dx + row * p.lddx + col, left, o);
   }
-  if (p.part) put8(p.part + (int64_t)blockIdx.y * p.d + col, left, acc);
+  if (p.part) put(p.part + (int64_t)blockIdx.y * p.d + col, left, acc);
 }
 
-// dw[j] = sum of n parts in a fixed order: 16 wavefronts take every 16th part of 64 columns each
+// dw[j] = sum of n parts in a fixed order: 64 groups of 16 lanes take every 64th part of 16 columns
 __global__ __launch_bounds__(1024) void k_sum_parts(const float* __restrict__ part, int64_t n, int d, float* __restrict__ out) {
-  __shared__ float sm[16][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, col = (int)blockIdx.x * 64 + lane;
+  __shared__ float sm[64][17];
+  const int lane = threadIdx.x & 15, g = threadIdx.x >> 4, col = (int)blockIdx.x * 16 + lane;
   float acc = 0.0f;
   if (col < d) {
     constexpr int U = 8;
-    for (int64_t i0 = g; i0 < n; i0 += 16 * U) {
+    for (int64_t i0 = g; i0 < n; i0 += 64 * U) {
       float v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = i0 + 16 * u < n ? part[(i0 + 16 * u) * d + col] : 0.0f;
+      for (int u = 0; u < U; ++u) v[u] = i0 + 64 * u < n ? part[(i0 + 64 * u) * d + col] : 0.0f;
 #pragma unroll
       for (int u = 0; u < U; ++u) acc += v[u];
     }
   }
   sm[g][lane] = acc;
   __syncthreads();
-  if (g == 0 && col < d) {
-#pragma unroll
-    for (int i = 1; i < 16; ++i) acc += sm[i][lane];
-    out[col] = acc;
-  }
+  if (threadIdx.x >= 256) return;
+  const int c = threadIdx.x >> 4, k = threadIdx.x & 15;        // 16 lanes to a column
+  acc = sum16(sm[4 * k][c] + sm[4 * k + 1][c] + (sm[4 * k + 2][c] + sm[4 * k + 3][c]));
+  if (k == 0 && (int)blockIdx.x * 16 + c < d) out[blockIdx.x * 16 + c] = acc;
 }
 
-constexpr int kInRegisters = 32768;                // columns
-// teams of a launch, each with a part of the weight's gradient
-int64_t grad_teams(int64_t rows, int64_t d) {
+constexpr int kInRegisters = 8192;                 // columns of a row, beside its gradient and the sums of the weight's
+// workgroups of a launch, each with a part of the weight's gradient
+int64_t grad_groups(int64_t rows, int64_t d) {
   if (d > kInRegisters) return rows < 64 ? rows : 64;
-  const int64_t most = d <= 1024 ? 256 * 4 * 4 : d <= 4096 ? 256 * 4 : 512;
-  const int64_t teams = d <= 1024 ? (rows + 3) / 4 * 4 : rows;
-  return teams < most ? teams : most;
+  const int64_t teams = d <= 128 ? 16 : d <= 256 ? 8 : d <= 1024 ? 4 : 1;
+  const int64_t want = (rows + teams - 1) / teams, most = d <= 512 || (d > 1024 && d <= 2048) ? 1024 : d <= 4096 ? 512 : 256;
+  return want < most ? want : most;
 }
 int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
 
-template <typename T, int W, int NV>
-int launch_grad_row(const NormGradArgs& p, int64_t teams, hipStream_t s) {
-  hipLaunchKernelGGL((k_rms_norm_grad<T, W, NV>), dim3((unsigned)(W == 1 ? teams / 4 : teams)), dim3(W == 1 ? 256 : 64 * W), 0, s, p);
+template <typename T, int LANES, int NV>
+int launch_grad_row(const NormGradArgs& p, int64_t groups, hipStream_t s) {
+  hipLaunchKernelGGL((p.stream ? k_rms_norm_grad<T, LANES, NV, true> : k_rms_norm_grad<T, LANES, NV, false>), dim3((unsigned)groups), dim3(LANES < 256 ? 256 : LANES), 0, s, p);
   return launch_status("rms_norm_backward");
 }
 template <typename T>
-int launch_grad(const NormGradArgs& p, int64_t teams, hipStream_t s) {
-  if (p.d <= 512) return launch_grad_row<T, 1, 1>(p, teams, s);
-  if (p.d <= 1024) return launch_grad_row<T, 1, 2>(p, teams, s);
-  if (p.d <= 2048) return launch_grad_row<T, 4, 1>(p, teams, s);
-  if (p.d <= 4096) return launch_grad_row<T, 4, 2>(p, teams, s);
-  if (p.d <= 8192) return launch_grad_row<T, 8, 2>(p, teams, s);
-  if (p.d <= 16384) return launch_grad_row<T, 16, 2>(p, teams, s);
-  if (p.d <= kInRegisters) return launch_grad_row<T, 16, 4>(p, teams, s);
+int launch_grad(const NormGradArgs& p, int64_t groups, hipStream_t s) {
+  if (p.d <= 128) return launch_grad_row<T, 16, 1>(p, groups, s);
+  if (p.d <= 256) return launch_grad_row<T, 32, 1>(p, groups, s);
+  if (p.d <= 512) return launch_grad_row<T, 64, 1>(p, groups, s);
+  if (p.d <= 1024) return launch_grad_row<T, 64, 2>(p, groups, s);
+  if (p.d <= 2048) return launch_grad_row<T, 256, 1>(p, groups, s);
+  if (p.d <= 4096) return launch_grad_row<T, 256, 2>(p, groups, s);
+  if (p.d <= kInRegisters) return launch_grad_row<T, 512, 2>(p, groups, s);
   hipLaunchKernelGGL((k_rms_norm_stat<T>), dim3((unsigned)(p.rows < 512 ? p.rows : 512)), dim3(WIDE), 0, s, p);
-  hipLaunchKernelGGL((k_rms_norm_grad_columns<T>), dim3((unsigned)((p.d + 2047) / 2048), (unsigned)teams), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_rms_norm_grad_columns<T>), dim3((unsigned)((p.d + 2047) / 2048), (unsigned)groups), dim3(256), 0, s, p);
   return launch_status("rms_norm_backward");
 }
 
@@ -482,7 +539,9 @@ extern "C" int model_rms_norm(const void* x, int64_t ldx, const void* residual, 
     return fail(AE_EINVAL, "model_rms_norm: rows of codes must begin on 16-byte borders and not overlap");
   if ((h && ((h == x && ldh != ldx) || (h == residual && ldh != ldr))) || (y && ((y == x && ldy != ldx) || (y == residual && ldy != ldr))) || (h && h == y))
     return fail(AE_EINVAL, "model_rms_norm: an output in an input's place has its stride, and h and y have places of their own");
-  const NormArgs p = {x, ldx, residual, ldr, weight, rows, (int)d, eps, h, ldh, y, ldy, (uint8_t*)q, ldq, scale};
+  const int64_t es = dtype_size(dtype);
+  const bool stream_norm = rows * d * (es * (1 + !!residual + !!h + !!y) + !!q) > kStreamBytes;
+  const NormArgs p = {x, ldx, residual, ldr, weight, rows, (int)d, eps, h, ldh, y, ldy, (uint8_t*)q, ldq, scale, stream_norm};
   return dtype == AE_BF16 ? launch_norm<bf16_t>(p, (hipStream_t)stream) : launch_norm<float>(p, (hipStream_t)stream);
 }
 
@@ -490,7 +549,7 @@ extern "C" int model_rms_norm_backward_workspace(int64_t rows, int64_t d, int dt
   using namespace ae;
   if (!bytes) return fail(AE_EINVAL, "model_rms_norm_backward_workspace: null argument");
   AE_TRY(check_norm("model_rms_norm_backward_workspace", rows, d, 1.0f, dtype));
-  *bytes = align16(grad_teams(rows, d) * d * 4) + (d > kInRegisters ? rows * 16 : 0);
+  *bytes = align16(grad_groups(rows, d) * d * 4) + (d > kInRegisters ? rows * 16 : 0);
   return AE_OK;
 }
 
@@ -506,18 +565,18 @@ extern "C" int model_rms_norm_backward(const void* dy, int64_t ldy, const void* 
   AE_TRY(model_rms_norm_backward_workspace(rows, d, dtype, &need));
   if (need && (!workspace || ((uintptr_t)workspace & 15))) return fail(AE_EINVAL, "model_rms_norm_backward: workspace is null or not on a 16-byte border");
   hipStream_t s = (hipStream_t)stream;
-  const int64_t teams = grad_teams(rows, d);
+  const int64_t groups = grad_groups(rows, d);
   if (rows > 0) {
     if (!dy || !h) return fail(AE_EINVAL, "model_rms_norm_backward: null argument");
     if (!rows_ok(dy, ldy, d, dtype) || !rows_ok(h, ldh, d, dtype) || !rows_ok(d_h, ldg, d, dtype) || !rows_ok(dx, lddx, d, dtype))
       return fail(AE_EINVAL, "model_rms_norm_backward: rows must not overlap and must lie on their elements' borders");
     if (dx && ((dx == dy && lddx != ldy) || (dx == h && lddx != ldh) || (dx == d_h && lddx != ldg)))
       return fail(AE_EINVAL, "model_rms_norm_backward: a gradient in an input's place has its stride");
-    NormGradArgs p = {dy, ldy, h, ldh, weight, d_h, ldg, rows, (int)d, eps, dx, lddx, nullptr, nullptr};
+    NormGradArgs p = {dy, ldy, h, ldh, weight, d_h, ldg, rows, (int)d, eps, dx, lddx, nullptr, nullptr, rows * d * (int64_t)dtype_size(dtype) * (2 + !!d_h + !!dx) > kStreamBytes};
     if (d_weight) p.part = (float*)workspace;
-    p.stat = (float*)((char*)workspace + align16(teams * d * 4));
-    AE_TRY(dtype == AE_BF16 ? launch_grad<bf16_t>(p, teams, s) : launch_grad<float>(p, teams, s));
+    p.stat = (float*)((char*)workspace + align16(groups * d * 4));
+    AE_TRY(dtype == AE_BF16 ? launch_grad<bf16_t>(p, groups, s) : launch_grad<float>(p, groups, s));
   }
-  if (d_weight) hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0, s, (const float*)workspace, teams, (int)d, d_weight);
+  if (d_weight) hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, s, (const float*)workspace, groups, (int)d, d_weight);
   return launch_status("rms_norm_backward");
 }
