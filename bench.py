@@ -588,6 +588,106 @@ def bench_output_layer(torch, ae, args):
     }
 
 
+def build_token_step(torch, ae, tokens, d, vocab, seed, top_k=64, temperature=1.5, rows=4):
+    """The two ends of a language model whose embedding is its 8-bit output layer's weight, too: everything a training step and a
+    decoding step need.  What lies between (the blocks) is a residual stream that is given."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    normal = lambda *sh: torch.randn(sh, generator=gen, device="cuda")      # noqa: E731
+    f32 = lambda *sh: torch.empty(sh, device="cuda")      # noqa: E731
+    bf = lambda *sh: torch.empty(sh, dtype=torch.bfloat16, device="cuda")      # noqa: E731
+    ints = lambda lo, hi, *sh: torch.randint(lo, hi, sh, generator=gen, device="cuda").to(torch.int32)      # noqa: E731
+    codes = lambda r, c: torch.empty((r, -(-c // 16) * 16), dtype=torch.float8_e4m3fn, device="cuda")[:, :c]      # noqa: E731
+    blocks = lambda n: -(-n // ae.FP8_BLOCK)      # noqa: E731
+    st = dict(tokens=tokens, d=d, vocab=vocab, top_k=top_k, temperature=temperature, rows=rows, eps=1e-6, embed_scale=float(d) ** 0.5)
+    st["table"] = (2.5 / d ** 0.5 * normal(vocab, d)).to(torch.bfloat16)
+    st["w"], st["w_s"], st["wt"], st["wt_s"] = codes(vocab, d), f32(blocks(vocab), blocks(d)), codes(d, vocab), f32(blocks(d), blocks(vocab))
+    ae.model_fp8_quantize(st["table"], vocab, d, "tiles", st["w"], st["w_s"], st["wt"], st["wt_s"])
+    st["gain"] = 1.0 + 0.1 * normal(d)
+    n = max(tokens, rows)
+    st["ids"] = ints(0, vocab, tokens)
+    st["ids"][tokens // 2:tokens // 2 + tokens // 8] = -1                       # padded places
+    st["stream"] = normal(n, d).to(torch.bfloat16)                              # what the blocks add
+    st["weight"] = torch.where(st["ids"] < 0, 0.0, 1.0 / tokens)
+    st["top_id"] = (ints(0, vocab // top_k, tokens, top_k) + torch.arange(top_k, device="cuda", dtype=torch.int32) * (vocab // top_k)).contiguous()
+    st["top_logit"] = (4.0 + normal(tokens, top_k)).sort(1, descending=True).values.contiguous()
+    st["teacher_lse"] = torch.logsumexp(st["top_logit"] / temperature, 1) + 0.3
+    st["x"], st["h"], st["y"], st["logits"], st["loss"] = bf(n, d), bf(n, d), bf(n, d), bf(n, vocab), f32(1)
+    st["q"], st["q_s"] = codes(n, d), {m: f32(blocks(d), m) for m in {tokens, rows}}
+    st["yt"], st["yt_s"] = codes(d, tokens), f32(blocks(tokens), d)
+    st["g"], st["g_s"], st["gt"], st["gt_s"] = codes(tokens, vocab), f32(blocks(vocab), tokens), codes(vocab, tokens), f32(blocks(tokens), vocab)
+    st["dy"], st["dx"], st["d_gain"], st["d_table"], st["norm"] = bf(tokens, d), bf(tokens, d), f32(d), f32(vocab, d), f32(1)
+    st["grads"] = ae.GradList([st["d_table"], st["d_gain"]], [st["d_table"], st["d_gain"]])
+    # decoding: the tokens so far, a grammar that allows half of the vocabulary, and what comes out
+    st["last"], st["history"], st["n_prompt"] = ints(0, vocab, rows), ints(0, vocab, rows, 256), ints(0, 256, rows)
+    st["repetition"], st["presence"], st["frequency"] = (torch.full((rows,), v, device="cuda") for v in (1.2, 0.3, 0.1))
+    st["bias_id"], st["bias"] = ints(0, vocab, rows, 4), normal(rows, 4)
+    st["allowed"] = ints(-2 ** 31, 2 ** 31, rows, -(-vocab // 32))
+    k = min(8, vocab)
+    st["best"], st["best_logit"], st["best_logprob"] = torch.empty((rows, k), dtype=torch.int32, device="cuda"), f32(rows, k), f32(rows, k)
+    bfc = ae.AE_BF16
+    room = max(ae.model_fp8_matmul_workspace(tokens, vocab, d), ae.model_fp8_matmul_workspace(tokens, d, vocab), ae.model_fp8_matmul_workspace(vocab, d, tokens),
+               ae.model_loss_distill_workspace(tokens, vocab, bfc), ae.model_rms_norm_backward_workspace(tokens, d, bfc),
+               ae.model_embedding_backward_workspace(tokens, vocab, d, bfc), ae.model_grad_clip_workspace(st["grads"]),
+               ae.model_token_logprobs_workspace(rows, vocab, k, bfc))
+    st["ws"] = torch.empty(max(16, room), dtype=torch.uint8, device="cuda")
+    return st
+
+
+def token_train_step(st, ae, max_norm=1.0):
+    """embedding -> residual's addition and norm into codes -> 8-bit product -> distillation -> both gradients of the product -> the
+    norm's gradients -> the embedding's gradient on top of the product's weight gradient -> clipping."""
+    n, d, v, ws = st["tokens"], st["d"], st["vocab"], st["ws"]
+    x, h, y, q, logits = (st[k][:n] for k in ("x", "h", "y", "q", "logits"))
+    ae.model_embedding(st["table"], v, d, st["ids"], n, x, scale=st["embed_scale"])
+    ae.model_rms_norm(x, n, d, st["gain"], st["eps"], h, y, q, st["q_s"][n], residual=st["stream"][:n])
+    ae.model_fp8_matmul(q, st["q_s"][n], st["w"], st["w_s"], "tiles", None, n, v, d, logits, ws)
+    ae.model_loss_distill(logits, n, v, st["top_id"], st["top_logit"], None, st["loss"], logits, ws, teacher_lse=st["teacher_lse"], weight=st["weight"],
+                          temperature=st["temperature"])
+    ae.model_fp8_quantize(logits, n, v, "rows", st["g"], st["g_s"], st["gt"], st["gt_s"])
+    ae.model_fp8_quantize(y, n, d, "rows", None, None, st["yt"], st["yt_s"])
+    ae.model_fp8_matmul(st["g"], st["g_s"], st["wt"], st["wt_s"], "tiles", None, n, d, v, st["dy"], ws)
+    ae.model_fp8_matmul(st["gt"], st["gt_s"], st["yt"], st["yt_s"], "rows", None, v, d, n, st["d_table"], ws)
+    ae.model_rms_norm_backward(st["dy"], h, n, d, st["gain"], st["eps"], st["dx"], st["d_gain"], ws)
+    ae.model_embedding_backward(st["dx"], st["ids"], n, v, d, st["d_table"], ws, scale=st["embed_scale"], accumulate=True)
+    ae.model_grad_clip(st["grads"], max_norm, st["norm"], ws)
+
+
+def token_decode_step(st, ae):
+    """embedding -> norm into codes -> 8-bit product -> penalties, biases and mask -> the most probable tokens."""
+    n, d, v, ws = st["rows"], st["d"], st["vocab"], st["ws"]
+    x, h, q, logits = (st[k][:n] for k in ("x", "h", "q", "logits"))
+    ae.model_embedding(st["table"], v, d, st["last"], n, x, scale=st["embed_scale"])
+    ae.model_rms_norm(x, n, d, st["gain"], st["eps"], h, None, q, st["q_s"][n], residual=st["stream"][:n])
+    ae.model_fp8_matmul(q, st["q_s"][n], st["w"], st["w_s"], "tiles", None, n, v, d, logits, ws)
+    ae.model_logits_adjust(logits, n, v, logits, history=st["history"], n_prompt=st["n_prompt"], repetition=st["repetition"], presence=st["presence"],
+                           frequency=st["frequency"], bias_id=st["bias_id"], bias=st["bias"], allowed=st["allowed"])
+    ae.model_token_logprobs(logits, n, v, None, st["best"].shape[1], None, None, None, st["best"], st["best_logit"], st["best_logprob"], ws)
+
+
+def bench_token_step(torch, ae, args):
+    """The training step above for 2 048 tokens, hidden width 4 096 and 32 768 tokens of vocabulary, and the decoding step for four rows."""
+    tokens, d, vocab = 2048, 4096, 32768
+    st = build_token_step(torch, ae, tokens, d, vocab, seed=37)
+    seconds = {}
+    for name, step in (("train", token_train_step), ("decode", token_decode_step)):
+        for _ in range(args.warmup):
+            step(st, ae)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(args.steps):
+            step(st, ae)
+        torch.cuda.synchronize()
+        seconds[name] = (time.perf_counter() - t0) / args.steps
+    return {
+        "metric": "tokens/sec, training step from tokens to an 8-bit output layer and back (embedding, norm, product, distillation, gradients, clipping)",
+        "value": tokens / seconds["train"], "unit": "tokens/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "ms_per_step": seconds["train"] * 1e3, "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "fp8", "data": "synthetic",
+        "config": {"workload": "token_step", "tokens": tokens, "d": d, "vocab": vocab, "top_k": 64, "temperature": 1.5},
+        "loss": st["loss"].item(), "gradient_norm": st["norm"].item(), "decode_ms_of_4_rows": seconds["decode"] * 1e3,
+    }
+
+
 # measured HBM bytes per product launch of the QR parametrisation (profiles/qr_param.md)
 QR_TRAFFIC_BYTES = {"f32": 8.56e8}
 
@@ -812,6 +912,9 @@ def main():
     ap.add_argument("--output-layer", action="store_true",
                     help="benchmark a calibration step of an 8-bit output layer (teacher's top logits, 8-bit products, log probabilities, "
                          "distillation loss and gradients) instead of a network: one JSON line")
+    ap.add_argument("--token-step", action="store_true",
+                    help="benchmark a training step (embedding, norm into 8-bit codes, output layer, distillation, all gradients, clipping) and a "
+                         "decoding step (up to penalties, grammar mask and top tokens) instead of a network: one JSON line")
     ap.add_argument("--mx-elem", default="fp4", choices=["fp4", "fp8", "int4"],
                     help="element format of --mx-quant (FP4 E2M1, FP8 E4M3, or the 4-bit integer reading)")
     ap.add_argument("--calibrate-mfma", action="store_true",
@@ -850,6 +953,9 @@ def main():
         return
     if args.output_layer:
         print(json.dumps(bench_output_layer(torch, ae, args)))
+        return
+    if args.token_step:
+        print(json.dumps(bench_token_step(torch, ae, args)))
         return
     if args.qr_param:
         print(json.dumps(bench_qr_param(torch, ae, args)))

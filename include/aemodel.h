@@ -482,10 +482,10 @@ int model_loss_distill(const void* logits, int64_t rows, int64_t vocab, int64_t 
  *
  * model_rms_norm  for every row of x [rows][d] and residual [rows][d] (nullable: none)
  *     h = x + residual,   y_j = h_j * weight_j / sqrt(mean_k h_k^2 + eps)
- *   in binary32 from the sum on (y is that of the sum, not of its rounding); weight binary32 [d], nullable (ones); eps a
- *   positive normal number.  Outputs, each nullable, one at least: h and y in dtype, rounded once; q with scale: y in E4M3
+ *   in binary32 from the sum on (y is that of the sum, not of its rounding); weight binary32 [d], nullable (ones); eps
+ *   2^-126 .. 2^60.  Outputs, each nullable, one at least: h and y in dtype, rounded once; q with scale: y in E4M3
  *   codes, AE_FP8_ROWS (what model_fp8_matmul takes as a; codes and scales of model_fp8_quantize applied to the binary32
- *   y).  h, or y where h is null, may be x or residual itself, with the same stride.  A row that holds an infinity gives NaN there and 0
+ *   y).  h and y may each take the place of x or of residual, with its stride.  A row that holds an infinity gives NaN there and 0
  *   elsewhere, one that holds a NaN gives NaN; other rows are not affected.  1 <= d <= 2^20, rows up to 2^31 - 513.
  * model_rms_norm_backward  from dy [rows][d] and the sum h [rows][d] that model_rms_norm wrote (or x, without residual), with
  *   r = 1 / sqrt(mean h^2 + eps), u = h r, g = dy weight:

@@ -508,11 +508,12 @@ int launch_grad(const NormGradArgs& p, int64_t groups, hipStream_t s) {
 
 constexpr int64_t kRowsMax = 0x7FFFFFFF - 512;
 constexpr int64_t kWidthMax = 1 << 20;
+constexpr float kEpsMax = 1152921504606846976.0f;     // 2^60: beside a mean of squares near binary32's end it plays no part
 int check_norm(const char* who, int64_t rows, int64_t d, float eps, int dtype) {
   if (dtype != AE_F32 && dtype != AE_BF16) return fail(AE_EINVAL, "%s: bad dtype", who);
   if (rows < 0 || rows > kRowsMax) return fail(AE_EINVAL, "%s: rows must be 0 .. 2^31 - 513", who);
   if (d < 1 || d > kWidthMax) return fail(AE_EINVAL, "%s: d must be 1 .. 2^20", who);
-  if (!(eps >= FLT_MIN && eps <= FLT_MAX)) return fail(AE_EINVAL, "%s: eps must be a positive normal number", who);
+  if (!(eps >= FLT_MIN && eps <= kEpsMax)) return fail(AE_EINVAL, "%s: eps must be 2^-126 .. 2^60", who);
   return AE_OK;
 }
 // a matrix of rows that do not overlap, on its elements' borders; null is no matrix
