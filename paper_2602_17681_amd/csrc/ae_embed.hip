@@ -217,10 +217,9 @@ __device__ __forceinline__ void add_row(const EmbedGrad& p, int v, int col, cons
 // W wavefronts add up the rows of a run of sorted places, NV times four neighbouring columns to a lane (16 bytes of the result, so
 // that a wavefront's stores are whole lines).  The workgroups behind `sums` write the zeros of tokens that do not occur.
 constexpr int ZERO_ROWS = 4;
-template <typename T, int W, int NV>
+template <typename T, int W, int NV, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
   constexpr int TEAM = 64 * W, TEAMS = 4 / W;
-  constexpr bool SHORT = W == 1 && NV == 1;
   if ((int)blockIdx.x >= p.sums) {
     const int lane = threadIdx.x & 63, v0 = ((int)blockIdx.x - p.sums) * ZERO_ROWS, v = v0 + lane;
     uint64_t todo = __ballot(lane < ZERO_ROWS && v < p.vocab && (!p.sort.start || p.sort.start[v] == p.sort.start[v + 1]));
@@ -347,6 +346,97 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedGrad p) {
   if (left > 0) add_row(p, v, col, acc);
 }
 
+// Few places: one launch without sorting.  Every place has a team, which compares its token with all ids at once; the first
+// place of a token goes on and adds up the rows of all its places in their order.  Against the three launches below, in us, bfloat16,
+// tokens as in text / all different / all the same, 4 000 tokens of vocabulary: 256 places of 1 024 columns 6.6 / 6.6 / 18 (three launches
+// 17.6 / 16.3 / 15), 512 7.5 / 7.4 / 32 (17.6 / 16.4 / 16), 1 024 9 / 9 / 58 (18 / 18 / 19); 512 of 4 096 columns 17 / 18 / 38 (23 / 23 / 23), 1 024
+// 22 / 24 / 67 (25 / 25 / 26): what one token costs a single team ends the rule at 512.
+constexpr int FEW = 512, FEW_ZERO_ROWS = 16;
+template <typename T, int W, int NV, bool SHORT>
+__global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __restrict__ ids) {
+  constexpr int TEAM = 64 * W, TEAMS = 4 / W;
+  __shared__ int places[4][FEW];                 // each wavefront's own list
+  const int n = (int)p.n, lane = threadIdx.x & 63;
+  if ((int)blockIdx.x >= p.sums) {
+    const int v0 = ((int)blockIdx.x - p.sums) * FEW_ZERO_ROWS, rows = p.vocab - v0 < FEW_ZERO_ROWS ? p.vocab - v0 : FEW_ZERO_ROWS;
+    int* there = places[0];
+    if (threadIdx.x < FEW_ZERO_ROWS) there[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < FEW / 256; ++k) {
+      const int i = k * 256 + (int)threadIdx.x;
+      const unsigned v = i < n ? (unsigned)ids[i] - (unsigned)v0 : ~0u;
+      if (v < (unsigned)rows) there[v] = 1;      // whoever writes, writes the same
+    }
+    __syncthreads();
+    const float zero[4] = {0, 0, 0, 0};
+    for (int v = 0; v < rows; ++v) {
+      if (there[v]) continue;
+      float* at = p.d_table + (int64_t)(v0 + v) * p.ldt;
+      for (int col = threadIdx.x * 4; col < p.d; col += 1024) put(at + col, p.d - col, zero);
+    }
+    return;
+  }
+  const int t = threadIdx.x % TEAM, wave = threadIdx.x >> 6;
+  const int group = (int)blockIdx.x / p.cols, c0 = ((int)blockIdx.x - group * p.cols) * (TEAM * 4 * NV) + t * 4;
+  const int mine = group * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+  if (mine >= n) return;
+  int id[FEW / 64];
+#pragma unroll
+  for (int k = 0; k < FEW / 64; ++k) id[k] = k * 64 + lane < n ? ids[k * 64 + lane] : -1;
+  const int v = ids[mine];
+  if (v < 0 || v >= p.vocab) return;
+  int count = 0;
+#pragma unroll
+  for (int k = 0; k < FEW / 64; ++k) {
+    const uint64_t m = __ballot(id[k] == v);
+    if (id[k] == v) places[wave][count + __popcll(m & (((uint64_t)1 << lane) - 1))] = k * 64 + lane;
+    count += __popcll(m);
+  }
+  if (__builtin_amdgcn_readfirstlane(places[wave][0]) != mine) return;         // written by this wavefront alone, in order
+  constexpr int U = NV * sizeof(T) > 4 ? 8 : 16;               // rows in flight
+  const bool edge = __any(c0 + (NV - 1) * TEAM * 4 > p.d - 4);   // the rows' end lies in this wavefront's columns
+  float acc[NV][4];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[k][j] = 0.0f;
+  for (int at = 0; at < count; at += U) {
+    Piece<T, 4> e[U][NV];
+    const int place = places[wave][at + lane < count ? at + lane : count - 1];           // behind the list's end: its last row again
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const T* row = (const T*)p.d_out + (int64_t)__builtin_amdgcn_readlane(place, u) * p.ldo;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) fetch_row<false, SHORT>(row, c0 + k * TEAM * 4, p.d, e[u][k]);
+    }
+    if (edge) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) settle<SHORT>(c0 + k * TEAM * 4, p.d, e[u][k]);
+    }
+    if (at + U <= count) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[k][j] += value(e[u][k], j);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[k][j] = at + u < count ? acc[k][j] + value(e[u][k], j) : acc[k][j];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (c0 + k * TEAM * 4 < p.d) add_row(p, v, c0 + k * TEAM * 4, acc[k]);
+}
+
 // Wavefronts and four-column pieces of a lane that share a run, and from them its positions: at least 16, and as many as leave
 // 1 024 workgroups.
 int team_of(int64_t d) { return d <= 512 ? 1 : 4; }
@@ -358,17 +448,33 @@ int64_t run_of(int64_t n, int64_t d) {
 }
 int64_t runs_of(int64_t n, int64_t d) { return (n + run_of(n, d) - 1) / run_of(n, d); }
 
-template <typename T, int W, int NV>
+template <typename T, int W, int NV, bool SHORT = false>
 int launch_embed_sum(EmbedGrad p, hipStream_t s) {
   constexpr int TEAMS = 4 / W, COLS = 64 * W * 4 * NV;
   p.cols = (p.d + COLS - 1) / COLS;
   p.sums = (int)((p.runs + TEAMS - 1) / TEAMS) * p.cols;
   const int zeros = p.accumulate ? 0 : (p.vocab + ZERO_ROWS - 1) / ZERO_ROWS;
-  hipLaunchKernelGGL((k_embed_sum<T, W, NV>), dim3((unsigned)(p.sums + zeros)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_embed_sum<T, W, NV, SHORT>), dim3((unsigned)(p.sums + zeros)), dim3(256), 0, s, p);
+  return launch_status("embedding_backward");
+}
+template <typename T, int W, int NV, bool SHORT = false>
+int launch_embed_few_team(EmbedGrad p, const int* ids, hipStream_t s) {
+  constexpr int TEAMS = 4 / W, COLS = 64 * W * 4 * NV;
+  p.cols = (p.d + COLS - 1) / COLS;
+  p.sums = (int)((p.n + TEAMS - 1) / TEAMS) * p.cols;
+  const int zeros = p.accumulate ? 0 : (p.vocab + FEW_ZERO_ROWS - 1) / FEW_ZERO_ROWS;
+  hipLaunchKernelGGL((k_embed_few<T, W, NV, SHORT>), dim3((unsigned)(p.sums + zeros)), dim3(256), 0, s, p, ids);
   return launch_status("embedding_backward");
 }
 template <typename T>
+int launch_embed_few(const EmbedGrad& p, const int* ids, hipStream_t s) {
+  if (p.d < 4) return launch_embed_few_team<T, 1, 1, true>(p, ids, s);       // rows shorter than a piece
+  if (team_of(p.d) == 1) return pieces_of(p.d) == 1 ? launch_embed_few_team<T, 1, 1>(p, ids, s) : launch_embed_few_team<T, 1, 2>(p, ids, s);
+  return launch_embed_few_team<T, 4, 1>(p, ids, s);
+}
+template <typename T>
 int launch_embed_sums(const EmbedGrad& p, hipStream_t s) {
+  if (p.d < 4) return launch_embed_sum<T, 1, 1, true>(p, s);       // rows shorter than a piece
   if (team_of(p.d) == 1) return pieces_of(p.d) == 1 ? launch_embed_sum<T, 1, 1>(p, s) : launch_embed_sum<T, 1, 2>(p, s);
   return launch_embed_sum<T, 4, 1>(p, s);
 }
@@ -425,7 +531,7 @@ extern "C" int model_embedding_backward_workspace(int64_t n, int64_t vocab, int6
   using namespace ae;
   if (!bytes) return fail(AE_EINVAL, "model_embedding_backward_workspace: null argument");
   AE_TRY(check_embedding("model_embedding_backward_workspace", n, vocab, d, dtype));
-  *bytes = n == 0 ? 0 : 2 * align16(n * 4) + align16((vocab + 1) * 4) + align16(runs_of(n, d) * 4) + runs_of(n, d) * 2 * d * 4;
+  *bytes = n <= FEW ? 0 : 2 * align16(n * 4) + align16((vocab + 1) * 4) + align16(runs_of(n, d) * 4) + runs_of(n, d) * 2 * d * 4;
   return AE_OK;
 }
 
@@ -441,13 +547,14 @@ extern "C" int model_embedding_backward(const void* d_out, int64_t ldo, const in
   if (n > 0) {
     if (!d_out || !ids) return fail(AE_EINVAL, "model_embedding_backward: null argument");
     if ((uintptr_t)d_out % dtype_size(dtype) || ((uintptr_t)ids & 3)) return fail(AE_EINVAL, "model_embedding_backward: misaligned argument");
-    if (!workspace || ((uintptr_t)workspace & 15)) return fail(AE_EINVAL, "model_embedding_backward: workspace is null or not on a 16-byte border");
+    if (need && (!workspace || ((uintptr_t)workspace & 15))) return fail(AE_EINVAL, "model_embedding_backward: workspace is null or not on a 16-byte border");
   } else if (accumulate) {
     return AE_OK;
   }
   char* ws = (char*)workspace;
   EmbedGrad p = {d_out, ldo, {}, (int)vocab, (int)d, (int)run_of(n, d), n, runs_of(n, d), 0, 0, scale, d_table, ldt, accumulate ? 1 : 0, nullptr, nullptr};
   if (n == 0) return launch_embed_sums<float>(p, s);       // zeros alone
+  if (n <= FEW) return dtype == AE_BF16 ? launch_embed_few<bf16_t>(p, ids, s) : launch_embed_few<float>(p, ids, s);
   p.sort.place = (int*)ws;
   p.sort.token = (int*)(ws + align16(n * 4));
   p.sort.start = (int*)(ws + 2 * align16(n * 4));

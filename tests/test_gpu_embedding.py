@@ -74,6 +74,25 @@ def test_gradient(n, vocab, d, kind, dtype):
     assert a.whole() and np.array_equal(a.m.cpu().numpy()[count == 0], there[count == 0])
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["text", "one", "none", "any"])
+@pytest.mark.parametrize("n,vocab,d,dtype", [(511, 40, 515, "f32"), (512, 40, 515, "bf16"), (513, 40, 515, "bf16"), (300, 90, 2051, "f32"), (500, 5000, 3, "bf16"), (512, 3, 300, "f32"),
+                                             (129, 1, 4, "f32"), (64, 17, 256, "bf16"), (65, 16, 257, "f32"), (513, 1000, 512, "f32")])
+def test_gradient_on_both_sides_of_the_rule_for_few_places(n, vocab, d, dtype, kind, accumulate):
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(n + d)
+    ids = tokens(rng, n, vocab, kind)
+    g, t = Room(n, d, dtype, 1, 3, dev(rng.standard_normal((n, d)).astype(np.float32))), Room(vocab, d, "f32", 2, 1)
+    there = host(t.m) if accumulate else 0.0
+    want, mag, count = to.embedding_backward(host(g.m), ids, vocab, -0.75)
+    ws = space(ae.model_embedding_backward_workspace(n, vocab, d, ae.DTYPES[dtype]))
+    assert (ws is None) == (n <= 512)
+    ae.model_embedding_backward(g.m, ints(ids), n, vocab, d, t.m, ws, scale=-0.75, accumulate=accumulate)
+    near(host(t.m), want + there, (count[:, None] + 2) * U * mag + accumulate * U * (np.abs(want) + np.abs(there)) * 1.001)
+    assert t.whole() and (not accumulate or np.array_equal(host(t.m)[count == 0], there[count == 0]))
+
+
 def test_gradient_of_long_lists():
     """A frequent token in hundreds of thousands of places, in binary32 partial sums of a run's length each."""
     import torch

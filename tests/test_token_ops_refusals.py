@@ -101,13 +101,13 @@ def test_embedding_backward(ae):
         refused(ae, call(**bad), "null")
     for bad in (dict(g=ODD), dict(ids=ODD)):
         refused(ae, call(**bad), "misaligned")
-    refused(ae, call(ws=None), "workspace")
-    refused(ae, call(ws=C.c_void_p(8)), "workspace")
+    refused(ae, call(n=600, ws=None), "workspace")
+    refused(ae, call(n=600, ws=C.c_void_p(8)), "workspace")
     assert call(n=0, acc=1, g=None, ids=None, ws=None) == 0        # nothing to add
     n = C.c_int64()
     refused(ae, ae.lib.model_embedding_backward_workspace(4, 100, 64, 0, None), "null")
     refused(ae, ae.lib.model_embedding_backward_workspace(4, 0, 64, 0, C.byref(n)), "vocab")
-    assert ae.lib.model_embedding_backward_workspace(4, 100, 64, 0, C.byref(n)) == 0 and n.value >= 101 * 4 + 2 * 64 * 4
+    assert ae.lib.model_embedding_backward_workspace(600, 100, 64, 0, C.byref(n)) == 0 and n.value >= 101 * 4 + 2 * 64 * 4
 
 
 def test_grad_clip(ae):
