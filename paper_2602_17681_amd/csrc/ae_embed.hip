@@ -3,6 +3,9 @@
 // The gradient sorts the places by token (stable, so that a sum's order does not change from call to call), cuts the sorted
 // list into runs of equal length and adds up each run's rows: a token that fills half the batch takes as many workgroups
 // as its places need, and what a token has in several runs is joined in their order.
+// Both are bound by memory.  16 384 tokens of 4 096 bfloat16 columns, tokens as in text: the lookup 39 us (repeated rows come from the
+// cache), the gradient over 32 768 tokens of vocabulary 149 us: sort 9.7, sums beside the zeros of 27 000 tokens that do not
+// occur 133 (690 MB at 5.2 TB/s), join 6.
 #include <hip/hip_runtime.h>
 
 #include "ae_device.h"
@@ -50,23 +53,25 @@ __global__ __launch_bounds__(256) void k_embedding(const T* __restrict__ table, 
 // all ids twice (they are few bytes beside the rows) and keeps its tokens' counters in LDS.  The first pass counts its
 // tokens and what lies below its range; the second puts its places down in their order.
 constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_RANGE = 4096;    // tokens of a range at most
-constexpr int SORT_LOADS = 4096 / SORT_NT, SORT_IDS = SORT_NT * 4 * SORT_LOADS;             // ids that a workgroup has in registers: four neighbours to a load
 struct EmbedSort {
   int* place;                             // [n]: places in the order of their tokens
   int* token;                             // [n]: the token at each position of that order
   int* start;                             // [vocab + 1]: each token's first position; null: no token occurs
 };
+// LOADS times four neighbouring ids are in a thread's registers at a time.
+template <int LOADS>
 __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ ids, int64_t n, int vocab, int range, EmbedSort out) {
+  constexpr int IDS = SORT_NT * 4 * LOADS, LANES = LOADS * SORT_WAVES;
   __shared__ int at[SORT_RANGE];
-  __shared__ uint32_t queue[SORT_IDS];           // token within the range << 14 | place within the ids at hand
-  __shared__ int sums[SORT_LOADS * SORT_WAVES];
-  static_assert(SORT_IDS == 1 << 14 && SORT_RANGE <= 1 << 18, "a queue entry holds both");
+  __shared__ uint32_t queue[IDS];                // token within the range << 14 | place within the ids at hand
+  __shared__ int sums[LANES < 2 * SORT_WAVES ? 2 * SORT_WAVES : LANES];
+  static_assert(IDS <= 1 << 14 && SORT_RANGE <= 1 << 18, "a queue entry holds both");
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int v0 = (int)blockIdx.x * range, mine = vocab - v0 < range ? vocab - v0 : range;
-  int id[SORT_LOADS][4];
+  int id[LOADS][4];
   auto load = [&](int64_t base) {
 #pragma unroll
-    for (int l = 0; l < SORT_LOADS; ++l) {
+    for (int l = 0; l < LOADS; ++l) {
       const int64_t i = base + (l * SORT_NT + t) * 4;
       if (i + 4 <= n) {
         __builtin_memcpy(id[l], ids + i, 16);
@@ -80,10 +85,10 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
   for (int v = t; v < mine; v += SORT_NT) at[v] = 0;
   __syncthreads();
   int below = 0;
-  for (int64_t base = 0; base < n; base += SORT_IDS) {
+  for (int64_t base = 0; base < n; base += IDS) {
     if (base) load(base);
 #pragma unroll
-    for (int l = 0; l < SORT_LOADS; ++l)
+    for (int l = 0; l < LOADS; ++l)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {              // a negative id is a large unsigned number
         below += (unsigned)id[l][k] < (unsigned)v0;
@@ -117,13 +122,13 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
     run += c;
   }
   if (v0 + mine == vocab && c0 < mine && c0 + each >= mine) out.start[vocab] = run;
-  for (int64_t base = 0; base < n; base += SORT_IDS) {
+  for (int64_t base = 0; base < n; base += IDS) {
     __syncthreads();
-    if (n > SORT_IDS) load(base);
+    if (n > IDS) load(base);
     // this range's tokens among these ids, in order
-    int before[SORT_LOADS];
+    int before[LOADS];
 #pragma unroll
-    for (int l = 0; l < SORT_LOADS; ++l) {
+    for (int l = 0; l < LOADS; ++l) {
       int total = 0;
       before[l] = 0;
 #pragma unroll
@@ -135,9 +140,9 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
       if (lane == 0) sums[l * SORT_WAVES + wave] = total;
     }
     __syncthreads();
-    // 64 sums, one to a lane: all wavefronts scan them alike
-    static_assert(SORT_LOADS * SORT_WAVES == 64, "a sum to a lane");
-    int scan = sums[lane];
+    // the sums one to a lane: all wavefronts scan them alike
+    static_assert(LANES <= 64, "a sum to a lane");
+    int scan = lane < LANES ? sums[lane] : 0;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(scan, o, 64);
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
     }
     const int all = __builtin_amdgcn_readlane(scan, 63);
 #pragma unroll
-    for (int l = 0; l < SORT_LOADS; ++l) {
+    for (int l = 0; l < LOADS; ++l) {
       const int slot = l * SORT_WAVES + wave;
       int q = before[l] + (slot ? __shfl(scan, slot - 1, 64) : 0);
 #pragma unroll
@@ -183,7 +188,7 @@ __global__ __launch_bounds__(SORT_NT) void k_embed_sort(const int* __restrict__ 
       }
       from = __shfl(from, leader, 64);
       if (live) {
-        out.place[from + rank] = (int)(base + (e & (SORT_IDS - 1)));
+        out.place[from + rank] = (int)(base + (e & ((1 << 14) - 1)));
         out.token[from + rank] = v0 + mv;
       }
     }
@@ -215,8 +220,9 @@ __device__ __forceinline__ void add_row(const EmbedGrad& p, int v, int col, cons
   put(at, left, o);
 }
 // W wavefronts add up the rows of a run of sorted places, NV times four neighbouring columns to a lane (16 bytes of the result, so
-// that a wavefront's stores are whole lines).  The workgroups behind `sums` write the zeros of tokens that do not occur.
-constexpr int ZERO_ROWS = 4;
+// that a wavefront's stores are whole lines).  The workgroups behind `sums` write the zeros of tokens that do not occur (among the sums,
+// one for one: 228 us against 162, since every second workgroup is on the same four of the eight dies; by eights 166 against 150).
+constexpr int ZERO_ROWS = 4;                     // (embed gradient above 150 us with 4 rows or 2, 152 with 16)
 template <typename T, int W, int NV, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
   constexpr int TEAM = 64 * W, TEAMS = 4 / W;
@@ -266,6 +272,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
     }
   };
   clear();
+  const bool edge = __any(c0 + (NV - 1) * TEAM * 4 > p.d - 4);   // the rows' end lies in this wavefront's columns
   int v = __builtin_amdgcn_readfirstlane(token);
   bool begun = earlier == v;                     // the sum at hand is of a token that began before the run
   for (int64_t s0 = from; s0 < to; s0 += 64) {
@@ -282,6 +289,12 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) fetch_row<true, SHORT>(row, c0 + k * TEAM * 4, p.d, e[u][k]);
       }
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < NV; ++k) settle<SHORT>(c0 + k * TEAM * 4, p.d, e[u][k]);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (u0 + u >= here) break;
@@ -295,7 +308,6 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          settle<SHORT>(c0 + k * TEAM * 4, p.d, e[u][k]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[k][j] += value(e[u][k], j);
         }
@@ -348,9 +360,9 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedGrad p) {
 
 // Few places: one launch without sorting.  Every place has a team, which compares its token with all ids at once; the first
 // place of a token goes on and adds up the rows of all its places in their order.  Against the three launches below, in us, bfloat16,
-// tokens as in text / all different / all the same, 4 000 tokens of vocabulary: 256 places of 1 024 columns 6.6 / 6.6 / 18 (three launches
-// 17.6 / 16.3 / 15), 512 7.5 / 7.4 / 32 (17.6 / 16.4 / 16), 1 024 9 / 9 / 58 (18 / 18 / 19); 512 of 4 096 columns 17 / 18 / 38 (23 / 23 / 23), 1 024
-// 22 / 24 / 67 (25 / 25 / 26): what one token costs a single team ends the rule at 512.
+// tokens as in text / all different / all the same, 4 000 tokens of vocabulary: 256 places of 1 024 columns 6.5 / 6.4 / 18 (three launches
+// 15.7 / 14.4 / 13), 512 7.2 / 7.1 / 31 (15.6 / 15.7 / 14), 1 024 9 / 9 / 58 (16 / 16 / 17); 512 of 4 096 columns 17 / 18 / 37 (21 / 21 / 21), 1 024
+// 22 / 24 / 67 (24 / 23 / 24): what one token costs a single team ends the rule at 512.
 constexpr int FEW = 512, FEW_ZERO_ROWS = 16;
 template <typename T, int W, int NV, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __restrict__ ids) {
@@ -438,7 +450,7 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __res
 }
 
 // Wavefronts and four-column pieces of a lane that share a run, and from them its positions: at least 16, and as many as leave
-// 1 024 workgroups.
+// 1 024 workgroups (16 384 x 4 096 150 us, with 2 048 148 and twice the workspace; 16 positions always 228: more partial sums).
 int team_of(int64_t d) { return d <= 512 ? 1 : 4; }
 int pieces_of(int64_t d) { return d > 256 && d <= 512 ? 2 : 1; }
 int64_t run_of(int64_t n, int64_t d) {
@@ -562,7 +574,9 @@ extern "C" int model_embedding_backward(const void* d_out, int64_t ldo, const in
   p.part = (float*)((char*)p.owner + align16(p.runs * 4));
   const int range = (int)((vocab + 255) / 256);
   static_assert(kVocabMax / 256 <= SORT_RANGE, "a range's counters fit into LDS");
-  hipLaunchKernelGGL(k_embed_sort, dim3((unsigned)((vocab + range - 1) / range)), dim3(SORT_NT), 0, s, ids, n, (int)vocab, range, p.sort);
+  // 1 024 places in one batch of four each 15.8 us with the sums, 17.8 in the kernel for four batches; 4 097 in two 18.2 and 19.4
+  const auto sort = n <= 4 * SORT_NT ? k_embed_sort<1> : n <= 8 * SORT_NT ? k_embed_sort<2> : k_embed_sort<4>;
+  hipLaunchKernelGGL(sort, dim3((unsigned)((vocab + range - 1) / range)), dim3(SORT_NT), 0, s, ids, n, (int)vocab, range, p.sort);
   AE_TRY(dtype == AE_BF16 ? launch_embed_sums<bf16_t>(p, s) : launch_embed_sums<float>(p, s));
   if (p.runs > 1)
     hipLaunchKernelGGL(k_embed_join, dim3((unsigned)(p.runs - 1), (unsigned)((d + 255) / 256)), dim3(256), 0, s, p);

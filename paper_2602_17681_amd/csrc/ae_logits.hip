@@ -2,7 +2,8 @@
 // biases of given tokens, and a mask of what a grammar allows.
 // A workgroup takes a slice of a row.  Every column of the slice has a word in LDS: how often the token was answered, whether
 // it occurred at all, and which bias it has.  The row's history and list of biases are read by each slice (they are short
-// beside it, and in the cache), then the slice passes through registers once.
+// beside it, and in the cache), then the slice passes through registers once.  Bound by memory: 333 x 50 021 in binary32 with mask, 777 tokens
+// of history and 5 biases 30.6 us (136 MB, 4.5 TB/s; rows begin on any 4-byte border), 256 x 131 072 in bfloat16 36 us; four rows 5.2 us.
 #include <hip/hip_runtime.h>
 
 #include "ae_device.h"
@@ -128,6 +129,8 @@ template <typename T>
 int launch_adjust_rows(const AdjustArgs& p, hipStream_t s) {
   constexpr int E = sizeof(T) / 2;               // pieces for 4 096 columns
   if (!p.n_history && !p.n_bias) return launch_adjust<T, 2 * E, false>(p, s);
+  // slices of 4 096 columns where they are fewer than 1 024: 4 rows of 131 072 5.2 us (8 192 columns 5.6), 64 of 50 021 8.7 (9.9), 32 of
+  // 131 072 7.3 (7.2), 128 of 131 072 23 (21), 128 of 50 021 14.6 (13.8), 512 of 32 000 25 (21); 2 048 columns and 256 threads 333 x 50 021 40, 37 with 8 192 and 512
   if (p.rows * ((p.vocab + 4095) / 4096) < 1024) return launch_adjust<T, E, true>(p, s);
   return launch_adjust<T, 2 * E, true>(p, s);
 }
