@@ -19,6 +19,7 @@ AE_F32, AE_BF16 = 0, 1
 DTYPES = {"f32": AE_F32, "bf16": AE_BF16}
 TORCH_DTYPE = {AE_F32: torch.float32, AE_BF16: torch.bfloat16}
 _DTYPE_CODE = {t: c for c, t in TORCH_DTYPE.items()}
+_CODE_DTYPES = (torch.float8_e4m3fn, torch.uint8)
 
 SYMBOLS = [
     "model_describe", "model_create", "model_destroy", "model_param_count", "model_io_shape",
@@ -155,7 +156,7 @@ def _mat(t, rows, cols, dtype=None):
     if t is None:
         return None, 0
     assert t.is_cuda and t.shape == (rows, cols), "device-resident [%d][%d] matrix required" % (rows, cols)
-    assert dtype is None or t.dtype == dtype, (t.dtype, dtype)
+    assert dtype is None or t.dtype is dtype, (t.dtype, dtype)
     ld, step = t.stride()
     if rows <= 1:
         ld = max(cols, ld)                          # the stride of a single row plays no part
@@ -167,11 +168,11 @@ def _codes(t, rows, cols):
     """(data pointer, row stride in bytes) of a matrix of 8-bit codes (float8_e4m3fn or uint8); null for None."""
     if t is None:
         return None, 0
-    assert t.dtype == torch.float8_e4m3fn or t.dtype == torch.uint8, t.dtype
+    assert t.dtype in _CODE_DTYPES, t.dtype
     p, ld = _mat(t, rows, cols)
     if rows == 1:
         ld = -(-ld // 16) * 16
-    assert rows == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= rows * ld, "all rows * stride bytes must be there"
+    assert ld == cols or rows == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= rows * ld, "all rows * stride bytes must be there"
     return p, ld
 
 
@@ -179,7 +180,7 @@ def _vec(t, n, dtype=torch.float32):
     """Data pointer of a contiguous device array of n elements; None for None."""
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), "contiguous device array of %d %s required" % (n, dtype)
+    assert t.is_cuda and t.dtype is dtype and t.numel() == n and t.is_contiguous(), "contiguous device array of %d %s required" % (n, dtype)
     return t.data_ptr()
 
 

@@ -100,6 +100,14 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* out, int64_t left, fl
     else if (left > at) put(out + at, (int)left - at, v);
   }
 }
+// the norm alone
+__global__ __launch_bounds__(NT) void k_grad_norm(const double* __restrict__ part, int parts, float* __restrict__ norm) {
+  __shared__ double sm[NT / 64 + 1];
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += NT) sum += part[i];
+  sum = block_sum<NT>(sum, sm);
+  if (threadIdx.x == 0) *norm = (float)sqrt(sum);
+}
 // Every workgroup adds up the shares' sums itself, in the same order (8 KB, from L2), so that no launch stands in between.
 __global__ __launch_bounds__(NT) void k_grad_scale(GradArgs p, const double* __restrict__ part, int parts, float max_norm, float* __restrict__ norm) {
   __shared__ double sm[NT / 64 + 1];
@@ -249,8 +257,7 @@ extern "C" int model_grad_clip(void* const* grads, const int64_t* sizes, const i
   }
   AE_TRY(launch_status("grad_clip"));
   if (!out || !launches) {
-    p.count = p.chunks = 0;
-    hipLaunchKernelGGL(k_grad_scale, dim3(1), dim3(NT), 0, s, p, part, (int)parts, max_norm, norm);
+    if (norm) hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(NT), 0, s, part, (int)parts, norm);
     return launch_status("grad_clip");
   }
   for (int k = 0; k < count;) {

@@ -199,7 +199,7 @@ struct EmbedGrad {
   const void* d_out;
   int64_t ldo;
   EmbedSort sort;
-  int vocab, d, run;                      // run: positions of the sorted list that are added up by one team
+  int vocab, d, run;                      // run: positions of the sorted list that are added up by one team (few places: rows of zeros to a workgroup)
   int64_t n, runs;
   int cols, sums;                         // pieces of a row, and workgroups that add up; the others write zeros
   float scale;
@@ -360,17 +360,17 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedGrad p) {
 
 // Few places: one launch without sorting.  Every place has a team, which compares its token with all ids at once; the first
 // place of a token goes on and adds up the rows of all its places in their order.  Against the three launches below, in us, bfloat16,
-// tokens as in text / all different / all the same, 4 000 tokens of vocabulary: 256 places of 1 024 columns 6.5 / 6.4 / 18 (three launches
-// 15.7 / 14.4 / 13), 512 7.2 / 7.1 / 31 (15.6 / 15.7 / 14), 1 024 9 / 9 / 58 (16 / 16 / 17); 512 of 4 096 columns 17 / 18 / 37 (21 / 21 / 21), 1 024
+// tokens as in text / all different / all the same, 4 000 tokens of vocabulary: 256 places of 1 024 columns 6.3 / 6.0 / 17 (three launches
+// 15.7 / 14.4 / 13), 512 6.6 / 6.9 / 30 (15.6 / 15.7 / 14), 1 024 9 / 9 / 58 (16 / 16 / 17); 512 of 4 096 columns 15 / 17 / 38 (21 / 21 / 21), 1 024
 // 22 / 24 / 67 (24 / 23 / 24): what one token costs a single team ends the rule at 512.
-constexpr int FEW = 512, FEW_ZERO_ROWS = 16;
+constexpr int FEW = 512, FEW_ZERO_ROWS = 16;     // at most: as many rows of zeros to a workgroup as leave 1 024 of them
 template <typename T, int W, int NV, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __restrict__ ids) {
   constexpr int TEAM = 64 * W, TEAMS = 4 / W;
   __shared__ int places[4][FEW];                 // each wavefront's own list
   const int n = (int)p.n, lane = threadIdx.x & 63;
   if ((int)blockIdx.x >= p.sums) {
-    const int v0 = ((int)blockIdx.x - p.sums) * FEW_ZERO_ROWS, rows = p.vocab - v0 < FEW_ZERO_ROWS ? p.vocab - v0 : FEW_ZERO_ROWS;
+    const int v0 = ((int)blockIdx.x - p.sums) * p.run, rows = p.vocab - v0 < p.run ? p.vocab - v0 : p.run;
     int* there = places[0];
     if (threadIdx.x < FEW_ZERO_ROWS) there[threadIdx.x] = 0;
     __syncthreads();
@@ -474,7 +474,8 @@ int launch_embed_few_team(EmbedGrad p, const int* ids, hipStream_t s) {
   constexpr int TEAMS = 4 / W, COLS = 64 * W * 4 * NV;
   p.cols = (p.d + COLS - 1) / COLS;
   p.sums = (int)((p.n + TEAMS - 1) / TEAMS) * p.cols;
-  const int zeros = p.accumulate ? 0 : (p.vocab + FEW_ZERO_ROWS - 1) / FEW_ZERO_ROWS;
+  p.run = p.vocab < 2048 ? 1 : p.vocab / 1024 < FEW_ZERO_ROWS ? p.vocab / 1024 : FEW_ZERO_ROWS;
+  const int zeros = p.accumulate ? 0 : (p.vocab + p.run - 1) / p.run;
   hipLaunchKernelGGL((k_embed_few<T, W, NV, SHORT>), dim3((unsigned)(p.sums + zeros)), dim3(256), 0, s, p, ids);
   return launch_status("embedding_backward");
 }
