@@ -17,6 +17,7 @@ namespace ae {
 namespace {
 
 constexpr float kDown = 7.8886090522101181e-31f;   // 2^-100
+constexpr float kUp = 1.2676506002282294e30f;       // 2^100
 
 // eight elements as numbers, zeros behind the row's end
 template <typename T>
@@ -266,13 +267,19 @@ struct NormGradArgs {
   bool stream;
 };
 
-// u = h times down (1 or 2^-100) times r; the gradient's common factor is r times down
+// u = h times down times r, where down is 1, or 2^-100 if the sum of h^2 leaves binary32; likewise g is taken times less
+// if the sum of g h does, and mean is that of such g
 struct RowStat {
-  float r, down, mean;                    // mean(g u)
+  float r, down, less, mean;
 };
-__device__ __forceinline__ RowStat row_stat(float hh, float gh, int d, float eps, bool down) {
+__device__ __forceinline__ RowStat row_stat(float hh, float gh, int d, float eps, bool down, bool far) {
   const float r = rms_inverse(hh, d, eps, down);
-  return {r, down ? kDown : 1.0f, r * gh / (float)d};
+  return {r, down ? kDown : 1.0f, far ? kDown : 1.0f, r * gh / (float)d};
+}
+// the gradient of h; of the powers of two only what is left of both is taken out, at the end
+__device__ __forceinline__ float norm_grad(const RowStat& s, float dy, float w, float u) {
+  const float tail = s.less == 1.0f ? s.down : s.down * kUp;
+  return (dy * s.less * w - u * s.mean) * s.r * tail;
 }
 
 template <typename T, int LANES, int NV, bool STREAM>
@@ -341,9 +348,9 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
       }
     };
     sums(sm[turn]);
-    const bool down = !(hh <= FLT_MAX) || !(fabsf(gh) <= FLT_MAX);
-    if (LANES <= 64 ? __any(down) : down) {        // of several rows in a wavefront the others are multiplied by one
-      const float by = down ? kDown : 1.0f;
+    const bool down = !(hh <= FLT_MAX), far = !(fabsf(gh) <= FLT_MAX);
+    if (LANES <= 64 ? __any(down || far) : down || far) {      // of several rows in a wavefront the others are multiplied by one
+      const float by = down ? kDown : 1.0f, less = far ? kDown : 1.0f;
       hh = gh = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
@@ -351,13 +358,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
         for (int j = 0; j < 8; ++j) {
           h[v][j] *= by;
           hh = fmaf(h[v][j], h[v][j], hh);
-          gh = fmaf(dy[v][j] * w[v][j], h[v][j], gh);
+          gh = fmaf(dy[v][j] * less * w[v][j], h[v][j], gh);
         }
       if constexpr (LANES > 64) __syncthreads();
       sums(sm[2]);
       if constexpr (LANES > 64) __syncthreads();
     }
-    const RowStat st = row_stat(hh, gh, p.d, p.eps, down);
+    const RowStat st = row_stat(hh, gh, p.d, p.eps, down, far);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int col = (v * LANES + t) * 8;
@@ -366,7 +373,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
       for (int j = 0; j < 8; ++j) {
         const float u = h[v][j] * st.r;
         if (live) acc[v][j] = fmaf(dy[v][j], u, acc[v][j]);
-        o[j] = (dy[v][j] * w[v][j] - u * st.mean) * st.r * st.down + add[v][j];
+        o[j] = norm_grad(st, dy[v][j], w[v][j], u) + add[v][j];
       }
       if (p.dx && live && col < p.d) put((T*)p.dx + row * p.lddx + col, p.d - col, o);
     }
@@ -396,13 +403,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
   }
 }
 
-// Rows that registers do not hold: r, 2^0 or 2^-100 and mean(g u) of every row first, then the gradients by columns.
+// Rows that registers do not hold: the RowStat of every row first, then the gradients by columns.
 template <typename T>
 __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
   __shared__ float sm[4][WIDE / 64];
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     float hh, gh;
-    auto sums = [&](float by) {
+    auto sums = [&](float by, float less) {
       hh = gh = 0.0f;
       for (int col = threadIdx.x * 8; col < p.d; col += WIDE * 8) {
         float h[8], g[8], w[8];
@@ -413,23 +420,23 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
         for (int j = 0; j < 8; ++j) {
           h[j] *= by;
           hh = fmaf(h[j], h[j], hh);
-          gh = fmaf(p.weight ? g[j] * w[j] : g[j], h[j], gh);
+          gh = fmaf(p.weight ? g[j] * less * w[j] : g[j] * less, h[j], gh);
         }
       }
     };
-    sums(1.0f);
+    sums(1.0f, 1.0f);
     hh = team_sum<WIDE>(hh, sm[0]);
     gh = team_sum<WIDE>(gh, sm[1]);
-    const bool down = !(hh <= FLT_MAX) || !(fabsf(gh) <= FLT_MAX);
-    if (down) {
-      sums(kDown);
+    const bool down = !(hh <= FLT_MAX), far = !(fabsf(gh) <= FLT_MAX);
+    if (down || far) {
+      sums(down ? kDown : 1.0f, far ? kDown : 1.0f);
       hh = team_sum<WIDE>(hh, sm[2]);
       gh = team_sum<WIDE>(gh, sm[3]);
     }
-    const RowStat st = row_stat(hh, gh, p.d, p.eps, down);
+    const RowStat st = row_stat(hh, gh, p.d, p.eps, down, far);
     if (threadIdx.x == 0) {
       float* at = p.stat + row * 4;
-      at[0] = st.r; at[1] = st.down; at[2] = st.mean;
+      at[0] = st.r; at[1] = st.down; at[2] = st.less; at[3] = st.mean;
     }
     __syncthreads();
   }
@@ -444,7 +451,7 @@ __global__ __launch_bounds__(256) void k_rms_norm_grad_columns(NormGradArgs p) {
   for (int j = 0; j < 8; ++j) { w[j] = 1.0f; acc[j] = 0.0f; }
   if (p.weight) numbers(p.weight + col, left, w);
   for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
-    const RowStat st = {p.stat[row * 4], p.stat[row * 4 + 1], p.stat[row * 4 + 2]};
+    const RowStat st = {p.stat[row * 4], p.stat[row * 4 + 1], p.stat[row * 4 + 2], p.stat[row * 4 + 3]};
     float h[8], dy[8], add[8], o[8];
     numbers((const T*)p.h + row * p.ldh + col, left, h);
     numbers((const T*)p.dy + row * p.ldy + col, left, dy);
@@ -453,7 +460,7 @@ __global__ __launch_bounds__(256) void k_rms_norm_grad_columns(NormGradArgs p) {
     for (int j = 0; j < 8; ++j) {
       const float u = h[j] * st.down * st.r;
       acc[j] = fmaf(dy[j], u, acc[j]);
-      o[j] = (dy[j] * w[j] - u * st.mean) * st.r * st.down + (p.d_h ? add[j] : 0.0f);
+      o[j] = norm_grad(st, dy[j], w[j], u) + (p.d_h ? add[j] : 0.0f);
     }
     if (p.dx) put((T*)p.dx + row * p.lddx + col, left, o);
   }

@@ -207,6 +207,43 @@ def test_backward_of_unusual_rows(d):
     assert np.all(np.isnan(host(dx)[6]))
 
 
+@pytest.mark.parametrize("d", [96, 200, 3000, 9000])
+def test_backward_where_only_the_sum_of_products_leaves_the_range(d):
+    """Gradients along h whose products with it add up beyond binary32, at ordinary, small (eps as large as the mean) and large h; other rows of the
+    same wavefront are not affected, nor is the weight's gradient by an infinite or NaN gradient of another column."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(d)
+    h = rng.standard_normal((9, d)).astype(np.float32)
+    dy = rng.standard_normal((9, d)).astype(np.float32)
+    h[2] *= np.float32(1e-3)
+    h[4] *= np.float32(1e20)
+    big = np.float32(3e38 / d * 4)
+    dy[0] = np.sign(h[0]) * big
+    dy[2] = np.sign(h[2]) * np.float32(1e35)
+    h[2, :8] = np.float32(1e5)                       # the products here leave the range, the mean is far above eps
+    dy[4] *= np.float32(1e25)
+    dy[6] = np.sign(h[6]) * big
+    ws, dx, dw = space(ae.model_rms_norm_backward_workspace(9, d, ae.AE_F32)), torch.empty((9, d), device="cuda"), torch.empty(d, device="cuda")
+    ae.model_rms_norm_backward(dev(dy), dev(h), 9, d, None, 1e-6, dx, dw, ws)
+    want, d_w, mag, mag_w = to.rms_norm_backward(dy, h, None, 1e-6)
+    near(host(dx), want, grad_bound(want, mag, d, "f32"))
+    near(host(dw), d_w, (9 + 45 + d / 2048) * U * mag_w + TINY)
+    # an infinity and a NaN among gradients of rows whose mean of squares is as small as eps
+    h = (rng.standard_normal((9, d)) * 1e-3).astype(np.float32)
+    dy = rng.standard_normal((9, d)).astype(np.float32)
+    _, d_w, _, mag_w = to.rms_norm_backward(dy, h, None, 1e-6)
+    dy[3, 5], dy[7, d - 1] = np.inf, np.nan
+    ae.model_rms_norm_backward(dev(dy), dev(h), 9, d, None, 1e-6, dx, dw, ws)
+    other = np.ones(d, bool)
+    other[[5, d - 1]] = False
+    near(host(dw)[other], d_w[other], (9 + 45 + d / 2048) * U * mag_w[other] + TINY)
+    assert np.isinf(host(dw)[5]) and np.isnan(host(dw)[d - 1])
+    fine = [0, 1, 2, 4, 5, 6, 8]
+    want, _, mag, _ = to.rms_norm_backward(dy[fine], h[fine], None, 1e-6)
+    near(host(dx)[fine], want, grad_bound(want, mag, d, "f32"))
+
+
 def test_backward_against_differences_of_the_forward_pass():
     """In binary32: differences over 2^-4, whose error is of third order in it and the forward pass's rounding over it."""
     import torch
