@@ -146,9 +146,19 @@ def _ptr(t, dtype=None):
     return C.c_void_p(t.data_ptr())
 
 
+_current_device = torch._C._cuda_getDevice
+
+
 def _raw_stream():
     """The current stream of the current device as a number: what _stream() wraps, without the Stream object in between."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return torch._C._cuda_getCurrentRawStream(_current_device())
+
+
+def _raw_stream_for(device):
+    """The same, for tensors on this device: a call runs on the current one."""
+    current = _current_device()
+    assert device == current, "tensors on device %d, the current one is %d" % (device, current)
+    return torch._C._cuda_getCurrentRawStream(current)
 
 
 def _mat(t, rows, cols, dtype=None):
@@ -635,7 +645,7 @@ def model_rms_norm(x, rows, d, weight, eps, h=None, y=None, q=None, scale=None, 
     yp, ldy = _mat(y, rows, d, x.dtype)
     qp, ldq = _codes(q, rows, d)
     _check(lib.model_rms_norm(xp, ldx, rp, ldr, _vec(weight, d), rows, d, eps, _dtype_of(x), hp, ldh, yp, ldy, qp, ldq,
-                              _fp8_scales(scale, rows, d, "rows"), _raw_stream()))
+                              _fp8_scales(scale, rows, d, "rows"), _raw_stream_for(x.get_device())))
 
 
 @functools.lru_cache(maxsize=1024)                # by sizes alone
@@ -653,14 +663,14 @@ def model_rms_norm_backward(dy, h, rows, d, weight, eps, dx, d_weight, workspace
     dp, ldd = _mat(dx, rows, d, dy.dtype)
     dtype = _dtype_of(dy)
     _check(lib.model_rms_norm_backward(gp, ldy, hp, ldh, _vec(weight, d), ap, lda, rows, d, eps, dtype, dp, ldd, _vec(d_weight, d),
-                                       _room(workspace, model_rms_norm_backward_workspace(rows, d, dtype)), _raw_stream()))
+                                       _room(workspace, model_rms_norm_backward_workspace(rows, d, dtype)), _raw_stream_for(dy.get_device())))
 
 
 def model_embedding(table, vocab, d, ids, n, out, scale=1.0):
     """out[i] = scale * table[ids[i]]; zeros for an id outside 0 .. vocab - 1."""
     tp, ldt = _mat(table, vocab, d)
     op, ldo = _mat(out, n, d, table.dtype)
-    _check(lib.model_embedding(tp, ldt, vocab, d, _vec(ids, n, torch.int32), n, scale, _dtype_of(table), op, ldo, _raw_stream()))
+    _check(lib.model_embedding(tp, ldt, vocab, d, _vec(ids, n, torch.int32), n, scale, _dtype_of(table), op, ldo, _raw_stream_for(table.get_device())))
 
 
 @functools.lru_cache(maxsize=1024)                # by sizes alone
@@ -676,7 +686,7 @@ def model_embedding_backward(d_out, ids, n, vocab, d, d_table, workspace, scale=
     tp, ldt = _mat(d_table, vocab, d, torch.float32)
     dtype = _dtype_of(d_out)
     _check(lib.model_embedding_backward(gp, ldo, _vec(ids, n, torch.int32), n, vocab, d, scale, dtype, tp, ldt, 1 if accumulate else 0,
-                                        _room(workspace, model_embedding_backward_workspace(n, vocab, d, dtype)), _raw_stream()))
+                                        _room(workspace, model_embedding_backward_workspace(n, vocab, d, dtype)), _raw_stream_for(d_table.get_device())))
 
 
 class GradList:
@@ -690,6 +700,9 @@ class GradList:
             assert g.is_cuda and g.is_contiguous() and g.dtype in (torch.float32, torch.bfloat16), "contiguous device tensors in float32 or bfloat16 required"
         assert out is None or (len(out) == len(grads) and all(o.numel() == g.numel() and o.dtype == g.dtype for o, g in zip(out, grads))), \
             "as many outputs as gradients, of their sizes and types"
+        devices = {g.get_device() for g in grads + (out or [])}
+        assert len(devices) <= 1, "tensors of one device required"
+        self.device = devices.pop() if devices else None
         self.grads, self.out, n = grads, out, len(grads)
         self._grads = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
         self._out = None if out is None else (C.c_void_p * n)(*[o.data_ptr() for o in out])
@@ -707,7 +720,7 @@ def model_grad_clip_workspace(grads):
 def model_grad_clip(grads, max_norm, norm, workspace):
     """norm[0] = the norm of a GradList's gradients together; each times min(1, max_norm / norm) into its output (norm may be None)."""
     _check(lib.model_grad_clip(grads._grads, grads._sizes, grads._dtypes, len(grads.grads), max_norm, _vec(norm, 1), grads._out,
-                               _room(workspace, grads.workspace_bytes), _raw_stream()))
+                               _room(workspace, grads.workspace_bytes), _raw_stream() if grads.device is None else _raw_stream_for(grads.device)))
 
 
 def model_logits_adjust(logits, rows, vocab, out, history=None, n_prompt=None, repetition=None, presence=None, frequency=None, bias_id=None, bias=None,
@@ -722,7 +735,7 @@ def model_logits_adjust(logits, rows, vocab, out, history=None, n_prompt=None, r
     _check(lib.model_logits_adjust(zp, rows, vocab, ld, _dtype_of(logits), _vec(history, rows * n_history, torch.int32), n_history,
                                    _vec(n_prompt, rows, torch.int32), _vec(repetition, rows), _vec(presence, rows), _vec(frequency, rows),
                                    _vec(bias_id, rows * n_bias, torch.int32), _vec(bias, rows * n_bias), n_bias,
-                                   _vec(allowed, rows * -(-vocab // 32), torch.int32), op, ldo, _raw_stream()))
+                                   _vec(allowed, rows * -(-vocab // 32), torch.int32), op, ldo, _raw_stream_for(logits.get_device())))
 
 
 def model_calibrate_mfma(lds_reads, random_data=0, iters=4000):

@@ -96,3 +96,22 @@ def test_decoding_step(tokens, d, vocab, rows):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a[:rows], st[k][:rows]) for a, k in zip(first, ("best", "best_logprob", "logits")))
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    x, ids, w = torch.zeros((4, 64), device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    lst, y = ae.GradList([x]), torch.full((4, 64), 7.0, device="cuda")
+    calls = [lambda: ae.model_rms_norm(x, 4, 64, None, 1e-6, y=y), lambda: ae.model_rms_norm_backward(x, x, 4, 64, None, 1e-6, y, None, w),
+             lambda: ae.model_embedding(x, 4, 64, ids, 4, y), lambda: ae.model_embedding_backward(x, ids, 4, 4, 64, y, w),
+             lambda: ae.model_grad_clip(lst, 1.0, y[0, :1], w), lambda: ae.model_logits_adjust(x, 4, 64, y)]
+    with monkeypatch.context() as m:
+        m.setattr(ae, "_current_device", lambda: 1)
+        for call in calls:
+            with pytest.raises(AssertionError, match="device 0"):
+                call()
+    torch.cuda.synchronize()
+    assert bool((y == 7).all())
+    for call in calls:
+        call()
