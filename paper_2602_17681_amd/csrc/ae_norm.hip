@@ -28,10 +28,15 @@ __device__ __forceinline__ void numbers(const T* p, int left, float (&v)[8]) {
   for (int i = 0; i < 8; ++i) v[i] = value(e, i);
 }
 
-// sum over the lanes that share a row: 16, 32 or 64 of a wavefront, or several wavefronts; sm is not written again before the
+// sum over the lanes that share a row: 8, 16, 32 or 64 of a wavefront, or several wavefronts; sm is not written again before the
 // workgroup's next barrier but one
 template <int LANES>
 __device__ __forceinline__ float team_sum(float v, float* sm) {
+  if constexpr (LANES == 8) {
+    v += __shfl_xor(v, 4, 64);
+    v += __shfl_xor(v, 2, 64);
+    return v + __shfl_xor(v, 1, 64);
+  }
   v = sum16(v);
   if constexpr (LANES == 32) return v + __shfl_xor(v, 16, 64);
   if constexpr (LANES >= 64) v = sum_rows(v);
@@ -62,8 +67,16 @@ struct NormArgs {
   bool stream;
 };
 
-// eight results of a row from column col on (behind the row's end: none); the 16 lanes of a block of 128 come here together
-template <typename T>
+// the largest value of the 16 lanes that hold a block of 128, or of 8 that hold a row of 64
+template <int LANES>
+__device__ __forceinline__ float block_max(float v) {
+  if constexpr (LANES != 8) return max16(v);
+  v = fmaxf(v, __shfl_xor(v, 4, 64));
+  v = fmaxf(v, __shfl_xor(v, 2, 64));
+  return fmaxf(v, __shfl_xor(v, 1, 64));
+}
+// eight results of a row from column col on (behind the row's end: none); the lanes of a block of 128 come here together
+template <typename T, int LANES>
 __device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, const float (&y)[8]) {
   const int left = p.d - col;
   if (p.y && left > 0) put((T*)p.y + row * p.ldy + col, left, y);
@@ -71,20 +84,20 @@ __device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, co
   float m = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
-  m = max16(m);
+  m = block_max<LANES>(m);
   const bool inf = __any(m > FLT_MAX);
   if (inf) {
     m = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(y[j]));
-    m = max16(m);
+    m = block_max<LANES>(m);
   }
   const float s = block_scale(m), inv = 1.0f / s;
   float u[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) u[j] = inf ? code_value<true>(y[j], inv) : code_value<false>(y[j], inv);
   if (left <= 0) return;
-  if ((threadIdx.x & 15) == 0) p.scale[(int64_t)(col / BLK) * p.rows + row] = s;
+  if (threadIdx.x % (LANES == 8 ? 8 : 16) == 0) p.scale[(int64_t)(col / BLK) * p.rows + row] = s;
   uint8_t* at = p.q + row * p.ldq + col;
   const uint32_t lo = codes4(u[0], u[1], u[2], u[3]), hi = codes4(u[4], u[5], u[6], u[7]);
   if (left >= 8) {
@@ -103,7 +116,7 @@ __device__ __forceinline__ float rms_inverse(float sum, int d, float eps, bool d
 template <typename T, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs p) {
   constexpr int TEAMS = LANES < 256 ? 256 / LANES : 1, W = LANES / 64 ? LANES / 64 : 1;
-  constexpr bool SHORT = LANES == 16;
+  constexpr bool SHORT = LANES == 8;
   __shared__ float sm[3][W];
   const int t = threadIdx.x % LANES, team = threadIdx.x / LANES, step = (int)gridDim.x * TEAMS;
   const T* x = (const T*)p.x;
@@ -173,7 +186,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] *= value(w[v], j);
       }
-      emit<T>(p, row, live ? (v * LANES + t) * 8 : p.d, y);
+      emit<T, LANES>(p, row, live ? (v * LANES + t) * 8 : p.d, y);
     }
   }
 }
@@ -217,7 +230,7 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
       if (p.h && col < p.d) put((T*)p.h + row * p.ldh + col, p.d - col, h);
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = (down ? h[j] * kDown : h[j]) * r * w[j];
-      emit<T>(p, row, col, y);
+      emit<T, WIDE>(p, row, col, y);
     }
     __syncthreads();
   }
@@ -230,11 +243,12 @@ int launch_norm_row(const NormArgs& p, hipStream_t s) {
   hipLaunchKernelGGL((p.stream ? k_rms_norm<T, LANES, NV, true> : k_rms_norm<T, LANES, NV, false>), dim3((unsigned)(want < most ? want : most)), dim3(LANES < 256 ? 256 : LANES), 0, s, p);
   return launch_status("rms_norm");
 }
-// Lanes by the row's length.  262 144 x 128 in bfloat16 16 lanes 43 us, 64 lanes 116; 131 072 x 256 32 lanes 43, 64 lanes 60;
+// Lanes by the row's length.  524 288 x 64 in bfloat16 8 lanes 44 us, 16 lanes 86; 262 144 x 128 16 lanes 43, 64 lanes 116; 131 072 x 256 32 lanes 43, 64 lanes 60;
 // 16 384 x 4 096 256 lanes of two pieces 81, 512 of one 83, 64 of eight 155; 1 677 x 20 000 read twice 71, 1 024 lanes of four pieces (which
 // spill) 147.
 template <typename T>
 int launch_norm(const NormArgs& p, hipStream_t s) {
+  if (p.d <= 64) return launch_norm_row<T, 8, 1>(p, s);
   if (p.d <= 128) return launch_norm_row<T, 16, 1>(p, s);
   if (p.d <= 256) return launch_norm_row<T, 32, 1>(p, s);
   if (p.d <= 512) return launch_norm_row<T, 64, 1>(p, s);
@@ -285,7 +299,7 @@ __device__ __forceinline__ float norm_grad(const RowStat& s, float dy, float w, 
 template <typename T, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(NormGradArgs p) {
   constexpr int TEAMS = LANES < 256 ? 256 / LANES : 1, W = LANES / 64 ? LANES / 64 : 1;
-  constexpr bool SHORT = LANES == 16;
+  constexpr bool SHORT = LANES == 8;
   __shared__ float sm[3][2][W];
   __shared__ float join[TEAMS > 1 ? TEAMS - 1 : 1][TEAMS > 1 ? NV * LANES * 8 : 1];
   const int t = threadIdx.x % LANES, team = threadIdx.x / LANES, step = (int)gridDim.x * TEAMS;
@@ -496,7 +510,7 @@ constexpr int kInRegisters = 8192;                 // columns of a row, beside i
 // in two passes 49 (12 288) and 44 (16 384), in 1 024 lanes' registers 110 and 103.
 int64_t grad_groups(int64_t rows, int64_t d) {
   if (d > kInRegisters) return rows < 64 ? rows : 64;
-  const int64_t teams = d <= 128 ? 16 : d <= 256 ? 8 : d <= 1024 ? 4 : 1;
+  const int64_t teams = d <= 64 ? 32 : d <= 128 ? 16 : d <= 256 ? 8 : d <= 1024 ? 4 : 1;
   const int64_t want = (rows + teams - 1) / teams, most = d <= 512 || (d > 1024 && d <= 2048) ? 1024 : d <= 4096 ? 512 : 256;
   return want < most ? want : most;
 }
@@ -509,6 +523,7 @@ int launch_grad_row(const NormGradArgs& p, int64_t groups, hipStream_t s) {
 }
 template <typename T>
 int launch_grad(const NormGradArgs& p, int64_t groups, hipStream_t s) {
+  if (p.d <= 64) return launch_grad_row<T, 8, 1>(p, groups, s);
   if (p.d <= 128) return launch_grad_row<T, 16, 1>(p, groups, s);
   if (p.d <= 256) return launch_grad_row<T, 32, 1>(p, groups, s);
   if (p.d <= 512) return launch_grad_row<T, 64, 1>(p, groups, s);

@@ -8,10 +8,10 @@ pytestmark = pytest.mark.gpu
 
 
 def test_norm_of_more_rows_than_one_round_takes():
-    """2^20 workgroups of 16 rows each, rows shorter than a piece."""
+    """2^20 workgroups of 32 rows each, rows shorter than a piece."""
     import torch
     from paper_2602_17681_amd import binding as ae
-    rows, d = (1 << 24) + 21, 3
+    rows, d = (1 << 25) + 21, 3
     x = torch.randn((rows, d), device="cuda").to(torch.bfloat16)
     y = torch.empty_like(x)
     ae.model_rms_norm(x, rows, d, None, 1e-5, y=y)
