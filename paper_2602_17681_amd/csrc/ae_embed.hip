@@ -17,7 +17,7 @@ namespace {
 
 // LANES threads take a row in pieces of eight elements, 256 / LANES rows at a time and U of them in flight; the scaled value
 // is rounded once.
-template <typename T, int LANES, int U>
+template <typename T, int LANES, int U, bool STREAM>
 __global__ __launch_bounds__(256) void k_embedding(const T* __restrict__ table, int64_t ldt, int64_t vocab, int d, const int* __restrict__ ids,
                                                    int64_t n, float scale, T* __restrict__ out, int64_t ldo, int64_t first) {
   constexpr int ROWS = 256 / LANES;
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void k_embedding(const T* __restrict__ table, 
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = at[u] < 0 ? 0.0f : value(e[u], j) * scale;
-      put(out + (i0 + u * ROWS) * ldo + col, left, v);
+      put<STREAM>(out + (i0 + u * ROWS) * ldo + col, left, v);
     }
   }
 }
@@ -503,14 +503,14 @@ int check_embedding(const char* who, int64_t n, int64_t vocab, int64_t d, int dt
 }
 bool stride_ok(int64_t ld, int64_t d) { return ld >= d && ld < ((int64_t)1 << 40); }
 
-template <typename T, int LANES, int U>
+template <typename T, int LANES, int U, bool STREAM = false>
 int launch_embedding(const void* table, int64_t ldt, int64_t vocab, int64_t d, const int* ids, int64_t n, float scale, void* out, int64_t ldo,
                      hipStream_t s) {
   const int64_t rows = 256 / LANES * U, want = (n + rows - 1) / rows, pieces = (d + LANES * 8 - 1) / (LANES * 8);
   const int64_t cols = pieces < 64 ? pieces : 64, most = launch_blocks(256) / cols;
   for (int64_t first = 0; first < want; first += most) {
     const int64_t left = want - first;
-    hipLaunchKernelGGL((k_embedding<T, LANES, U>), dim3((unsigned)(left < most ? left : most), (unsigned)cols), dim3(256), 0, s, (const T*)table, ldt, vocab,
+    hipLaunchKernelGGL((k_embedding<T, LANES, U, STREAM>), dim3((unsigned)(left < most ? left : most), (unsigned)cols), dim3(256), 0, s, (const T*)table, ldt, vocab,
                        (int)d, ids, n, scale, (T*)out, ldo, first);
   }
   return launch_status("embedding");
@@ -521,6 +521,7 @@ int launch_embedding_rows(const void* table, int64_t ldt, int64_t vocab, int64_t
   if (d <= 128) return launch_embedding<T, 16, 1>(table, ldt, vocab, d, ids, n, scale, out, ldo, s);
   if (d <= 512) return launch_embedding<T, 64, 1>(table, ldt, vocab, d, ids, n, scale, out, ldo, s);
   if (n < 1024) return launch_embedding<T, 256, 1>(table, ldt, vocab, d, ids, n, scale, out, ldo, s);
+  if (2 * n * d * (int64_t)sizeof(T) > kStreamBytes) return launch_embedding<T, 256, 4, true>(table, ldt, vocab, d, ids, n, scale, out, ldo, s);
   return launch_embedding<T, 256, 4>(table, ldt, vocab, d, ids, n, scale, out, ldo, s);
 }
 

@@ -16,6 +16,7 @@ namespace {
 constexpr int NT = 512;
 // a column's word: bits 0 .. 19 how often among the answers, bit 20 in the prompt, bits 21 .. 31 place in the list of biases + 1
 constexpr uint32_t kCount = (1u << 20) - 1, kPrompt = 1u << 20, kSeen = kCount | kPrompt;
+constexpr int AHEAD = 4;                         // tokens of the history that a thread asks for at once
 constexpr int kBiasAt = 21, kMaxHistory = kCount, kMaxBias = 2047;
 
 struct AdjustArgs {
@@ -35,6 +36,21 @@ struct AdjustArgs {
   int slices;
   int64_t first;
 };
+
+// -infinity in the place of the elements whose bit is 0, in the elements' own form
+template <typename T, int N>
+__device__ __forceinline__ void forbid(uint32_t ok, Piece<T, N>& e) {
+#pragma unroll
+  for (int i = 0; i < Piece<T, N>::WORDS; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      e.w[i] = ok >> i & 1 ? e.w[i] : 0xFF800000u;
+    } else {
+      const uint32_t lo = (uint32_t)((int)(ok << (31 - 2 * i)) >> 31), hi = (uint32_t)((int)(ok << (30 - 2 * i)) >> 31);      // all bits or none
+      const uint32_t keep = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+      e.w[i] = (e.w[i] & keep) | (0xFF80FF80u & ~keep);
+    }
+  }
+}
 
 template <typename T, int NP, bool LISTS>
 __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
@@ -57,23 +73,35 @@ __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
   }
   float repetition = 1.0f, presence = 0.0f, frequency = 0.0f;
   if constexpr (LISTS) {
+    // the lists' first entries are asked for with the logits
+    const int t = threadIdx.x, prompt = p.n_prompt ? p.n_prompt[row] : 0;
+    const int bias0 = t < p.n_bias ? p.bias_id[row * p.n_bias + t] : -1;
+    int token[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) token[k] = k * NT + t < p.n_history ? p.history[row * p.n_history + k * NT + t] : -1;
     for (int i = threadIdx.x; i < S / 4; i += NT) word4[i] = make_uint4(0, 0, 0, 0);
     if (p.repetition) repetition = p.repetition[row];
     if (p.presence) presence = p.presence[row];
     if (p.frequency) frequency = p.frequency[row];
     __syncthreads();
-    for (int i = threadIdx.x; i < p.n_bias; i += NT) {
-      const unsigned c = (unsigned)p.bias_id[row * p.n_bias + i] - (unsigned)s0;
+    auto set_bias = [&](int i, int id) {
+      const unsigned c = (unsigned)id - (unsigned)s0;
       if (c < (unsigned)mine) atomicMax(&word[c], (uint32_t)(i + 1) << kBiasAt);       // the last entry of a token counts
-    }
-    if (p.n_bias) __syncthreads();
-    const int prompt = p.n_prompt ? p.n_prompt[row] : 0;
-    for (int i = threadIdx.x; i < p.n_history; i += NT) {
-      const unsigned c = (unsigned)p.history[row * p.n_history + i] - (unsigned)s0;
-      if (c >= (unsigned)mine) continue;
+    };
+    auto count = [&](int i, int id) {
+      const unsigned c = (unsigned)id - (unsigned)s0;
+      if (c >= (unsigned)mine) return;
       if (i < prompt) atomicOr(&word[c], kPrompt);
       else atomicAdd(&word[c], 1u);
+    };
+    if (p.n_bias) {
+      set_bias(t, bias0);
+      for (int i = t + NT; i < p.n_bias; i += NT) set_bias(i, p.bias_id[row * p.n_bias + i]);
+      __syncthreads();
     }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) count(k * NT + t, token[k]);
+    for (int i = AHEAD * NT + t; i < p.n_history; i += NT) count(i, p.history[row * p.n_history + i]);
     __syncthreads();
   }
   const bool in_place = p.logits == p.out;
@@ -82,35 +110,34 @@ __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
     const int c = (k * NT + (int)threadIdx.x) * VEC;
     if (c >= mine) continue;
     if (mine < S) settle<true>(s0 + c, p.vocab, e[k]);
-    float v[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) v[j] = value(e[k], j);
+    T* const at_out = (T*)p.out + row * p.ldo + s0 + c;
+    uint32_t w[VEC], touched = 0;
     if constexpr (LISTS) {
-      uint32_t w[VEC], any = 0;
 #pragma unroll
       for (int j = 0; j < VEC; j += 4) {
         const uint4 a = word4[(c + j) / 4];
         w[j] = a.x; w[j + 1] = a.y; w[j + 2] = a.z; w[j + 3] = a.w;
-        any |= a.x | a.y | a.z | a.w;
+        touched |= a.x | a.y | a.z | a.w;
       }
-      const bool touched = any != 0;
-      if (in_place && !touched && ok[k] == ALL) continue;      // stays as it is
-      if (touched) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          if (w[j] & kSeen) v[j] = v[j] > 0.0f ? v[j] / repetition : v[j] * repetition;
-          if (w[j] & kCount) v[j] = v[j] - frequency * (float)(w[j] & kCount) - presence;
-          if (w[j] >> kBiasAt) v[j] += p.bias[row * p.n_bias + (w[j] >> kBiasAt) - 1];
-        }
-      }
-    } else {
-      if (in_place && ok[k] == ALL) continue;
     }
+    if (in_place && !touched && ok[k] == ALL) continue;        // stays as it is
+    if (touched) {
+      float v[VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j)
-      if (!(ok[k] >> j & 1)) v[j] = -INFINITY;
-    if (mine == S) put_whole<false>((T*)p.out + row * p.ldo + s0 + c, v);
-    else put((T*)p.out + row * p.ldo + s0 + c, mine - c, v);
+      for (int j = 0; j < VEC; ++j) v[j] = value(e[k], j);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        if (w[j] & kSeen) v[j] = v[j] > 0.0f ? v[j] / repetition : v[j] * repetition;
+        if (w[j] & kCount) v[j] = v[j] - frequency * (float)(w[j] & kCount) - presence;
+        if (w[j] >> kBiasAt) v[j] += p.bias[row * p.n_bias + (w[j] >> kBiasAt) - 1];
+      }
+      make_piece(v, e[k]);
+    }
+    forbid(ok[k], e[k]);
+    if (mine - c >= VEC) put_piece<false>(at_out, e[k]);
+    else
+      for (int j = 0; j < VEC; ++j)
+        if (j < mine - c) Store<T>::st(at_out + j, value(e[k], j));
   }
 }
 

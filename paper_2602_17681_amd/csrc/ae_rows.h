@@ -113,19 +113,34 @@ __device__ __forceinline__ float value(const Piece<T, N>& e, int i) {
   if constexpr (sizeof(T) == 4) return __uint_as_float(e.w[i]);
   return __uint_as_float(i & 1 ? e.w[i >> 1] & 0xFFFF0000u : e.w[i >> 1] << 16);
 }
+// rounded to nearest, ties to even
+template <typename T, int N>
+__device__ __forceinline__ void make_piece(const float (&v)[N], Piece<T, N>& e) {
+#pragma unroll
+  for (int i = 0; i < Piece<T, N>::WORDS; ++i) {
+    if constexpr (sizeof(T) == 4) e.w[i] = __float_as_uint(v[i]);
+    else e.w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  }
+}
 template <bool STREAM, typename T, int N>
-__device__ __forceinline__ void put_whole(T* p, const float (&v)[N]) {
+__device__ __forceinline__ void put_piece(T* p, const Piece<T, N>& e) {
   typedef typename Words<T, N>::type words;
   constexpr int PER = Words<T, N>::PER;
 #pragma unroll
   for (int i = 0; i < Words<T, N>::COUNT; ++i) {
     words w;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) w[k] = sizeof(T) == 4 ? __float_as_uint(v[i * PER + k]) : pack_bf16(v[2 * (i * PER + k) % N], v[(2 * (i * PER + k) + 1) % N]);
+    for (int k = 0; k < PER; ++k) w[k] = e.w[i * PER + k];
     words* at = reinterpret_cast<words*>(p) + i;
     if constexpr (STREAM) __builtin_nontemporal_store(w, at);
     else *at = w;
   }
+}
+template <bool STREAM, typename T, int N>
+__device__ __forceinline__ void put_whole(T* p, const float (&v)[N]) {
+  Piece<T, N> e;
+  make_piece(v, e);
+  put_piece<STREAM>(p, e);
 }
 // STREAM is no argument: of two branches that differ in the hint alone the compiler makes one without it
 template <bool STREAM = false, typename T, int N>
