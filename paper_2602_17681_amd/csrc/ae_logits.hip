@@ -3,7 +3,8 @@
 // A workgroup takes a slice of a row.  Every column of the slice has a word in LDS: how often the token was answered, whether
 // it occurred at all, and which bias it has.  The row's history and list of biases are read by each slice (they are short
 // beside it, and in the cache), then the slice passes through registers once.  Bound by memory: 333 x 50 021 in binary32 with mask, 777 tokens
-// of history and 5 biases 30.6 us (136 MB, 4.5 TB/s; rows begin on any 4-byte border), 256 x 131 072 in bfloat16 36 us; four rows 5.2 us.
+// of history and 5 biases 29.3 us (136 MB, 4.7 TB/s); 256 x 131 072 in bfloat16 without lists 25 us, with 1 024 tokens of history, 16 biases and mask 34, with
+// 8 192 tokens 46 (with one of a thread's tokens asked for after the other 53); four rows 4.3 us.
 #include <hip/hip_runtime.h>
 
 #include "ae_device.h"
@@ -16,7 +17,7 @@ namespace {
 constexpr int NT = 512;
 // a column's word: bits 0 .. 19 how often among the answers, bit 20 in the prompt, bits 21 .. 31 place in the list of biases + 1
 constexpr uint32_t kCount = (1u << 20) - 1, kPrompt = 1u << 20, kSeen = kCount | kPrompt;
-constexpr int AHEAD = 4;                         // tokens of the history that a thread asks for at once
+constexpr int AHEAD = 4;                          // tokens of the history that a thread asks for at once
 constexpr int kBiasAt = 21, kMaxHistory = kCount, kMaxBias = 2047;
 
 struct AdjustArgs {
@@ -76,9 +77,13 @@ __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
     // the lists' first entries are asked for with the logits
     const int t = threadIdx.x, prompt = p.n_prompt ? p.n_prompt[row] : 0;
     const int bias0 = t < p.n_bias ? p.bias_id[row * p.n_bias + t] : -1;
+    const int* const history = p.history + row * p.n_history;
     int token[AHEAD];
+    auto ask = [&](int base) {
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) token[k] = k * NT + t < p.n_history ? p.history[row * p.n_history + k * NT + t] : -1;
+      for (int k = 0; k < AHEAD; ++k) token[k] = base + k * NT + t < p.n_history ? history[base + k * NT + t] : -1;
+    };
+    ask(0);
     for (int i = threadIdx.x; i < S / 4; i += NT) word4[i] = make_uint4(0, 0, 0, 0);
     if (p.repetition) repetition = p.repetition[row];
     if (p.presence) presence = p.presence[row];
@@ -99,9 +104,11 @@ __global__ __launch_bounds__(NT) void k_logits_adjust(AdjustArgs p) {
       for (int i = t + NT; i < p.n_bias; i += NT) set_bias(i, p.bias_id[row * p.n_bias + i]);
       __syncthreads();
     }
+    for (int base = 0; base < p.n_history; base += AHEAD * NT) {
+      if (base) ask(base);
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) count(k * NT + t, token[k]);
-    for (int i = AHEAD * NT + t; i < p.n_history; i += NT) count(i, p.history[row * p.n_history + i]);
+      for (int k = 0; k < AHEAD; ++k) count(base + k * NT + t, token[k]);
+    }
     __syncthreads();
   }
   const bool in_place = p.logits == p.out;
@@ -156,8 +163,8 @@ template <typename T>
 int launch_adjust_rows(const AdjustArgs& p, hipStream_t s) {
   constexpr int E = sizeof(T) / 2;               // pieces for 4 096 columns
   if (!p.n_history && !p.n_bias) return launch_adjust<T, 2 * E, false>(p, s);
-  // slices of 4 096 columns where they are fewer than 1 024: 4 rows of 131 072 5.2 us (8 192 columns 5.6), 64 of 50 021 8.7 (9.9), 32 of
-  // 131 072 7.3 (7.2), 128 of 131 072 23 (21), 128 of 50 021 14.6 (13.8), 512 of 32 000 25 (21); 2 048 columns and 256 threads 333 x 50 021 40, 37 with 8 192 and 512
+  // slices of 4 096 columns where they are fewer than 1 024, as measured when 4 rows of 131 072 took 5.2 us (8 192 columns 5.6): 64 of 50 021 8.7
+  // (9.9), 32 of 131 072 7.3 (7.2), 128 of 131 072 23 (21), 128 of 50 021 14.6 (13.8), 512 of 32 000 25 (21); 333 x 50 021 by 256 threads 40 (2 048 columns), 38 (4 096), 48 (8 192), by 512 37
   if (p.rows * ((p.vocab + 4095) / 4096) < 1024) return launch_adjust<T, E, true>(p, s);
   return launch_adjust<T, 2 * E, true>(p, s);
 }
