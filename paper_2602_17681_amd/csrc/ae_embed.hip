@@ -4,9 +4,11 @@
 // list into runs of equal length and adds up each run's rows: a token that fills half the batch takes as many workgroups
 // as its places need, and what a token has in several runs is joined in their order.
 // Both are bound by memory.  16 384 tokens of 4 096 bfloat16 columns, tokens as in text: the lookup 27 us (repeated rows come from the
-// cache; its results written as a stream, 39 without), the gradient over 32 768 tokens of vocabulary 149 us: sort 9.7, sums beside the zeros of 27 000 tokens that do not
-// occur 133 (690 MB at 5.2 TB/s), join 6.
+// cache; its results written as a stream, 39 without), the gradient over 32 768 tokens of vocabulary 141 us: sort 9.5, sums and the zeros of 27 000 tokens that do not
+// occur 126 (690 MB at 5.5 TB/s), join 5.7.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "ae_device.h"
 #include "ae_internal.h"
@@ -206,6 +208,7 @@ struct EmbedGrad {
   float* d_table;
   int64_t ldt;
   int accumulate;
+  bool stream;                            // the table is large, and whole lines are written
   int* owner;                             // [runs]: the token that begins in a run and goes on behind it, or -1
   float* part;                            // [runs][2][d]: a run's share of a token that begins before it, of one that goes on behind it
 };
@@ -228,13 +231,18 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
   constexpr int TEAM = 64 * W, TEAMS = 4 / W;
   if ((int)blockIdx.x >= p.sums) {
     const int lane = threadIdx.x & 63, v0 = ((int)blockIdx.x - p.sums) * ZERO_ROWS, v = v0 + lane;
-    uint64_t todo = __ballot(lane < ZERO_ROWS && v < p.vocab && (!p.sort.start || p.sort.start[v] == p.sort.start[v + 1]));
-    const float zero[4] = {0, 0, 0, 0};
-    while (todo) {
-      float* at = p.d_table + (int64_t)(v0 + __ffsll((unsigned long long)todo) - 1) * p.ldt;
-      for (int col = threadIdx.x * 4; col < p.d; col += 1024) put(at + col, p.d - col, zero);
-      todo &= todo - 1;
-    }
+    const uint64_t todo = __ballot(lane < ZERO_ROWS && v < p.vocab && (!p.sort.start || p.sort.start[v] == p.sort.start[v + 1]));
+    // a large table's zeros as a stream: 16 384 tokens into 32 768 x 4 096 149 us without, 141 with, its sums too 150; 6 022 tokens into
+    // 22 088 x 4 555, whose rows begin on 4-byte borders, 120 without and 124 with
+    auto write = [&](auto stream) {
+      const float zero[4] = {0, 0, 0, 0};
+      for (uint64_t left = todo; left; left &= left - 1) {
+        float* at = p.d_table + (int64_t)(v0 + __ffsll((unsigned long long)left) - 1) * p.ldt;
+        for (int col = threadIdx.x * 4; col < p.d; col += 1024) put<stream>(at + col, p.d - col, zero);
+      }
+    };
+    if (p.stream) write(std::true_type());
+    else write(std::false_type());
     return;
   }
   const int t = threadIdx.x % TEAM, lane = threadIdx.x & 63;
@@ -382,7 +390,7 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __res
     }
     __syncthreads();
     const float zero[4] = {0, 0, 0, 0};
-    for (int v = 0; v < rows; ++v) {
+    for (int v = 0; v < rows; ++v) {               // (500 tokens into 24 576 x 4 096 81 us, as a stream 84: nothing beside them)
       if (there[v]) continue;
       float* at = p.d_table + (int64_t)(v0 + v) * p.ldt;
       for (int col = threadIdx.x * 4; col < p.d; col += 1024) put(at + col, p.d - col, zero);
@@ -450,7 +458,8 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __res
 }
 
 // Wavefronts and four-column pieces of a lane that share a run, and from them its positions: at least 16, and as many as leave
-// 1 024 workgroups (16 384 x 4 096 150 us, with 2 048 148 and twice the workspace; 16 positions always 228: more partial sums).
+// 1 024 workgroups (16 384 x 4 096 150 us, with 2 048 148 and twice the workspace; 16 positions always 228: more partial sums; all before the
+// zeros went as a stream).
 int team_of(int64_t d) { return d <= 512 ? 1 : 4; }
 int pieces_of(int64_t d) { return d > 256 && d <= 512 ? 2 : 1; }
 int64_t run_of(int64_t n, int64_t d) {
@@ -566,7 +575,8 @@ extern "C" int model_embedding_backward(const void* d_out, int64_t ldo, const in
     return AE_OK;
   }
   char* ws = (char*)workspace;
-  EmbedGrad p = {d_out, ldo, {}, (int)vocab, (int)d, (int)run_of(n, d), n, runs_of(n, d), 0, 0, scale, d_table, ldt, accumulate ? 1 : 0, nullptr, nullptr};
+  EmbedGrad p = {d_out, ldo, {}, (int)vocab, (int)d, (int)run_of(n, d), n, runs_of(n, d), 0, 0, scale, d_table, ldt, accumulate ? 1 : 0,
+                 vocab * d * 4 > kStreamBytes && ldt % 4 == 0 && ((uintptr_t)d_table & 15) == 0, nullptr, nullptr};
   if (n == 0) return launch_embed_sums<float>(p, s);       // zeros alone
   if (n <= FEW) return dtype == AE_BF16 ? launch_embed_few<bf16_t>(p, ids, s) : launch_embed_few<float>(p, ids, s);
   p.sort.place = (int*)ws;

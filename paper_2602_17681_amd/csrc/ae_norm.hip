@@ -121,12 +121,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
   const int t = threadIdx.x % LANES, team = threadIdx.x / LANES, step = (int)gridDim.x * TEAMS;
   const T* x = (const T*)p.x;
   const T* res = (const T*)p.residual;
-  Eight<float> w[NV];
-  if (p.weight) {
+  constexpr bool LATE = NV > 2;                  // the weights behind the sum: two workgroups to a compute unit
+  Eight<float> w[LATE ? 1 : NV];
+  if (!LATE && p.weight) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) fetch_row<false, SHORT>(p.weight, (v * LANES + t) * 8, p.d, w[v]);
+    for (int v = 0; v < NV; ++v) fetch_row<false, SHORT>(p.weight, (v * LANES + t) * 8, p.d, w[LATE ? 0 : v]);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) settle<SHORT>((v * LANES + t) * 8, p.d, w[v]);
+    for (int v = 0; v < NV; ++v) settle<SHORT>((v * LANES + t) * 8, p.d, w[LATE ? 0 : v]);
   }
   int turn = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < p.rows; row0 += step, turn ^= 1) {
@@ -183,8 +184,12 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = h[v][j] * r;
       if (p.weight) {
+        if (LATE) {
+          fetch_row<false, SHORT>(p.weight, (v * LANES + t) * 8, p.d, w[0]);
+          settle<SHORT>((v * LANES + t) * 8, p.d, w[0]);
+        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= value(w[v], j);
+        for (int j = 0; j < 8; ++j) y[j] *= value(w[LATE ? 0 : v], j);
       }
       emit<T, LANES>(p, row, live ? (v * LANES + t) * 8 : p.d, y);
     }
@@ -244,8 +249,8 @@ int launch_norm_row(const NormArgs& p, hipStream_t s) {
   return launch_status("rms_norm");
 }
 // Lanes by the row's length.  524 288 x 64 in bfloat16 8 lanes 44 us, 16 lanes 86; 262 144 x 128 16 lanes 43, 64 lanes 116; 131 072 x 256 32 lanes 43, 64 lanes 60;
-// 16 384 x 4 096 256 lanes of two pieces 81, 512 of one 83, 64 of eight 155; 1 677 x 20 000 read twice 71, 1 024 lanes of four pieces (which
-// spill) 147.
+// 16 384 x 4 096 256 lanes of two pieces 81, 512 of one 83, 64 of eight 155; 2 730 x 12 288 512 lanes of three
+// pieces 50, 1 024 of two 58, of which only one workgroup fits into a compute unit; 1 677 x 20 000 read twice 71, 1 024 lanes of four pieces (which spill) 147.
 template <typename T>
 int launch_norm(const NormArgs& p, hipStream_t s) {
   if (p.d <= 64) return launch_norm_row<T, 8, 1>(p, s);
@@ -256,7 +261,8 @@ int launch_norm(const NormArgs& p, hipStream_t s) {
   if (p.d <= 2048) return launch_norm_row<T, 256, 1>(p, s);
   if (p.d <= 4096) return launch_norm_row<T, 256, 2>(p, s);
   if (p.d <= 8192) return launch_norm_row<T, 512, 2>(p, s);
-  if (p.d <= 16384) return launch_norm_row<T, 1024, 2>(p, s);
+  if (p.d <= 12288) return launch_norm_row<T, 512, 3>(p, s);
+  if (p.d <= 16384) return launch_norm_row<T, 512, 4>(p, s);
   const int64_t most = 512;
   hipLaunchKernelGGL((k_rms_norm_wide<T>), dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(WIDE), 0, s, p);
   return launch_status("rms_norm");
@@ -504,12 +510,14 @@ __global__ __launch_bounds__(1024) void k_sum_parts(const float* __restrict__ pa
   if (k == 0 && (int)blockIdx.x * 16 + c < d) out[blockIdx.x * 16 + c] = acc;
 }
 
-constexpr int kInRegisters = 8192;                 // columns of a row, beside its gradient and the sums of the weight's
+// columns of a row that registers hold beside its gradient, the next row and the sums of the weight's (four binary32 pieces spill: 1 024 x
+// 16 384 60 us, in two passes 44)
+int64_t in_registers(int dtype) { return dtype == AE_BF16 ? 16384 : 12288; }
 // workgroups of a launch, each with a part of the weight's gradient: as many as the registers of 256 compute units hold.  16.8 M elements in
-// bfloat16, us with 256 / 512 / 1 024: rows of 512 50 / 32 / 33, of 2 048 55 / 36 / 35, of 4 096 33 / 32 / 39, of 8 192 33 / 39 / 50.  Rows from 8 193 on
-// in two passes 49 (12 288) and 44 (16 384), in 1 024 lanes' registers 110 and 103.
-int64_t grad_groups(int64_t rows, int64_t d) {
-  if (d > kInRegisters) return rows < 64 ? rows : 64;
+// bfloat16, us with 256 / 512 / 1 024: rows of 512 50 / 32 / 33, of 2 048 55 / 36 / 35, of 4 096 33 / 32 / 39, of 8 192 33 / 39 / 50.  Rows of
+// 12 288 and 16 384 in 512 lanes 35 and 36, in two passes 50 and 44, in 1 024 lanes without the next row 110 and 103.
+int64_t grad_groups(int64_t rows, int64_t d, int dtype) {
+  if (d > in_registers(dtype)) return rows < 64 ? rows : 64;
   const int64_t teams = d <= 64 ? 32 : d <= 128 ? 16 : d <= 256 ? 8 : d <= 1024 ? 4 : 1;
   const int64_t want = (rows + teams - 1) / teams, most = d <= 512 || (d > 1024 && d <= 2048) ? 1024 : d <= 4096 ? 512 : 256;
   return want < most ? want : most;
@@ -530,7 +538,10 @@ int launch_grad(const NormGradArgs& p, int64_t groups, hipStream_t s) {
   if (p.d <= 1024) return launch_grad_row<T, 64, 2>(p, groups, s);
   if (p.d <= 2048) return launch_grad_row<T, 256, 1>(p, groups, s);
   if (p.d <= 4096) return launch_grad_row<T, 256, 2>(p, groups, s);
-  if (p.d <= kInRegisters) return launch_grad_row<T, 512, 2>(p, groups, s);
+  if (p.d <= 8192) return launch_grad_row<T, 512, 2>(p, groups, s);
+  if (p.d <= 12288) return launch_grad_row<T, 512, 3>(p, groups, s);
+  if constexpr (sizeof(T) == 2)
+    if (p.d <= 16384) return launch_grad_row<T, 512, 4>(p, groups, s);
   hipLaunchKernelGGL((k_rms_norm_stat<T>), dim3((unsigned)(p.rows < 512 ? p.rows : 512)), dim3(WIDE), 0, s, p);
   hipLaunchKernelGGL((k_rms_norm_grad_columns<T>), dim3((unsigned)((p.d + 2047) / 2048), (unsigned)groups), dim3(256), 0, s, p);
   return launch_status("rms_norm_backward");
@@ -580,7 +591,7 @@ extern "C" int model_rms_norm_backward_workspace(int64_t rows, int64_t d, int dt
   using namespace ae;
   if (!bytes) return fail(AE_EINVAL, "model_rms_norm_backward_workspace: null argument");
   AE_TRY(check_norm("model_rms_norm_backward_workspace", rows, d, 1.0f, dtype));
-  *bytes = align16(grad_groups(rows, d) * d * 4) + (d > kInRegisters ? rows * 16 : 0);
+  *bytes = align16(grad_groups(rows, d, dtype) * d * 4) + (d > in_registers(dtype) ? rows * 16 : 0);
   return AE_OK;
 }
 
@@ -596,7 +607,7 @@ extern "C" int model_rms_norm_backward(const void* dy, int64_t ldy, const void* 
   AE_TRY(model_rms_norm_backward_workspace(rows, d, dtype, &need));
   if (need && (!workspace || ((uintptr_t)workspace & 15))) return fail(AE_EINVAL, "model_rms_norm_backward: workspace is null or not on a 16-byte border");
   hipStream_t s = (hipStream_t)stream;
-  const int64_t groups = grad_groups(rows, d);
+  const int64_t groups = grad_groups(rows, d, dtype);
   if (rows > 0) {
     if (!dy || !h) return fail(AE_EINVAL, "model_rms_norm_backward: null argument");
     if (!rows_ok(dy, ldy, d, dtype) || !rows_ok(h, ldh, d, dtype) || !rows_ok(d_h, ldg, d, dtype) || !rows_ok(dx, lddx, d, dtype))

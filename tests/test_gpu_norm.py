@@ -17,9 +17,9 @@ TINY = 1e-37                     # where binary32 ends
 
 #        rows, d: one piece, parts of one, each number of wavefronts to a row, its borders, rows that are read twice
 SIZES = [(1, 1), (3, 7), (37, 8), (70, 57), (33, 64), (34, 65), (5, 128), (4, 511), (7, 513), (1, 1024), (33, 1003), (9, 2047), (2, 2049), (1, 4096), (130, 4096), (3, 4100), (3, 8192), (2, 8200),
-         (2, 16384), (3, 20001), (2, 32768), (2, 32776), (1, 70001)]
+         (3, 12288), (2, 12291), (2, 16384), (3, 16386), (3, 20001), (2, 32768), (2, 32776), (1, 70001)]
 #        more rows than teams of the launch
-MANY = [(40000, 50), (33001, 64), (9001, 130), (8200, 1000), (2500, 1100), (2300, 4096), (1100, 5000), (600, 9000), (600, 17000), (530, 33000)]
+MANY = [(40000, 50), (33001, 64), (9001, 130), (8200, 1000), (2500, 1100), (2300, 4096), (1100, 5000), (600, 9000), (560, 13001), (600, 17000), (530, 33000)]
 
 
 def rel(d):

@@ -68,6 +68,19 @@ def test_embedding_of_more_tokens_than_one_launch_takes():
         assert torch.equal(b[:, 0], want)
 
 
+@pytest.mark.parametrize("d", [2056, 3001])
+def test_embedding_of_calls_that_write_as_a_stream(d):
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    n, vocab = 20000, 700
+    table = torch.randn((vocab, d), device="cuda").to(torch.bfloat16)
+    ids = torch.randint(-1, vocab + 1, (n,), device="cuda", dtype=torch.int32)
+    out = torch.empty((n, d), dtype=torch.bfloat16, device="cuda")
+    ae.model_embedding(table, vocab, d, ids, n, out, scale=1.25)
+    want = torch.where(((ids >= 0) & (ids < vocab))[:, None], (table.float() * 1.25).to(torch.bfloat16)[ids.clamp(0, vocab - 1).long()], torch.zeros((), dtype=torch.bfloat16, device="cuda"))
+    assert torch.equal(out, want)
+
+
 def test_embedding_and_gradient_beyond_32_bits():
     import torch
     from paper_2602_17681_amd import binding as ae
