@@ -225,7 +225,7 @@ __device__ __forceinline__ void add_row(const EmbedGrad& p, int v, int col, cons
 // W wavefronts add up the rows of a run of sorted places, NV times four neighbouring columns to a lane (16 bytes of the result, so
 // that a wavefront's stores are whole lines).  The workgroups behind `sums` write the zeros of tokens that do not occur (among the sums,
 // one for one: 228 us against 162, since every second workgroup is on the same four of the eight dies; by eights 166 against 150).
-constexpr int ZERO_ROWS = 4;                     // (embed gradient above 150 us with 4 rows or 2, 152 with 16)
+constexpr int ZERO_ROWS = 4;                     // (embed gradient above 150 us with 4 rows or 2, 152 with 16; beside the join instead of the sums no faster)
 template <typename T, int W, int NV, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedGrad p) {
   constexpr int TEAM = 64 * W, TEAMS = 4 / W;
@@ -413,7 +413,8 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGrad p, const int* __res
     if (id[k] == v) places[wave][count + __popcll(m & (((uint64_t)1 << lane) - 1))] = k * 64 + lane;
     count += __popcll(m);
   }
-  if (__builtin_amdgcn_readfirstlane(places[wave][0]) != mine) return;         // written by this wavefront alone, in order
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // the list is written and read by this wavefront alone
+  if (__builtin_amdgcn_readfirstlane(places[wave][0]) != mine) return;
   constexpr int U = NV * sizeof(T) > 4 ? 8 : 16;               // rows in flight
   const bool edge = __any(c0 + (NV - 1) * TEAM * 4 > p.d - 4);   // the rows' end lies in this wavefront's columns
   float acc[NV][4];
