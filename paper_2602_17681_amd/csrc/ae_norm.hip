@@ -197,8 +197,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
 }
 
 // Rows that registers do not hold are read twice; each element's results are written by the thread that reads it, behind
-// its second read, so that h may take the place of x or of the residual here too.  1 677 x 20 000 72 us, 670 x 50 021 88; with
-// four pieces of a thread in flight 80 and 93 (512 threads), three 75 and 96, two 82 and 91: fewer wavefronts fit.
+// its second read, so that h may take the place of x or of the residual here too.  1 676 x 20 000 72 us, 670 x 50 021 88; with
+// more pieces of a thread in flight fewer wavefronts fit: 512 threads of four 80 and 93, of two 70 and 95, 1 024 of three 75 and 96, of two 82 and 91.
 constexpr int WIDE = 1024;
 template <typename T>
 __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
@@ -251,7 +251,7 @@ int launch_norm_row(const NormArgs& p, hipStream_t s) {
 }
 // Lanes by the row's length.  524 288 x 64 in bfloat16 8 lanes 44 us, 16 lanes 86; 262 144 x 128 16 lanes 43, 64 lanes 116; 131 072 x 256 32 lanes 43, 64 lanes 60;
 // 16 384 x 4 096 256 lanes of two pieces 81, 512 of one 83, 64 of eight 155; 2 730 x 12 288 512 lanes of three
-// pieces 50, 1 024 of two 58, of which only one workgroup fits into a compute unit; 1 677 x 20 000 read twice 71, 1 024 lanes of four pieces (which spill) 147.
+// pieces 50, 1 024 of two 58, of which only one workgroup fits into a compute unit; 1 676 x 20 000 read twice 72, 1 024 lanes of four pieces (which spill) 147.
 template <typename T>
 int launch_norm(const NormArgs& p, hipStream_t s) {
   if (p.d <= 64) return launch_norm_row<T, 8, 1>(p, s);
