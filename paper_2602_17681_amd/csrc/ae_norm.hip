@@ -3,8 +3,9 @@
 //   g = dy w,   u = h r:   dh = d_h + r (g - u mean(g u)),   dw = sum over rows of dy u
 // Both are bound by memory: a row is read once and stays in registers between its sum and its results.  16 384 x 4 096 in bfloat16 with
 // residual into codes 80 us (472 MB, 5.9 TB/s); the adjoint of 4 096 x 4 096 with the residual path's gradient 29.4 us (134 MB,
-// 4.6 TB/s, of which the sum of the weight's gradient over workgroups 4 us).  Sums are binary32.  A row whose sum of squares leaves binary32's range
-// (|h| from 2^60 on) is multiplied by 2^-100 first, in its registers: exact, and u does not change.
+// 4.6 TB/s, of which the sum of the weight's gradient over workgroups 4 us).  Sums are binary32.  Where a row's sum of squares leaves binary32's range
+// (|h| from 2^54 on), that of h 2^-100 is taken instead: what becomes subnormal there has no part in it.  The row itself stays as it is, since its
+// small elements would lose bits: u = (h r) 2^-100 with the r of that sum, and h r is at most 2^100 sqrt(d).
 #include <hip/hip_runtime.h>
 #include <float.h>
 
@@ -107,7 +108,7 @@ __device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, co
   }
 }
 
-// 1 / sqrt(mean + eps) of a row; down: of the row times 2^-100, whose mean is so large that eps plays no part
+// 1 / sqrt(mean + eps) of a row; down: of the row times 2^-100, whose mean was so large that eps plays no part
 __device__ __forceinline__ float rms_inverse(float sum, int d, float eps, bool down) { return 1.0f / sqrtf(sum / (float)d + (down ? 0.0f : eps)); }
 
 // LANES lanes hold a row in NV pieces of eight elements each; a workgroup has 256 / LANES rows at a time, or one, and many
@@ -163,16 +164,14 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
     }
     sum = team_sum<LANES>(sum, sm[turn]);
     const bool down = !(sum <= FLT_MAX);           // the same in all threads of the row
-    if (LANES <= 64 ? __any(down) : down) {        // of several rows in a wavefront the others are multiplied by one
-      const float by = down ? kDown : 1.0f;
+    const bool any = LANES <= 64 ? __any(down) : down;
+    const float by = down ? kDown : 1.0f;          // of several rows in a wavefront the others are multiplied by one
+    if (any) {
       sum = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          h[v][j] *= by;
-          sum = fmaf(h[v][j], h[v][j], sum);
-        }
+        for (int j = 0; j < 8; ++j) sum = fmaf(h[v][j] * by, h[v][j] * by, sum);
       if constexpr (LANES > 64) __syncthreads();
       sum = team_sum<LANES>(sum, sm[2]);
       if constexpr (LANES > 64) __syncthreads();
@@ -183,6 +182,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
       float y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = h[v][j] * r;
+      if (any) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] *= by;
+      }
       if (p.weight) {
         if (LATE) {
           fetch_row<false, SHORT>(p.weight, (v * LANES + t) * 8, p.d, w[0]);
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_wide(NormArgs p) {
       if (p.weight) numbers(p.weight + col, p.d - col, w);
       if (p.h && col < p.d) put((T*)p.h + row * p.ldh + col, p.d - col, h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = (down ? h[j] * kDown : h[j]) * r * w[j];
+      for (int j = 0; j < 8; ++j) y[j] = (down ? h[j] * r * kDown : h[j] * r) * w[j];
       emit<T, WIDE>(p, row, col, y);
     }
     __syncthreads();
