@@ -300,6 +300,8 @@ __device__ __forceinline__ RowStat row_stat(float hh, float gh, int d, float eps
   const float r = rms_inverse(hh, d, eps, down);
   return {r, down ? kDown : 1.0f, far ? kDown : 1.0f, r * gh / (float)d};
 }
+// whether g h has to be added up again with smaller g: the sum, or the sum times r, leaves binary32 (a row whose squares leave it has an r of its own later)
+__device__ __forceinline__ bool far_sum(float hh, float gh, int d, float eps) { return !(fabsf(gh) * fmaxf(1.0f, rms_inverse(hh, d, eps, false)) <= FLT_MAX); }
 // the gradient of h; of the powers of two only what is left of both is taken out, at the end
 __device__ __forceinline__ float norm_grad(const RowStat& s, float dy, float w, float u) {
   const float tail = s.less == 1.0f ? s.down : s.down * kUp;
@@ -372,7 +374,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
       }
     };
     sums(sm[turn]);
-    const bool down = !(hh <= FLT_MAX), far = !(fabsf(gh) <= FLT_MAX);
+    const bool down = !(hh <= FLT_MAX), far = far_sum(hh, gh, p.d, p.eps);
     if (LANES <= 64 ? __any(down || far) : down || far) {      // of several rows in a wavefront the others are multiplied by one
       const float by = down ? kDown : 1.0f, less = far ? kDown : 1.0f;
       hh = gh = 0.0f;
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
     sums(1.0f, 1.0f);
     hh = team_sum<WIDE>(hh, sm[0]);
     gh = team_sum<WIDE>(gh, sm[1]);
-    const bool down = !(hh <= FLT_MAX), far = !(fabsf(gh) <= FLT_MAX);
+    const bool down = !(hh <= FLT_MAX), far = far_sum(hh, gh, p.d, p.eps);
     if (down || far) {
       sums(down ? kDown : 1.0f, far ? kDown : 1.0f);
       hh = team_sum<WIDE>(hh, sm[2]);
