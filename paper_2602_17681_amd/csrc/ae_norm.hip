@@ -4,8 +4,8 @@
 // Both are bound by memory: a row is read once and stays in registers between its sum and its results.  16 384 x 4 096 in bfloat16 with
 // residual into codes 80 us (472 MB, 5.9 TB/s); the adjoint of 4 096 x 4 096 with the residual path's gradient 29.4 us (134 MB,
 // 4.6 TB/s, of which the sum of the weight's gradient over workgroups 4 us).  Sums are binary32.  Where a row's sum of squares leaves binary32's range
-// (|h| from 2^54 on), that of h 2^-100 is taken instead: what becomes subnormal there has no part in it.  The row itself stays as it is, since its
-// small elements would lose bits: u = (h r) 2^-100 with the r of that sum, and h r is at most 2^100 sqrt(d).
+// (|h| from 2^54 on), that of h 2^-76 is taken instead: what becomes subnormal there has no part in it.  The row itself stays as it is, since its
+// small elements would lose bits: u = (h r) 2^-76 with the r of that sum, and h r is at most 2^76 sqrt(d).
 #include <hip/hip_runtime.h>
 #include <float.h>
 
@@ -17,8 +17,7 @@
 namespace ae {
 namespace {
 
-constexpr float kDown = 7.8886090522101181e-31f;   // 2^-100
-constexpr float kUp = 1.2676506002282294e30f;       // 2^100
+constexpr float kDown = 1.3234889800848443e-23f;   // 2^-76
 
 // eight elements as numbers, zeros behind the row's end
 template <typename T>
@@ -108,7 +107,7 @@ __device__ __forceinline__ void emit(const NormArgs& p, int64_t row, int col, co
   }
 }
 
-// 1 / sqrt(mean + eps) of a row; down: of the row times 2^-100, whose mean was so large that eps plays no part
+// 1 / sqrt(mean + eps) of a row; down: of the row times 2^-76, whose mean was so large that eps plays no part
 __device__ __forceinline__ float rms_inverse(float sum, int d, float eps, bool down) { return 1.0f / sqrtf(sum / (float)d + (down ? 0.0f : eps)); }
 
 // LANES lanes hold a row in NV pieces of eight elements each; a workgroup has 256 / LANES rows at a time, or one, and many
@@ -287,25 +286,37 @@ struct NormGradArgs {
   void* dx;
   int64_t lddx;
   float* part;                            // [workgroups][d]: each one's sum of dy u over its rows; null: not wanted
-  float* stat;                            // [rows][4], rows that registers do not hold
+  struct RowStat* stat;                   // [rows], rows that registers do not hold
   bool stream;
 };
 
-// u = h times down times r, where down is 1, or 2^-100 if the sum of h^2 leaves binary32; likewise g is taken times less
-// if the sum of g h does, and mean is that of such g
+// What a row's gradients take:  u = h r down,   dh = d_h + (dy part w - u mean) t.  In an ordinary row down and part are 1, t is r and mean that of g u.
+// Two kinds of rows have their sums taken once more, of h times by and g times scale:
+//   down  the sum of h^2 leaves binary32: by = down = 2^-76, and r is that of h 2^-76
+//   far   r times the sum of g h leaves 2^90, or the sum itself binary32 (in all other rows the part along h is less than the rounding of binary32's largest number):
+//         scale = 2^-90
+// In such rows `part` has (most of) r in it, so that what is subnormal on the way is so in the result, and what leaves the range, too.
 struct RowStat {
-  float r, down, less, mean;
+  float r, down, part, mean, t;
 };
-__device__ __forceinline__ RowStat row_stat(float hh, float gh, int d, float eps, bool down, bool far) {
-  const float r = rms_inverse(hh, d, eps, down);
-  return {r, down ? kDown : 1.0f, far ? kDown : 1.0f, r * gh / (float)d};
-}
-// whether g h has to be added up again with smaller g: the sum, or the sum times r, leaves binary32 (a row whose squares leave it has an r of its own later)
-__device__ __forceinline__ bool far_sum(float hh, float gh, int d, float eps) { return !(fabsf(gh) * fmaxf(1.0f, rms_inverse(hh, d, eps, false)) <= FLT_MAX); }
-// the gradient of h; of the powers of two only what is left of both is taken out, at the end
-__device__ __forceinline__ float norm_grad(const RowStat& s, float dy, float w, float u) {
-  const float tail = s.less == 1.0f ? s.down : s.down * kUp;
-  return (dy * s.less * w - u * s.mean) * s.r * tail;
+constexpr float kFar = 1.2379400392853803e27f;        // 2^90
+struct Again {
+  bool down, far;
+  __device__ __forceinline__ Again(float hh, float gh, float r) {
+    down = !(hh <= FLT_MAX);
+    far = !(fabsf(r * gh) <= kFar && fabsf(gh) <= FLT_MAX);
+  }
+  __device__ __forceinline__ bool any() const { return down || far; }
+  __device__ __forceinline__ float by() const { return down ? kDown : 1.0f; }
+  __device__ __forceinline__ float scale() const { return far ? 1.0f / kFar : 1.0f; }
+};
+__device__ __forceinline__ RowStat row_stat(float gh, float r, int d) { return {r, 1.0f, 1.0f, r * gh / (float)d, r}; }
+// from the second sums
+__device__ __forceinline__ RowStat row_stat(const Again& a, float hh, float gh, int d, float eps) {
+  const float r = rms_inverse(hh, d, eps, a.down), c = gh / (float)d * r;            // mean(g u) times scale
+  // r = part t but for down: 2^-64 2^-12 there, and where h is as it is min(r, 1) 2^-12 and max(r, 1) 2^12
+  const float part = a.down ? r * 5.4210108624275222e-20f : fminf(r, 1.0f) * 0.000244140625f, t = a.down ? 0.000244140625f : fmaxf(r, 1.0f) * 4096.0f;
+  return {r, a.by(), part, a.far ? c * (part * kFar) : c * part, t};
 }
 
 template <typename T, int LANES, int NV, bool STREAM>
@@ -374,32 +385,33 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
       }
     };
     sums(sm[turn]);
-    const bool down = !(hh <= FLT_MAX), far = far_sum(hh, gh, p.d, p.eps);
-    if (LANES <= 64 ? __any(down || far) : down || far) {      // of several rows in a wavefront the others are multiplied by one
-      const float by = down ? kDown : 1.0f, less = far ? kDown : 1.0f;
+    const float r1 = rms_inverse(hh, p.d, p.eps, false);
+    RowStat st = row_stat(gh, r1, p.d);
+    const Again again(hh, gh, r1);
+    if (LANES <= 64 ? __any(again.any()) : again.any()) {      // of several rows in a wavefront the others keep what they have
+      const float by = again.by(), scale = again.scale();
       hh = gh = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          h[v][j] *= by;
-          hh = fmaf(h[v][j], h[v][j], hh);
-          gh = fmaf(dy[v][j] * less * w[v][j], h[v][j], gh);
+          hh = fmaf(h[v][j] * by, h[v][j] * by, hh);
+          gh = fmaf(dy[v][j] * scale * w[v][j], h[v][j] * by, gh);
         }
       if constexpr (LANES > 64) __syncthreads();
       sums(sm[2]);
       if constexpr (LANES > 64) __syncthreads();
+      if (again.any()) st = row_stat(again, hh, gh, p.d, p.eps);
     }
-    const RowStat st = row_stat(hh, gh, p.d, p.eps, down, far);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int col = (v * LANES + t) * 8;
       float o[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float u = h[v][j] * st.r;
+        const float u = h[v][j] * st.r * st.down;
         if (live) acc[v][j] = fmaf(dy[v][j], u, acc[v][j]);
-        o[j] = norm_grad(st, dy[v][j], w[v][j], u) + add[v][j];
+        o[j] = (dy[v][j] * st.part * w[v][j] - u * st.mean) * st.t + add[v][j];
       }
       if (p.dx && live && col < p.d) put((T*)p.dx + row * p.lddx + col, p.d - col, o);
     }
@@ -435,7 +447,7 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
   __shared__ float sm[4][WIDE / 64];
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     float hh, gh;
-    auto sums = [&](float by, float less) {
+    auto sums = [&](float by, float scale) {
       hh = gh = 0.0f;
       for (int col = threadIdx.x * 8; col < p.d; col += WIDE * 8) {
         float h[8], g[8], w[8];
@@ -446,24 +458,23 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
         for (int j = 0; j < 8; ++j) {
           h[j] *= by;
           hh = fmaf(h[j], h[j], hh);
-          gh = fmaf(p.weight ? g[j] * less * w[j] : g[j] * less, h[j], gh);
+          gh = fmaf(p.weight ? g[j] * scale * w[j] : g[j] * scale, h[j], gh);
         }
       }
     };
     sums(1.0f, 1.0f);
     hh = team_sum<WIDE>(hh, sm[0]);
     gh = team_sum<WIDE>(gh, sm[1]);
-    const bool down = !(hh <= FLT_MAX), far = far_sum(hh, gh, p.d, p.eps);
-    if (down || far) {
-      sums(down ? kDown : 1.0f, far ? kDown : 1.0f);
+    const float r = rms_inverse(hh, p.d, p.eps, false);
+    RowStat st = row_stat(gh, r, p.d);
+    const Again again(hh, gh, r);
+    if (again.any()) {
+      sums(again.by(), again.scale());
       hh = team_sum<WIDE>(hh, sm[2]);
       gh = team_sum<WIDE>(gh, sm[3]);
+      st = row_stat(again, hh, gh, p.d, p.eps);
     }
-    const RowStat st = row_stat(hh, gh, p.d, p.eps, down, far);
-    if (threadIdx.x == 0) {
-      float* at = p.stat + row * 4;
-      at[0] = st.r; at[1] = st.down; at[2] = st.less; at[3] = st.mean;
-    }
+    if (threadIdx.x == 0) p.stat[row] = st;
     __syncthreads();
   }
 }
@@ -477,16 +488,16 @@ __global__ __launch_bounds__(256) void k_rms_norm_grad_columns(NormGradArgs p) {
   for (int j = 0; j < 8; ++j) { w[j] = 1.0f; acc[j] = 0.0f; }
   if (p.weight) numbers(p.weight + col, left, w);
   for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
-    const RowStat st = {p.stat[row * 4], p.stat[row * 4 + 1], p.stat[row * 4 + 2], p.stat[row * 4 + 3]};
+    const RowStat st = p.stat[row];
     float h[8], dy[8], add[8], o[8];
     numbers((const T*)p.h + row * p.ldh + col, left, h);
     numbers((const T*)p.dy + row * p.ldy + col, left, dy);
     if (p.d_h) numbers((const T*)p.d_h + row * p.ldg + col, left, add);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float u = h[j] * st.down * st.r;
+      const float u = h[j] * st.r * st.down;
       acc[j] = fmaf(dy[j], u, acc[j]);
-      o[j] = norm_grad(st, dy[j], w[j], u) + (p.d_h ? add[j] : 0.0f);
+      o[j] = (dy[j] * st.part * w[j] - u * st.mean) * st.t + (p.d_h ? add[j] : 0.0f);
     }
     if (p.dx) put((T*)p.dx + row * p.lddx + col, left, o);
   }
@@ -597,7 +608,7 @@ extern "C" int model_rms_norm_backward_workspace(int64_t rows, int64_t d, int dt
   using namespace ae;
   if (!bytes) return fail(AE_EINVAL, "model_rms_norm_backward_workspace: null argument");
   AE_TRY(check_norm("model_rms_norm_backward_workspace", rows, d, 1.0f, dtype));
-  *bytes = align16(grad_groups(rows, d, dtype) * d * 4) + (d > in_registers(dtype) ? rows * 16 : 0);
+  *bytes = align16(grad_groups(rows, d, dtype) * d * 4) + (d > in_registers(dtype) ? align16(rows * (int64_t)sizeof(RowStat)) : 0);
   return AE_OK;
 }
 
@@ -622,7 +633,7 @@ extern "C" int model_rms_norm_backward(const void* dy, int64_t ldy, const void* 
       return fail(AE_EINVAL, "model_rms_norm_backward: a gradient in an input's place has its stride");
     NormGradArgs p = {dy, ldy, h, ldh, weight, d_h, ldg, rows, (int)d, eps, dx, lddx, nullptr, nullptr, rows * d * (int64_t)dtype_size(dtype) * (2 + !!d_h + !!dx) > kStreamBytes};
     if (d_weight) p.part = (float*)workspace;
-    p.stat = (float*)((char*)workspace + align16(groups * d * 4));
+    p.stat = (RowStat*)((char*)workspace + align16(groups * d * 4));
     AE_TRY(dtype == AE_BF16 ? launch_grad<bf16_t>(p, groups, s) : launch_grad<float>(p, groups, s));
   }
   if (d_weight) hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, s, (const float*)workspace, groups, (int)d, d_weight);

@@ -59,3 +59,70 @@ def test_the_sum_of_products_just_inside_the_range(d, rms, spread, dtype):
     dx = to.rms_norm_backward(dy, h, None, 1e-9)[0]
     dy *= np.minimum(1.0, 0.9 * LARGEST / np.maximum(np.abs(dx), np.abs(dy)).max(1, keepdims=True))
     check(dy.astype(np.float32), h.astype(np.float32), None, 1e-9, dtype, neighbours=(0, 2, 3, 6))
+
+
+@pytest.mark.parametrize("d", [2, 64] + WIDTHS)
+def test_large_gradients_of_large_rows(d):
+    """One element of 2^64, gradients of 2^90 elsewhere: the gradient of h is 2^26 sqrt(d)."""
+    h, dy = np.zeros((3, d), np.float32), np.ones((3, d), np.float32)
+    h[0, 0] = h[2, d - 1] = 2.0 ** 64
+    h[1] = 1.0
+    dy[0, 1] = 2.0 ** 90
+    dy[2, 0] = -2.0 ** 120
+    check(dy, h, None, 1e-6, neighbours=(1,))
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_small_gradients_beside_large_ones(d):
+    """Where the sum of products leaves the range, columns with h = 0 keep gradients of 10^-20 and 10^-30."""
+    rng = np.random.default_rng(d)
+    h = rng.standard_normal((6, d)).astype(np.float32)
+    dy = rng.standard_normal((6, d)).astype(np.float32)
+    for i in (0, 3):
+        h[i] = np.sign(h[i]) * (0.5 + np.abs(h[i]))
+        dy[i] = np.sign(h[i]) * np.float32(2e38 / d * 8)
+        h[i, 1:3] = 0
+        dy[i, 1], dy[i, 2] = 1e-20, -1e-30
+    check(dy, h, None, 1e-6, neighbours=(1, 2, 4, 5))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_rows_of_large_and_small_elements(d, dtype):
+    """Rows beyond the range of squares with elements of 10^-15 in them, and gradients of every size; the weight's gradient of the small ones."""
+    rng = np.random.default_rng(d)
+    h = rng.standard_normal((5, d))
+    dy = rng.standard_normal((5, d))
+    h[1] *= 1e-15
+    h[1, 0] = 2.0 ** 65
+    h[2, : d // 2] *= 1e20
+    dy[2] *= 1e10
+    h[4] *= 1e-10
+    h[4, d - 1] = 3e38
+    dy[4] *= 1e25
+    dy[[0, 3]] = 0                              # the weight's gradient is that of these rows
+    check(dy.astype(np.float32), h.astype(np.float32), (1 + 0.2 * rng.standard_normal(d)).astype(np.float32), 1e-6, dtype, d_h=(rng.standard_normal((5, d)) * (rng.random((5, d)) < 0.5)).astype(np.float32), neighbours=(0, 3))
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_products_with_the_weight_beyond_the_range(d):
+    """dy times weight beyond binary32, whose product with 1 / rms is not; beside h = 0, too."""
+    rng = np.random.default_rng(d)
+    h = (rng.standard_normal((4, d)) * 1e12).astype(np.float32)
+    dy = rng.standard_normal((4, d)).astype(np.float32)
+    w = np.full(d, 1e6, np.float32)
+    dy[1] *= np.float32(1e34)
+    dy[2, 3] = 1e37
+    h[2, 3] = 0
+    check(dy, h, w, 1e-6, neighbours=(0, 3))
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_differences_near_the_largest_number(d):
+    """The largest gradients against a part along h of the other sign, rms 10: their difference is beyond binary32, a tenth of it is not."""
+    rng = np.random.default_rng(d)
+    h = (10 * np.sign(rng.standard_normal((3, d)))).astype(np.float32)
+    dy = rng.standard_normal((3, d)).astype(np.float32)
+    dy[1] = np.sign(h[1]) * np.float32(3.3e38)
+    dy[1, 0] *= -1
+    check(dy, h, None, 1e-6, neighbours=(0, 2))
