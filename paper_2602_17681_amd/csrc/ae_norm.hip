@@ -291,28 +291,33 @@ struct NormGradArgs {
 };
 
 // What a row's gradients take:  u = h r down,   dh = d_h + (dy part w - u mean) t.  In an ordinary row down and part are 1, t is r and mean that of g u.
-// Two kinds of rows have their sums taken once more, of h times by and g times scale:
+// Three kinds of rows have their sums taken once more, of h times by and g times scale:
 //   down  the sum of h^2 leaves binary32: by = down = 2^-76, and r is that of h 2^-76
 //   far   r times the sum of g h leaves 2^90, or the sum itself binary32 (in all other rows the part along h is less than the rounding of binary32's largest number):
 //         scale = 2^-90
-// In such rows `part` has (most of) r in it, so that what is subnormal on the way is so in the result, and what leaves the range, too.
+//   near  r is large and the sum of g h so small that products in it are subnormal: scale = 2^60
+// In rows of the first two kinds `part` has (most of) r in it, so that what is subnormal on the way is so in the result, and what leaves the range, too.
 struct RowStat {
   float r, down, part, mean, t;
 };
 constexpr float kFar = 1.2379400392853803e27f;        // 2^90
+constexpr float kNear = 7.8886090522101181e-31f;      // 2^-100
+constexpr float kMore = 1.1529215046068470e18f;       // 2^60
 struct Again {
-  bool down, far;
+  bool down, far, near;
   __device__ __forceinline__ Again(float hh, float gh, float r) {
     down = !(hh <= FLT_MAX);
     far = !(fabsf(r * gh) <= kFar && fabsf(gh) <= FLT_MAX);
+    near = hh > 0.0f && r > 1024.0f && fabsf(gh) < kNear;
   }
-  __device__ __forceinline__ bool any() const { return down || far; }
+  __device__ __forceinline__ bool any() const { return down || far || near; }
   __device__ __forceinline__ float by() const { return down ? kDown : 1.0f; }
-  __device__ __forceinline__ float scale() const { return far ? 1.0f / kFar : 1.0f; }
+  __device__ __forceinline__ float scale() const { return far ? 1.0f / kFar : near ? kMore : 1.0f; }
 };
 __device__ __forceinline__ RowStat row_stat(float gh, float r, int d) { return {r, 1.0f, 1.0f, r * gh / (float)d, r}; }
-// from the second sums
-__device__ __forceinline__ RowStat row_stat(const Again& a, float hh, float gh, int d, float eps) {
+// from the second sums; first: that of an ordinary row.  Large products that cancel leave the range in 2^60 of them: then there is nothing subnormal to lose
+__device__ __forceinline__ RowStat row_stat(const Again& a, float hh, float gh, int d, float eps, const RowStat& first) {
+  if (a.near) return fabsf(gh) <= FLT_MAX ? RowStat{first.r, 1.0f, 1.0f, first.r * gh / (float)d * (1.0f / kMore), first.r} : first;
   const float r = rms_inverse(hh, d, eps, a.down), c = gh / (float)d * r;            // mean(g u) times scale
   // r = part t but for down: 2^-64 2^-12 there, and where h is as it is min(r, 1) 2^-12 and max(r, 1) 2^12
   const float part = a.down ? r * 5.4210108624275222e-20f : fminf(r, 1.0f) * 0.000244140625f, t = a.down ? 0.000244140625f : fmaxf(r, 1.0f) * 4096.0f;
@@ -401,7 +406,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
       if constexpr (LANES > 64) __syncthreads();
       sums(sm[2]);
       if constexpr (LANES > 64) __syncthreads();
-      if (again.any()) st = row_stat(again, hh, gh, p.d, p.eps);
+      if (again.any()) st = row_stat(again, hh, gh, p.d, p.eps, st);
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -472,7 +477,7 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
       sums(again.by(), again.scale());
       hh = team_sum<WIDE>(hh, sm[2]);
       gh = team_sum<WIDE>(gh, sm[3]);
-      st = row_stat(again, hh, gh, p.d, p.eps);
+      st = row_stat(again, hh, gh, p.d, p.eps, st);
     }
     if (threadIdx.x == 0) p.stat[row] = st;
     __syncthreads();

@@ -126,3 +126,21 @@ def test_differences_near_the_largest_number(d):
     dy[1] = np.sign(h[1]) * np.float32(3.3e38)
     dy[1, 0] *= -1
     check(dy, h, None, 1e-6, neighbours=(0, 2))
+
+
+@pytest.mark.parametrize("size", [1e-21, 1e-24, 1e-27])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_products_below_the_range(d, size):
+    """h, gradients and eps so small that the products of h and the gradients are subnormal or zero, while gradient over rms is ordinary."""
+    rng = np.random.default_rng(d)
+    h = (rng.standard_normal((6, d)) * 1e-19).astype(np.float32)
+    dy = (rng.standard_normal((6, d)) * size).astype(np.float32)
+    dy[2] = np.sign(h[2]) * np.float32(10 * size)
+    h[3] = 0
+    h[4], dy[4] = np.abs(h[4, 0]), 0                       # large products that cancel
+    dy[4, 0], dy[4, 1] = 1e20, -1e20
+    h[4, 2], dy[4, 2] = 0, 1e10
+    dy[5] = np.abs(dy[5]) * np.sign(h[5])
+    h[5, ::3] = np.abs(h[5, ::3])
+    dy[5, ::3] = 0                                         # nothing but the part along h there
+    check(dy, h, None, 2.0 ** -125)
