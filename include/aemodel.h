@@ -503,9 +503,10 @@ int model_loss_distill(const void* logits, int64_t rows, int64_t vocab, int64_t 
  * model_grad_clip  grads: `count` device tensors of sizes[k] elements in dtypes[k]; the four arrays are HOST memory and
  *   read during the call (a captured call keeps the addresses in it).
  *     *norm = sqrt(sum of all squares)  (binary32, device, nullable; squares are added up in binary64)
- *     out[k] = grads[k] * min(1, max_norm / norm), rounded once
- *   out null: the norm alone.  out[k] = grads[k] clips in place, and writes nothing if norm <= max_norm.  Where the norm is
- *   infinite or NaN nothing is scaled: out has the gradients as they are.  max_norm > 0 (infinity: never clip).  No output may overlap another, or
+ *     out[k] = grads[k] * min(1, max_norm / norm)  (quotient and product in binary64, rounded to binary32, and from there to bfloat16)
+ *   out null: the norm alone.  out[k] = grads[k] clips in place, and writes nothing if norm <= max_norm.  Where an element is infinite or
+ *   NaN the norm is, too, and nothing is scaled: out has the gradients as they are.  Finite gradients are clipped also where their norm is beyond binary32; *norm is
+ *   infinite then, and all elements of out are finite.  max_norm > 0 (infinity: never clip).  No output may overlap another, or
  *   another's gradient.  Tensors of size 0 may be null.
  *
  * model_logits_adjust  for every row of logits z [rows][vocab], in this order and in binary32, rounded once:

@@ -86,8 +86,9 @@ __global__ __launch_bounds__(NT) void k_grad_squares(GradArgs p, double* __restr
   if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
 
+// The product is binary64's and rounded once: max_norm / norm may be less than any binary32 number while the product is an ordinary one.
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const T* p, T* out, int64_t left, float factor) {
+__device__ __forceinline__ void chunk_scale(const T* p, T* out, int64_t left, double factor) {
   Piece<T, VEC<T>> e[PIECES<T>];
   chunk_load<T, true>(p, left, e);
 #pragma unroll
@@ -95,7 +96,7 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* out, int64_t left, fl
     const int at = (u * NT + (int)threadIdx.x) * VEC<T>;
     float v[VEC<T>];
 #pragma unroll
-    for (int j = 0; j < VEC<T>; ++j) v[j] = value(e[u], j) * factor;
+    for (int j = 0; j < VEC<T>; ++j) v[j] = (float)((double)value(e[u], j) * factor);
     if (left >= CHUNK) put_whole<true>(out + at, v);
     else if (left > at) put(out + at, (int)left - at, v);
   }
@@ -115,13 +116,14 @@ __global__ __launch_bounds__(NT) void k_grad_scale(GradArgs p, const double* __r
   for (int i = threadIdx.x; i < parts; i += NT) sum += part[i];
   const double all = sqrt(block_sum<NT>(sum, sm));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
-  // a norm that is no number, or infinite, scales nothing
-  const float factor = all > (double)max_norm && all <= DBL_MAX ? (float)((double)max_norm / all) : 1.0f;
+  // no number or infinite: an element is; nothing is scaled.  Finite gradients whose norm binary32 does not hold are
+  const double factor = all > (double)max_norm && all <= DBL_MAX ? (double)max_norm / all : 1.0;
+  const bool same = (float)factor == 1.0f;         // from 1 - 2^-25 on every product rounds to its gradient
   const int from = share(p, blockIdx.x), to = share(p, blockIdx.x + 1);
   int k = from < to ? tensor_of(p, to - 1) : 0;
   for (int c = to - 1; c >= from; --c) {           // backwards: what the first pass read last is still in the cache
     while (k > 0 && c < p.end[k - 1]) --k;
-    if (factor == 1.0f && p.in[k] == p.out[k]) continue;
+    if (same && p.in[k] == p.out[k]) continue;
     const int64_t at = (int64_t)(c - (k ? p.end[k - 1] : 0)) * CHUNK, left = p.size[k] - at;
     if (p.bf16[k]) chunk_scale((const bf16_t*)p.in[k] + at, (bf16_t*)p.out[k] + at, left, factor);
     else chunk_scale((const float*)p.in[k] + at, (float*)p.out[k] + at, left, factor);

@@ -1,0 +1,75 @@
+"""Clipping by norms that binary32 does not hold, and by factors that it does not.
+
+Bounds.  The factor is a quotient in binary64, the product is rounded to binary32 once: U, and 2^-150 where it is subnormal; to bfloat16 from there: 2^-8."""
+import numpy as np
+import pytest
+
+from oracle import token_oracle as to
+from token_util import HALF, U, dev, host, near, space, td
+
+pytestmark = pytest.mark.gpu
+ONCE = U * (1 + 2.0 ** -20)
+
+
+def run(ae, grads, max_norm, out):
+    import torch
+    lst, norm = ae.GradList(grads, out), torch.full((1,), 5.0, device="cuda")
+    ae.model_grad_clip(lst, max_norm, norm, space(ae.model_grad_clip_workspace(lst)))
+    return norm.item()
+
+
+def bound(want, dtype):
+    return (ONCE if dtype == "f32" else HALF["bf16"] + U) * np.abs(want) + (2.0 ** -150 if dtype == "f32" else 2.0 ** -134) * 1.001
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("size,max_norm", [(3e38, 1e-3), (3e38, 1.0), (1e38, 1e-37), (1e30, 1e-10), (1e25, 1e-20), (1e10, 1e-30), (3e38, 3e38)])
+def test_factors_below_binary32(size, max_norm, in_place, dtype):
+    """max_norm / norm is subnormal or less; clipped gradients are as exact as any.  A norm beyond binary32 reads as infinity and clips all the same."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(3)
+    g = [host(dev((size * rng.uniform(-1, 1, n)).astype(np.float32), dtype)) for n in (1, 1000, 9001)]
+    g[0][0] = host(dev(np.float32([size]), dtype))[0]
+    norm, want = to.grad_clip(g, float(np.float32(max_norm)))
+    ts = [dev(v, dtype) for v in g]
+    out = ts if in_place else [torch.empty_like(t) for t in ts]
+    got = run(ae, ts, max_norm, out)
+    assert abs(got - norm) <= 1.001 * U * norm if norm < 3.4e38 else got == np.inf
+    for o, w in zip(out, want):
+        near(host(o), w, bound(w, dtype))
+    assert abs(host(out[1])).max() > 0 or max_norm < 1e-36
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_one_rounding(dtype):
+    """Factor and product are not rounded to binary32 one after the other."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(7)
+    g = host(dev(rng.standard_normal(200000).astype(np.float32), dtype))
+    norm, (want,) = to.grad_clip([g], float(np.float32(0.7)))
+    out = torch.empty(200000, dtype=td(dtype), device="cuda")
+    run(ae, [dev(g, dtype)], 0.7, [out])
+    near(host(out), want, bound(want, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norms_next_to_the_largest(dtype):
+    """Lists clipped to a norm just below their own, by factors within 2^-25 of one and further off: elsewhere and in place alike."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(11)
+    g = [host(dev((2.0 ** np.arange(-20, 20).repeat(50) * (1 + rng.integers(0, 2 ** 23, 2000) * 2.0 ** -23)).astype(np.float32), dtype))]
+    norm, _ = to.grad_clip(g, 1.0)
+    for steps in (1, 2, 3, 8, 1000):
+        limit = float(np.float32(norm))
+        for _ in range(steps):
+            limit = float(np.nextafter(np.float32(limit), np.float32(0)))
+        _, (want,) = to.grad_clip(g, limit)
+        a, out = dev(g[0], dtype), torch.empty(2000, dtype=td(dtype), device="cuda")
+        run(ae, [a], limit, [out])
+        near(host(out), want, bound(want, dtype))
+        run(ae, [a], limit, [a])
+        assert torch.equal(a, out)
