@@ -1,4 +1,4 @@
-"""Clipping by norms that binary32 does not hold, and by factors that it does not.
+"""Clipping by norms that binary32 does not hold, by factors that it does not, and lists at the border of a launch.
 
 Bounds.  The factor is a quotient in binary64, the product is rounded to binary32 once: U, and 2^-150 where it is subnormal; to bfloat16 from there: 2^-8."""
 import numpy as np
@@ -73,3 +73,35 @@ def test_norms_next_to_the_largest(dtype):
         near(host(out), want, bound(want, dtype))
         run(ae, [a], limit, [a])
         assert torch.equal(a, out)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "both"])
+@pytest.mark.parametrize("full", [127, 128, 129, 256, 257, 1000])
+def test_lists_at_the_border_of_a_launch(full, kind):
+    """As many tensors as a launch takes, and one more or less, with tensors of no elements before, at and behind the border."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(full)
+    for empty_at in ((), (0,), (full,), (127, 128), (126, 127, 128, 129, full)):
+        sizes, at = [], 0
+        for i in range(full + 1):
+            sizes += [0] * empty_at.count(i)
+            if i < full:
+                sizes.append(int(rng.integers(1, 40)) if i != full - 1 else 8193)
+        dtypes = [("f32", "bf16")[i % 2] if kind == "both" else kind for i in range(len(sizes))]
+        bufs = {t: torch.full((sum(sizes) + 64 * len(sizes),), 77.0, device="cuda").to(td(t)) for t in ("f32", "bf16")}
+        g = [host(dev(rng.standard_normal(n).astype(np.float32), t)) for n, t in zip(sizes, dtypes)]
+        ts, out, inside = [], [], {t: torch.zeros(b.shape, dtype=torch.bool, device="cuda") for t, b in bufs.items()}
+        for v, n, t in zip(g, sizes, dtypes):
+            ts.append(dev(v, t))
+            out.append(bufs[t][at:at + n])
+            inside[t][at:at + n] = True
+            at += n + int(rng.integers(0, 5))
+        norm, want = to.grad_clip(g, 1.0)
+        assert abs(run(ae, ts, 1.0, None) - norm) <= 1.001 * U * norm
+        assert abs(run(ae, ts, 1.0, out) - norm) <= 1.001 * U * norm
+        for o, w, t in zip(out, want, dtypes):
+            near(host(o), w, bound(w, t))
+        assert all(bool((b[~inside[t]] == 77).all()) for t, b in bufs.items())
+        assert abs(run(ae, ts, 1.0, ts) - norm) <= 1.001 * U * norm
+        assert all(torch.equal(a, b) for a, b in zip(ts, out))
