@@ -105,3 +105,28 @@ def test_lists_at_the_border_of_a_launch(full, kind):
         assert all(bool((b[~inside[t]] == 77).all()) for t, b in bufs.items())
         assert abs(run(ae, ts, 1.0, ts) - norm) <= 1.001 * U * norm
         assert all(torch.equal(a, b) for a, b in zip(ts, out))
+
+
+@pytest.mark.parametrize("count", [500, 640, 641, 1000, 5000])
+def test_long_lists(count):
+    """Dozens of launches, whose shares of the sum are added up once; replayed as a graph, too."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    from token_util import replayed
+    rng = np.random.default_rng(5)
+    sizes = [int(n) for n in rng.integers(1, 30, count - 1)] + [20000]
+    g = [rng.standard_normal(n).astype(np.float32) for n in sizes]
+    flat = dev(np.concatenate(g))
+    ts, res = list(flat.split(sizes)), torch.empty_like(flat)
+    out = list(res.split(sizes))
+    norm, want = to.grad_clip(g, 2.0)
+    assert abs(run(ae, ts, 2.0, out) - norm) <= 1.001 * U * norm
+    near(host(res), np.concatenate(want), bound(np.concatenate(want), "f32"))
+    lst, n = ae.GradList(ts, out), torch.empty(1, device="cuda")
+    ws = space(ae.model_grad_clip_workspace(lst))
+    first = flat.clone()
+    for i, got in enumerate(replayed(lambda: ae.model_grad_clip(lst, 2.0, n, ws), [n, res], lambda i: flat.copy_(first * (i + 1)))):
+        flat.copy_(first * (i + 1))
+        ae.model_grad_clip(lst, 2.0, n, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], n) and torch.equal(got[1], res)
