@@ -147,6 +147,7 @@ def _ptr(t, dtype=None):
 
 
 _current_device = torch._C._cuda_getDevice
+_stream_of = torch._C._cuda_getCurrentRawStream               # of a device: the current stream as a number
 
 
 def _raw_stream():
@@ -154,18 +155,21 @@ def _raw_stream():
     return torch._C._cuda_getCurrentRawStream(_current_device())
 
 
-def _raw_stream_for(device):
-    """The same, for tensors on this device: a call runs on the current one."""
+def _device(t):
+    """The device of a call, which is that of its first tensor and has to be the current one; its other tensors are held against it where they are looked at."""
+    device = t.get_device()
+    assert device >= 0, "device-resident tensor required"
     current = _current_device()
     assert device == current, "tensors on device %d, the current one is %d" % (device, current)
-    return torch._C._cuda_getCurrentRawStream(current)
+    return device
 
 
-def _mat(t, rows, cols, dtype=None):
-    """(data pointer, row stride) of a device matrix whose rows are contiguous; (null, 0) for None."""
+def _mat(t, rows, cols, dtype=None, device=None):
+    """(data pointer, row stride) of a matrix whose rows are contiguous, on this device or on any; (null, 0) for None."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.shape == (rows, cols), "device-resident [%d][%d] matrix required" % (rows, cols)
+    assert t.is_cuda if device is None else t.get_device() == device, "tensor on device %d, device %s required" % (t.get_device(), device)
+    assert t.shape == (rows, cols), "device-resident [%d][%d] matrix required" % (rows, cols)
     assert dtype is None or t.dtype is dtype, (t.dtype, dtype)
     ld, step = t.stride()
     if rows <= 1:
@@ -174,32 +178,34 @@ def _mat(t, rows, cols, dtype=None):
     return t.data_ptr(), ld
 
 
-def _codes(t, rows, cols):
+def _codes(t, rows, cols, device=None):
     """(data pointer, row stride in bytes) of a matrix of 8-bit codes (float8_e4m3fn or uint8); null for None."""
     if t is None:
         return None, 0
     assert t.dtype in _CODE_DTYPES, t.dtype
-    p, ld = _mat(t, rows, cols)
+    p, ld = _mat(t, rows, cols, None, device)
     if rows == 1:
         ld = -(-ld // 16) * 16
     assert ld == cols or rows == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= rows * ld, "all rows * stride bytes must be there"
     return p, ld
 
 
-def _vec(t, n, dtype=torch.float32):
+def _vec(t, n, dtype=torch.float32, device=None):
     """Data pointer of a contiguous device array of n elements; None for None."""
     if t is None:
         return None
-    assert t.is_cuda and t.dtype is dtype and t.numel() == n and t.is_contiguous(), "contiguous device array of %d %s required" % (n, dtype)
+    assert t.is_cuda if device is None else t.get_device() == device, "tensor on device %d, device %s required" % (t.get_device(), device)
+    assert t.dtype is dtype and t.numel() == n and t.is_contiguous(), "contiguous device array of %d %s required" % (n, dtype)
     return t.data_ptr()
 
 
-def _room(t, nbytes):
+def _room(t, nbytes, device=None):
     """Data pointer of a workspace of at least nbytes; None will do where none is needed."""
     if t is None:
         assert nbytes == 0, "a workspace of %d bytes is needed" % nbytes
         return None
-    assert t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes, "a workspace of %d bytes is needed" % nbytes
+    assert t.is_cuda if device is None else t.get_device() == device, "tensor on device %d, device %s required" % (t.get_device(), device)
+    assert t.is_contiguous() and t.numel() * t.element_size() >= nbytes, "a workspace of %d bytes is needed" % nbytes
     return t.data_ptr()
 
 
@@ -553,9 +559,9 @@ FP8_BLOCKS = {"rows": 0, "tiles": 1}
 FP8_BLOCK = 128
 
 
-def _fp8_scales(t, rows, cols, blocks):
+def _fp8_scales(t, rows, cols, blocks, device=None):
     rb, cb = -(-rows // FP8_BLOCK), -(-cols // FP8_BLOCK)
-    return _vec(t, cb * rows if blocks == "rows" else rb * cb)
+    return _vec(t, cb * rows if blocks == "rows" else rb * cb, device=device)
 
 
 def model_fp8_quantize(x, rows, cols, blocks, q=None, scale=None, qt=None, scale_t=None):
@@ -639,13 +645,14 @@ def model_loss_distill(logits, rows, vocab, top_id, top_logit, loss_rows, loss, 
 
 def model_rms_norm(x, rows, d, weight, eps, h=None, y=None, q=None, scale=None, residual=None):
     """h = x + residual; y = h / sqrt(mean h^2 + eps) * weight in x's type and / or as codes q with row blocks' scales (each output may be None)."""
+    dev = _device(x)
     xp, ldx = _mat(x, rows, d)
-    rp, ldr = _mat(residual, rows, d, x.dtype)
-    hp, ldh = _mat(h, rows, d, x.dtype)
-    yp, ldy = _mat(y, rows, d, x.dtype)
-    qp, ldq = _codes(q, rows, d)
-    _check(lib.model_rms_norm(xp, ldx, rp, ldr, _vec(weight, d), rows, d, eps, _dtype_of(x), hp, ldh, yp, ldy, qp, ldq,
-                              _fp8_scales(scale, rows, d, "rows"), _raw_stream_for(x.get_device())))
+    rp, ldr = _mat(residual, rows, d, x.dtype, dev)
+    hp, ldh = _mat(h, rows, d, x.dtype, dev)
+    yp, ldy = _mat(y, rows, d, x.dtype, dev)
+    qp, ldq = _codes(q, rows, d, dev)
+    _check(lib.model_rms_norm(xp, ldx, rp, ldr, _vec(weight, d, device=dev), rows, d, eps, _dtype_of(x), hp, ldh, yp, ldy, qp, ldq,
+                              _fp8_scales(scale, rows, d, "rows", dev), _stream_of(dev)))
 
 
 @functools.lru_cache(maxsize=1024)                # by sizes alone
@@ -657,20 +664,22 @@ def model_rms_norm_backward_workspace(rows, d, dtype):
 
 def model_rms_norm_backward(dy, h, rows, d, weight, eps, dx, d_weight, workspace, d_h=None):
     """Gradients of h (d_h, what arrives there from elsewhere, added) and of the weight; dx or d_weight may be None."""
+    dev = _device(dy)
     gp, ldy = _mat(dy, rows, d)
-    hp, ldh = _mat(h, rows, d, dy.dtype)
-    ap, lda = _mat(d_h, rows, d, dy.dtype)
-    dp, ldd = _mat(dx, rows, d, dy.dtype)
+    hp, ldh = _mat(h, rows, d, dy.dtype, dev)
+    ap, lda = _mat(d_h, rows, d, dy.dtype, dev)
+    dp, ldd = _mat(dx, rows, d, dy.dtype, dev)
     dtype = _dtype_of(dy)
-    _check(lib.model_rms_norm_backward(gp, ldy, hp, ldh, _vec(weight, d), ap, lda, rows, d, eps, dtype, dp, ldd, _vec(d_weight, d),
-                                       _room(workspace, model_rms_norm_backward_workspace(rows, d, dtype)), _raw_stream_for(dy.get_device())))
+    _check(lib.model_rms_norm_backward(gp, ldy, hp, ldh, _vec(weight, d, device=dev), ap, lda, rows, d, eps, dtype, dp, ldd, _vec(d_weight, d, device=dev),
+                                       _room(workspace, model_rms_norm_backward_workspace(rows, d, dtype), dev), _stream_of(dev)))
 
 
 def model_embedding(table, vocab, d, ids, n, out, scale=1.0):
     """out[i] = scale * table[ids[i]]; zeros for an id outside 0 .. vocab - 1."""
+    dev = _device(table)
     tp, ldt = _mat(table, vocab, d)
-    op, ldo = _mat(out, n, d, table.dtype)
-    _check(lib.model_embedding(tp, ldt, vocab, d, _vec(ids, n, torch.int32), n, scale, _dtype_of(table), op, ldo, _raw_stream_for(table.get_device())))
+    op, ldo = _mat(out, n, d, table.dtype, dev)
+    _check(lib.model_embedding(tp, ldt, vocab, d, _vec(ids, n, torch.int32, dev), n, scale, _dtype_of(table), op, ldo, _stream_of(dev)))
 
 
 @functools.lru_cache(maxsize=1024)                # by sizes alone
@@ -682,11 +691,12 @@ def model_embedding_backward_workspace(n, vocab, d, dtype):
 
 def model_embedding_backward(d_out, ids, n, vocab, d, d_table, workspace, scale=1.0, accumulate=False):
     """d_table[v] = scale * sum of d_out[i] with ids[i] = v, or added to what is there."""
+    dev = _device(d_out)
     gp, ldo = _mat(d_out, n, d)
-    tp, ldt = _mat(d_table, vocab, d, torch.float32)
+    tp, ldt = _mat(d_table, vocab, d, torch.float32, dev)
     dtype = _dtype_of(d_out)
-    _check(lib.model_embedding_backward(gp, ldo, _vec(ids, n, torch.int32), n, vocab, d, scale, dtype, tp, ldt, 1 if accumulate else 0,
-                                        _room(workspace, model_embedding_backward_workspace(n, vocab, d, dtype)), _raw_stream_for(d_table.get_device())))
+    _check(lib.model_embedding_backward(gp, ldo, _vec(ids, n, torch.int32, dev), n, vocab, d, scale, dtype, tp, ldt, 1 if accumulate else 0,
+                                        _room(workspace, model_embedding_backward_workspace(n, vocab, d, dtype), dev), _stream_of(dev)))
 
 
 class GradList:
@@ -719,23 +729,26 @@ def model_grad_clip_workspace(grads):
 
 def model_grad_clip(grads, max_norm, norm, workspace):
     """norm[0] = the norm of a GradList's gradients together; each times min(1, max_norm / norm) into its output (norm may be None)."""
-    _check(lib.model_grad_clip(grads._grads, grads._sizes, grads._dtypes, len(grads.grads), max_norm, _vec(norm, 1), grads._out,
-                               _room(workspace, grads.workspace_bytes), _raw_stream() if grads.device is None else _raw_stream_for(grads.device)))
+    dev = _current_device()
+    assert grads.device is None or grads.device == dev, "tensors on device %d, the current one is %d" % (grads.device, dev)
+    _check(lib.model_grad_clip(grads._grads, grads._sizes, grads._dtypes, len(grads.grads), max_norm, _vec(norm, 1, device=dev), grads._out,
+                               _room(workspace, grads.workspace_bytes, dev), _stream_of(dev)))
 
 
 def model_logits_adjust(logits, rows, vocab, out, history=None, n_prompt=None, repetition=None, presence=None, frequency=None, bias_id=None, bias=None,
                         allowed=None):
     """Penalties for the tokens of each row's history, biases of given tokens, -infinity where `allowed` has no bit; out may be logits."""
+    dev = _device(logits)
     zp, ld = _mat(logits, rows, vocab)
-    op, ldo = _mat(out, rows, vocab, logits.dtype)
+    op, ldo = _mat(out, rows, vocab, logits.dtype, dev)
     assert (history is None or history.dim() == 2) and (bias_id is None or bias_id.dim() == 2), "[rows][n] lists required"
     assert (bias_id is None) == (bias is None), "biases and their tokens go together"
     n_history = 0 if history is None else history.shape[1]
     n_bias = 0 if bias_id is None else bias_id.shape[1]
-    _check(lib.model_logits_adjust(zp, rows, vocab, ld, _dtype_of(logits), _vec(history, rows * n_history, torch.int32), n_history,
-                                   _vec(n_prompt, rows, torch.int32), _vec(repetition, rows), _vec(presence, rows), _vec(frequency, rows),
-                                   _vec(bias_id, rows * n_bias, torch.int32), _vec(bias, rows * n_bias), n_bias,
-                                   _vec(allowed, rows * -(-vocab // 32), torch.int32), op, ldo, _raw_stream_for(logits.get_device())))
+    _check(lib.model_logits_adjust(zp, rows, vocab, ld, _dtype_of(logits), _vec(history, rows * n_history, torch.int32, dev), n_history,
+                                   _vec(n_prompt, rows, torch.int32, dev), _vec(repetition, rows, device=dev), _vec(presence, rows, device=dev),
+                                   _vec(frequency, rows, device=dev), _vec(bias_id, rows * n_bias, torch.int32, dev), _vec(bias, rows * n_bias, device=dev), n_bias,
+                                   _vec(allowed, rows * -(-vocab // 32), torch.int32, dev), op, ldo, _stream_of(dev)))
 
 
 def model_calibrate_mfma(lds_reads, random_data=0, iters=4000):
