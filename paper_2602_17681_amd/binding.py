@@ -699,28 +699,46 @@ def model_embedding_backward(d_out, ids, n, vocab, d, d_table, workspace, scale=
                                         _room(workspace, model_embedding_backward_workspace(n, vocab, d, dtype), dev), _stream_of(dev)))
 
 
+_data_ptr = torch.Tensor.data_ptr
+
+
 class GradList:
     """Gradients that are clipped together, and where the clipped ones go: `out` None leaves the gradients alone (the norm only),
-    the same list puts them in their place.  Holds the tensors; made once for buffers that a program keeps."""
+    the same list puts them in their place.  Holds these tensors, for a program that keeps them from step to step: a call takes them as they are then (if
+    one was given other memory, the list is laid out again), a captured call as they were.  A gradient that a program has replaced by another tensor is not
+    in the list any more: gradients that are made anew every step need a list every step."""
 
     def __init__(self, grads, out=None):
-        grads = list(grads)
-        out = None if out is None else list(out)
-        for g in grads + (out or []):
-            assert g.is_cuda and g.is_contiguous() and g.dtype in (torch.float32, torch.bfloat16), "contiguous device tensors in float32 or bfloat16 required"
-        assert out is None or (len(out) == len(grads) and all(o.numel() == g.numel() and o.dtype == g.dtype for o, g in zip(out, grads))), \
+        self.grads, self.out = list(grads), None if out is None else list(out)
+        # in place: the same tensors
+        in_place = self.out is not None and len(self.out) == len(self.grads) and all(o is g for o, g in zip(self.out, self.grads))
+        self._tensors = self.grads if in_place else self.grads + (self.out or [])
+        self._lay_out()
+
+    def _lay_out(self):
+        grads, out, n = self.grads, self.out, len(self.grads)
+        self._where = None                                     # of a list that is refused: nowhere
+        for t in self._tensors:
+            assert t.is_cuda and t.is_contiguous() and t.dtype in (torch.float32, torch.bfloat16), "contiguous device tensors in float32 or bfloat16 required"
+        assert out is None or (len(out) == n and all(o.numel() == g.numel() and o.dtype == g.dtype for o, g in zip(out, grads))), \
             "as many outputs as gradients, of their sizes and types"
-        devices = {g.get_device() for g in grads + (out or [])}
+        devices = {t.get_device() for t in self._tensors}
         assert len(devices) <= 1, "tensors of one device required"
         self.device = devices.pop() if devices else None
-        self.grads, self.out, n = grads, out, len(grads)
-        self._grads = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
-        self._out = None if out is None else (C.c_void_p * n)(*[o.data_ptr() for o in out])
+        where = list(map(_data_ptr, self._tensors))
+        self._grads = (C.c_void_p * n)(*where[:n])
+        self._out = None if out is None else (C.c_void_p * n)(*where[-n:] if n else [])
         self._sizes = (C.c_int64 * n)(*[g.numel() for g in grads])
         self._dtypes = (C.c_int * n)(*[_dtype_of(g) for g in grads])
         b = C.c_int64()
         _check(lib.model_grad_clip_workspace(self._sizes, n, C.byref(b)))
         self.workspace_bytes = b.value
+        self._where = where
+
+    def _follow(self):
+        """Laid out again if a tensor lies elsewhere now (40 ns a tensor)."""
+        if list(map(_data_ptr, self._tensors)) != self._where:
+            self._lay_out()
 
 
 def model_grad_clip_workspace(grads):
@@ -729,6 +747,7 @@ def model_grad_clip_workspace(grads):
 
 def model_grad_clip(grads, max_norm, norm, workspace):
     """norm[0] = the norm of a GradList's gradients together; each times min(1, max_norm / norm) into its output (norm may be None)."""
+    grads._follow()
     dev = _current_device()
     assert grads.device is None or grads.device == dev, "tensors on device %d, the current one is %d" % (grads.device, dev)
     _check(lib.model_grad_clip(grads._grads, grads._sizes, grads._dtypes, len(grads.grads), max_norm, _vec(norm, 1, device=dev), grads._out,

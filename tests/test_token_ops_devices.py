@@ -1,4 +1,4 @@
-"""Every tensor of a call has to be on the current device; on the host, before any call into the library."""
+"""Every tensor of a call has to be on the current device, and a list of gradients is of where they lie now; on the host, before any call into the library."""
 import pytest
 import torch
 
@@ -92,3 +92,42 @@ def test_a_list_of_another_device_is_refused(ae):
     with pytest.raises(AssertionError):
         ae.GradList([on(0, D), on(1, D)])
     assert not ae.lib.calls
+
+
+def addresses(call):
+    return [None if call[1][i] is None else list(call[1][i]) for i in (0, 6)], list(call[1][1])
+
+
+def test_a_list_follows_its_tensors(ae):
+    """Tensors that were given other memory since the list was made: the call takes what they are now, or refuses it."""
+    g, o = [on(0, D), on(0, 8)], [on(0, D), on(0, 8)]
+    lst, norm, ws = ae.GradList(g, o), on(0, 1), on(0, 64, dtype=torch.uint8)
+    ae.model_grad_clip(lst, 1.0, norm, ws)
+    where = lambda ts: [t.data_ptr() for t in ts]      # noqa: E731
+    assert addresses(ae.lib.calls.pop()) == ([where(g), where(o)], [D, 8])
+    for k, ts in enumerate((g, o)):
+        before = ts[1].data_ptr()
+        ts[1].data = torch.ones(8)
+        assert ts[1].data_ptr() != before
+        ae.model_grad_clip(lst, 1.0, norm, ws)
+        assert addresses(ae.lib.calls.pop()) == ([where(g), where(o)], [D, 8])
+    for t in (g[0], o[0]):
+        t.data = torch.zeros(2 * D)
+    ae.model_grad_clip(lst, 1.0, norm, ws)
+    assert addresses(ae.lib.calls.pop()) == ([where(g), where(o)], [2 * D, 8])
+    g[0].data = torch.zeros(3 * D)                       # no longer of its output's size
+    with pytest.raises(AssertionError):
+        ae.model_grad_clip(lst, 1.0, norm, ws)
+    alone = ae.GradList(g)
+    g[1].data = torch.zeros(8)
+    ae.model_grad_clip(alone, 1.0, norm, ws)
+    assert addresses(ae.lib.calls.pop()) == ([where(g), None], [3 * D, 8])
+
+
+def test_a_list_in_place_follows_its_tensors(ae):
+    g = [on(0, D), on(0, 8)]
+    lst, norm, ws = ae.GradList(g, g), on(0, 1), on(0, 64, dtype=torch.uint8)
+    g[0].data = torch.zeros(D)
+    ae.model_grad_clip(lst, 1.0, norm, ws)
+    where = [t.data_ptr() for t in g]
+    assert addresses(ae.lib.calls.pop()) == ([where, where], [D, 8])
