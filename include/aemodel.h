@@ -491,11 +491,12 @@ int model_loss_distill(const void* logits, int64_t rows, int64_t vocab, int64_t 
  *   r = 1 / sqrt(mean h^2 + eps), u = h r, g = dy weight:
  *     dx = d_h + r (g - u mean(g u)),   d_weight_j = sum over the rows of dy_j u_j
  *   d_h [rows][d] (nullable): the gradient that reaches h on the residual path; dx is the gradient of x and of residual
- *   alike, it may be dy, h or d_h itself with the same stride.  dx or d_weight may be null.  Sums are binary32 in an order that depends on the sizes alone.
+ *   alike, it may be dy, h or d_h itself with the same stride.  dx or d_weight may be null.  Sums are binary32 in an order that depends on the
+ *   sizes and dtype alone; rows whose sums of squares or of g h leave binary32's range have their gradients like any other.
  *
  * model_embedding  out[i] = scale * table[ids[i]] (n rows of d, rounded once); ids int32, an id outside 0 .. vocab - 1 gives zeros.
  * model_embedding_backward  d_table[v] = scale * (sum of d_out[i] over all i with ids[i] = v, added in binary32 in an order
- *   that depends on ids alone), binary32 [vocab][d] with row stride ldt.  accumulate = 0: every row is written, zeros where no
+ *   that depends on ids, vocab and d alone), binary32 [vocab][d] with row stride ldt.  accumulate = 0: every row is written, zeros where no
  *   id is v; otherwise the sum is added to what is there, and rows without an id are left alone (a table that is the
  *   output layer's weight, too, has that layer's weight gradient there).  ids outside 0 .. vocab - 1 have no part.
  *   vocab and d up to 2^20, n up to 2^30.
