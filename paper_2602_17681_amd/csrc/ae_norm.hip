@@ -291,33 +291,36 @@ struct NormGradArgs {
 };
 
 // What a row's gradients take:  u = h r down,   dh = d_h + (dy part w - u mean) t.  In an ordinary row down and part are 1, t is r and mean that of g u.
-// Three kinds of rows have their sums taken once more, of h times by and g times scale:
-//   down  the sum of h^2 leaves binary32: by = down = 2^-76, and r is that of h 2^-76
+// Three kinds of rows have their sums taken once more, that of h^2 with h times by, that of g h with g times scale and h times lift:
+//   down  the sum of h^2 leaves binary32: by = lift = down = 2^-76, and r is that of h 2^-76
 //   far   r times the sum of g h leaves 2^90, or the sum itself binary32 (in all other rows the part along h is less than the rounding of binary32's largest number):
 //         scale = 2^-90
-//   near  r is large and the sum of g h so small that products in it are subnormal: scale = 2^60
-// In rows of the first two kinds `part` has (most of) r in it, so that what is subnormal on the way is so in the result, and what leaves the range, too.
+//   near  r is large and the sum of g h so small that products in it are subnormal: lift = 2^120 (h is less than 1 there)
+// In these rows `part` has (most of) r in it, so that what is subnormal on the way is so in the result, and what leaves the range, too.
 struct RowStat {
   float r, down, part, mean, t;
 };
 constexpr float kFar = 1.2379400392853803e27f;        // 2^90
 constexpr float kNear = 7.8886090522101181e-31f;      // 2^-100
-constexpr float kMore = 1.1529215046068470e18f;       // 2^60
+constexpr float kLift = 1.3292279957849159e36f;       // 2^120
 struct Again {
   bool down, far, near;
   __device__ __forceinline__ Again(float hh, float gh, float r) {
     down = !(hh <= FLT_MAX);
     far = !(fabsf(r * gh) <= kFar && fabsf(gh) <= FLT_MAX);
-    near = hh > 0.0f && r > 1024.0f && fabsf(gh) < kNear;
+    // products are off by 2^-150, u mean too, and a gradient by r^2 u or r times that: with u up to 2^5 below 2^-126 up to r = 2^10.  Where the sum of h^2 is 0, h is
+    // below 2^-75, and u below r 2^-75: up to r = 2^24.  So rows of zeros (padding) are ordinary for every eps from 2^-48 on
+    near = r > (hh > 0.0f ? 1024.0f : 16777216.0f) && fabsf(gh) < kNear;
   }
   __device__ __forceinline__ bool any() const { return down || far || near; }
   __device__ __forceinline__ float by() const { return down ? kDown : 1.0f; }
-  __device__ __forceinline__ float scale() const { return far ? 1.0f / kFar : near ? kMore : 1.0f; }
+  __device__ __forceinline__ float scale() const { return far ? 1.0f / kFar : 1.0f; }
+  __device__ __forceinline__ float lift() const { return near ? kLift : by(); }
 };
 __device__ __forceinline__ RowStat row_stat(float gh, float r, int d) { return {r, 1.0f, 1.0f, r * gh / (float)d, r}; }
-// from the second sums; first: that of an ordinary row.  Large products that cancel leave the range in 2^60 of them: then there is nothing subnormal to lose
+// from the second sums; first: that of an ordinary row.  Large products that cancel leave the range in 2^120 of them: then there is nothing subnormal to lose
 __device__ __forceinline__ RowStat row_stat(const Again& a, float hh, float gh, int d, float eps, const RowStat& first) {
-  if (a.near) return fabsf(gh) <= FLT_MAX ? RowStat{first.r, 1.0f, 1.0f, first.r * gh / (float)d * (1.0f / kMore), first.r} : first;
+  if (a.near) return fabsf(gh) <= FLT_MAX ? RowStat{first.r, 1.0f, first.r, gh / (float)d * first.r * (first.r * (1.0f / kLift)), 1.0f} : first;
   const float r = rms_inverse(hh, d, eps, a.down), c = gh / (float)d * r;            // mean(g u) times scale
   // r = part t but for down: 2^-64 2^-12 there, and where h is as it is min(r, 1) 2^-12 and max(r, 1) 2^12
   const float part = a.down ? r * 5.4210108624275222e-20f : fminf(r, 1.0f) * 0.000244140625f, t = a.down ? 0.000244140625f : fmaxf(r, 1.0f) * 4096.0f;
@@ -394,14 +397,14 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
     RowStat st = row_stat(gh, r1, p.d);
     const Again again(hh, gh, r1);
     if (LANES <= 64 ? __any(again.any()) : again.any()) {      // of several rows in a wavefront the others keep what they have
-      const float by = again.by(), scale = again.scale();
+      const float by = again.by(), scale = again.scale(), lift = again.lift();
       hh = gh = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           hh = fmaf(h[v][j] * by, h[v][j] * by, hh);
-          gh = fmaf(dy[v][j] * scale * w[v][j], h[v][j] * by, gh);
+          gh = fmaf(dy[v][j] * scale * w[v][j], h[v][j] * lift, gh);
         }
       if constexpr (LANES > 64) __syncthreads();
       sums(sm[2]);
@@ -448,11 +451,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm_grad(Nor
 
 // Rows that registers do not hold: the RowStat of every row first, then the gradients by columns.
 template <typename T>
-__global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
+__global__ __launch_bounds__(WIDE, 8) void k_rms_norm_stat(NormGradArgs p) {       // 64 registers: two workgroups to a compute unit
   __shared__ float sm[4][WIDE / 64];
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     float hh, gh;
-    auto sums = [&](float by, float scale) {
+    auto sums = [&](float by, float scale, float lift) {
       hh = gh = 0.0f;
       for (int col = threadIdx.x * 8; col < p.d; col += WIDE * 8) {
         float h[8], g[8], w[8];
@@ -461,20 +464,19 @@ __global__ __launch_bounds__(WIDE) void k_rms_norm_stat(NormGradArgs p) {
         if (p.weight) numbers(p.weight + col, p.d - col, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          h[j] *= by;
-          hh = fmaf(h[j], h[j], hh);
-          gh = fmaf(p.weight ? g[j] * scale * w[j] : g[j] * scale, h[j], gh);
+          hh = fmaf(h[j] * by, h[j] * by, hh);
+          gh = fmaf(p.weight ? g[j] * scale * w[j] : g[j] * scale, h[j] * lift, gh);
         }
       }
     };
-    sums(1.0f, 1.0f);
+    sums(1.0f, 1.0f, 1.0f);
     hh = team_sum<WIDE>(hh, sm[0]);
     gh = team_sum<WIDE>(gh, sm[1]);
     const float r = rms_inverse(hh, p.d, p.eps, false);
     RowStat st = row_stat(gh, r, p.d);
     const Again again(hh, gh, r);
     if (again.any()) {
-      sums(again.by(), again.scale());
+      sums(again.by(), again.scale(), again.lift());
       hh = team_sum<WIDE>(hh, sm[2]);
       gh = team_sum<WIDE>(gh, sm[3]);
       st = row_stat(again, hh, gh, p.d, p.eps, st);

@@ -144,3 +144,16 @@ def test_products_below_the_range(d, size):
     h[5, ::3] = np.abs(h[5, ::3])
     dy[5, ::3] = 0                                         # nothing but the part along h there
     check(dy, h, None, 2.0 ** -125)
+
+
+@pytest.mark.parametrize("size", [1e-21, 1e-24, 1e-27])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_products_below_the_range_of_rows_far_below_eps(d, size):
+    """h so far below the root of eps that u times mean(g u) is subnormal, too, though 1 / rms times it is ordinary; gradients in every second column."""
+    rng = np.random.default_rng(d)
+    h = (rng.standard_normal((4, d)) * 1e-26).astype(np.float32)
+    dy = (rng.standard_normal((4, d)) * size).astype(np.float32)
+    dy[1] = np.sign(h[1]) * np.float32(size)
+    dy[:, 1::2] = 0
+    dy[2, 1] = 1e-5
+    check(dy, h, None, 2.0 ** -125)
