@@ -130,3 +130,35 @@ def test_long_lists(count):
         ae.model_grad_clip(lst, 2.0, n, ws)
         torch.cuda.synchronize()
         assert torch.equal(got[0], n) and torch.equal(got[1], res)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_a_kept_list_follows_its_tensors(in_place):
+    """Gradients, and places of the clipped ones, that are given other memory between two calls: the old memory stays as it is."""
+    import torch
+    from paper_2602_17681_amd import binding as ae
+    rng = np.random.default_rng(2)
+    ts = [dev(rng.standard_normal(n).astype(np.float32)) for n in (5000, 3, 9000)]
+    out = ts if in_place else [torch.empty_like(t) for t in ts]
+    lst, norm = ae.GradList(ts, out), torch.empty(1, device="cuda")
+    ws = space(ae.model_grad_clip_workspace(lst))
+    for step in range(4):
+        if step:
+            old = [t.detach() for t in ts] + [o.detach() for o in out]
+            kept = [o.clone() for o in old]
+            g = [rng.standard_normal(t.numel()).astype(np.float32) for t in ts]
+            for k, t in enumerate(ts):
+                if step == 3 or k == step:
+                    t.data = dev(g[k])
+                else:
+                    t.copy_(dev(g[k]))
+            if not in_place and step == 2:
+                out[1].data = torch.full_like(out[1], 9.0)
+        h = [host(t) for t in ts]
+        want_norm, want = to.grad_clip(h, 1.0)
+        ae.model_grad_clip(lst, 1.0, norm, ws)
+        assert abs(norm.item() - want_norm) <= 1.001 * U * want_norm
+        for o, w in zip(out, want):
+            near(host(o), w, bound(w, "f32"))
+        if step == 3:
+            assert all(torch.equal(a, b) for a, b in zip(old[:3], kept[:3]))
