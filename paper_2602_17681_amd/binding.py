@@ -705,7 +705,7 @@ _data_ptr = torch.Tensor.data_ptr
 class GradList:
     """Gradients that are clipped together, and where the clipped ones go: `out` None leaves the gradients alone (the norm only),
     the same list puts them in their place.  Holds these tensors, for a program that keeps them from step to step: a call takes them as they are then (if
-    one was given other memory, the list is laid out again), a captured call as they were.  A gradient that a program has replaced by another tensor is not
+    one was given other memory, the list is laid out again; a change of size or type at the same address is not seen), a captured call as they were.  A gradient that a program has replaced by another tensor is not
     in the list any more: gradients that are made anew every step need a list every step."""
 
     def __init__(self, grads, out=None):
